@@ -595,6 +595,110 @@ mosaic_status mosaic_freivalds_check(int k, const uint32_t *a, const uint32_t *Y
                                      const uint32_t *Xp, int64_t ldx, uint32_t *bad,
                                      uint32_t *n_bad, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------ */
+/* Key/value cache of a decode step (Sec. 3.2 "Local attention computation": */
+/* attention stays on the trusted side, so its cache does too).              */
+/* ------------------------------------------------------------------------ */
+/* Element types of cached keys and values. */
+typedef enum { MOSAIC_KV_F32 = 0, MOSAIC_KV_BF16 = 1, MOSAIC_KV_F16 = 2 } mosaic_kv_type;
+
+/* A paged cache.  The pool holds `pages` pages of page_size slots for each of
+ * kv_heads heads; slot `o` of page `p`, head `h` starts at element
+ * p page_stride + h head_stride + o slot_stride of k and of v (both have the
+ * same strides), head_dim contiguous elements.  Slot s of sequence i lies in
+ * page table[i ld_table + s / page_size] at offset s % page_size, the same for
+ * every head.  position and weight (each pages x kv_heads x page_size,
+ * contiguous) may be NULL where an operation does not need them: the ordinal
+ * position of the token in a slot, and the attention weight that the slot has
+ * gathered so far.
+ * head_dim: a multiple of 8, 8..256.  page_size: 1..65536.  table_cols
+ * page_size < 2^31.  k, v and the three strides in bytes: multiples of 16.
+ * The struct is a host struct of device pointers, read during the call only.
+ * Kernels check every slot against table_cols and every page id against
+ * `pages`: a slot without a page is skipped when written and masked when read.
+ * Pages that are written (by any call) must belong to one sequence; pages
+ * that are only read may be shared. */
+typedef struct {
+    int32_t type, kv_heads, head_dim, page_size;
+    int64_t pages, seqs, table_cols, ld_table;
+    int64_t page_stride, head_stride, slot_stride;
+    void *k, *v;
+    const int32_t *table;
+    int32_t *position;
+    float *weight;
+} mosaic_kv_cache;
+
+/* Rotary positions with one to four axes.  Channel pair j < rot_dim / 2 turns
+ * by pos[axis[j]] turns[j] / 2^64 of a full turn; turns[j] is 2^64 times the
+ * pair's frequency in turns a position (mosaic_rope_turns fills the usual
+ * base^(-2j/rot_dim) / 2 pi), so the product modulo 2^64 is the exact phase at
+ * any position.  Pair j is channels (j, j + rot_dim / 2), or (2j, 2j + 1) when
+ * interleaved; channels from rot_dim on are left as they are.  rot_dim: a
+ * multiple of 8, at most head_dim; 0: no rotation (the other fields are not
+ * read).  turns, axis (NULL: all 0; entries outside [0, axes) count as 0) and
+ * pos (axes x l, leading dimension ldp >= l) are device pointers. */
+typedef struct {
+    int32_t rot_dim, interleaved, axes;
+    const uint64_t *turns;
+    const int32_t *axis;
+    const int32_t *pos;
+    int64_t ldp;
+} mosaic_rope;
+
+/* turns[j] = round(2^64 base^(-2j/rot_dim) / 2 pi), j < rot_dim / 2; turns is a
+ * HOST array.  base > 1 and finite; rot_dim even, 2..256. */
+mosaic_status mosaic_rope_turns(int64_t rot_dim, double base, uint64_t *turns);
+
+/* Appends l tokens.  Row t of qkv (fp32, leading dimension ldx) is a fused QKV
+ * projection: heads query heads, then kv_heads key heads, then kv_heads value
+ * heads of head_dim.  Queries and keys are rotated; queries go to q (l x heads
+ * head_dim fp32, leading dimension ldq; must not overlap qkv), key and value
+ * are rounded to nearest into slot[t] of sequence seq[t], whose position
+ * becomes index[t] and whose weight 0 (where the cache has them; index may be
+ * NULL if it has no position).  A token with a negative slot, a slot past the
+ * table or a sequence outside [0, seqs) is rotated and not stored.  Two tokens
+ * of one call must not share a slot.  rope may be NULL (no rotation). */
+mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, int64_t ldx, int64_t l, int64_t heads,
+                               const int32_t *seq, const int32_t *slot, const int32_t *index,
+                               const mosaic_rope *rope, float *q, int64_t ldq, void *stream);
+
+/* Attention of one new token per sequence.  Query head h of sequence i (row i
+ * of q, seqs x heads head_dim fp32, leading dimension ldq) reads key/value head
+ * h / (heads / kv_heads):
+ *     s_j = scale q . k_j,  p = softmax(s) over the live slots,  out = sum_j p_j v_j
+ * Live: j < lens[i] (clamped to [0, max_len] and the table) and, with `first`
+ * (seqs entries; needs cache->position), position_j >= first[i].  A slot that
+ * is not live is never used, whatever its page holds; a row without a live
+ * slot gives zeros.  A live key or value that is infinite counts as NaN.  With
+ * cache->weight, every slot j < lens[i] gets
+ *     weight_j = decay weight_j + sum of p_j over the head's query heads.
+ * Products of queries, weights and 16-bit values are carried to 22 bits or
+ * more and summed in fp32.  heads: a multiple of kv_heads, at most 64 query
+ * heads a key/value head.  max_len: an upper bound of the lengths, which
+ * sizes the workspace (mosaic_kv_attention_workspace bytes for the same
+ * cache, heads and max_len; 0 if they are not valid).  out: seqs x heads
+ * head_dim fp32 (ldo), no overlap with q.  Results do not depend on the run. */
+size_t mosaic_kv_attention_workspace(const mosaic_kv_cache *cache, int64_t heads, int64_t max_len);
+mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, int64_t ldq, int64_t heads,
+                                  const int32_t *lens, int64_t max_len, const int32_t *first, float scale,
+                                  float decay, float *out, int64_t ldo, void *ws, size_t ws_bytes, void *stream);
+
+/* Eviction by gathered attention weight (needs cache->weight).  A sequence
+ * longer than `keep` slots (lens[i], clamped as above) is cut to keep: in each
+ * key/value head the lens[i] - keep slots of the least (weight, slot) leave.
+ * With recent_from (seqs entries; needs cache->position) a slot whose position
+ * is >= recent_from[i] ranks as +inf; a NaN weight ranks as -inf, and -0 as 0.
+ * The k-th slot below keep that left takes key, value, position and weight of
+ * the k-th slot from keep on that stayed (both in ascending order): the least
+ * rows that can move do.  Heads choose for themselves, so position differs
+ * between heads.  new_lens[i] = min(lens[i], keep); new_lens may be lens.
+ * The pages of slots from keep on are free afterwards (their contents are
+ * left).  keep >= 1.  ws: mosaic_kv_evict_workspace bytes. */
+size_t mosaic_kv_evict_workspace(const mosaic_kv_cache *cache, int64_t max_len, int64_t keep);
+mosaic_status mosaic_kv_evict(const mosaic_kv_cache *cache, const int32_t *lens, int64_t max_len, int64_t keep,
+                              const int32_t *recent_from, int32_t *new_lens, void *ws, size_t ws_bytes,
+                              void *stream);
+
 /* Workspace sizes. */
 typedef enum {
     MOSAIC_OP_RING_GEMM = 1,        /* M = rows of A, n_pad = rows of B (N), l = K */

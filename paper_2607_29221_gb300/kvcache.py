@@ -1,0 +1,186 @@
+"""Paged key/value cache of a decode step: append, attention, eviction.
+
+Attention stays on the trusted side (Sec. 3.2 "Local attention computation"),
+and so does its cache.  ``PagedCache`` is a handle on a pool of pages that the
+caller allocated (or ``PagedCache.empty`` does); every method is one library
+call on the current stream:
+
+  rope  = Rope(128, base=500000.0, device="cuda")
+  cache = PagedCache.empty(pages, kv_heads, page_size, head_dim, table, torch.bfloat16)
+  q     = cache.append(qkv, heads, seq, slot, index, rope=rope, pos=pos)
+  out   = cache.attend(q, lens, max_len)
+  lens  = cache.evict(lens, max_len, keep, recent_from=recent_from)
+
+Arguments are tensors on the cache's device; scratch comes from torch's
+allocator for the current stream.  ``PageTable`` is the host's account of which
+page belongs to whom.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import mosaic as M
+
+_TYPES = {torch.float32: M.KV_F32, torch.bfloat16: M.KV_BF16, torch.float16: M.KV_F16}
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _int32(t, name: str, shape, device) -> None:
+    _need(t.dtype == torch.int32 and t.device == device and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+          f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on {device} is needed")
+
+
+class Rope:
+    """Rotary frequencies of ``rot_dim`` channels.  ``sections`` gives the
+    number of channel pairs that each of up to four position axes turns (text:
+    one axis; images and video: time, height, width), in order."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, sections=None, interleaved: bool = False,
+                 device="cuda"):
+        sections = [rot_dim // 2] if sections is None else [int(n) for n in sections]
+        _need(rot_dim % 8 == 0 and rot_dim > 0, "rot_dim: a positive multiple of 8")
+        _need(1 <= len(sections) <= 4 and min(sections) >= 0 and sum(sections) == rot_dim // 2,
+              "sections: one to four counts that add up to rot_dim / 2")
+        self.rot_dim, self.axes, self.interleaved = rot_dim, len(sections), bool(interleaved)
+        self.turns = torch.from_numpy(M.mosaic_rope_turns(rot_dim, base).view("int64")).to(device)
+        self.axis = torch.repeat_interleave(torch.arange(self.axes, dtype=torch.int32),
+                                            torch.tensor(sections)).to(device)
+
+    def at(self, pos: torch.Tensor) -> M.mosaic_rope:
+        """The rotation of tokens at ``pos`` (axes x tokens, or tokens for one axis)."""
+        pos = pos[None] if pos.dim() == 1 else pos
+        _need(pos.dtype == torch.int32 and pos.dim() == 2 and pos.shape[0] == self.axes
+              and (pos.shape[1] <= 1 or pos.stride(1) == 1) and pos.device == self.turns.device,
+              f"pos: int32, {self.axes} x tokens, rows contiguous")
+        return M.mosaic_rope(self.rot_dim, self.interleaved, self.axes, self.turns.data_ptr(), self.axis.data_ptr(),
+                             pos.data_ptr(), max(pos.stride(0), pos.shape[1]))
+
+
+class PagedCache:
+    """Handle on a paged cache.  k, v: pages x kv_heads x page_size x head_dim
+    views (float32, bfloat16 or float16; equal strides, channels contiguous),
+    table: seqs x columns int32 page ids; position (int32) and weight
+    (float32): contiguous pages x kv_heads x page_size, or None."""
+
+    def __init__(self, k, v, table, position=None, weight=None):
+        _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
+              and k.dtype in _TYPES and k.stride(3) == 1 and k.is_cuda and v.device == k.device,
+              "k and v: CUDA tensors of one type and shape (4 axes), equal strides, channels contiguous")
+        pages, kv_heads, page, dim = k.shape
+        _need(table.dtype == torch.int32 and table.dim() == 2 and table.device == k.device
+              and (table.shape[1] <= 1 or table.stride(1) == 1), "table: int32, seqs x columns, rows contiguous")
+        for t, dt, name in ((position, torch.int32, "position"), (weight, torch.float32, "weight")):
+            _need(t is None or (t.dtype == dt and t.shape == k.shape[:3] and t.is_contiguous()
+                                and t.device == k.device),
+                  f"{name}: contiguous {dt}, pages x kv_heads x page_size, on the cache's device")
+        self.k, self.v, self.table, self.position, self.weight = k, v, table, position, weight
+        self.device, self.kv_heads, self.head_dim, self.seqs = k.device, kv_heads, dim, table.shape[0]
+        ptr = [None if t is None else t.data_ptr() for t in (k, v, table, position, weight)]
+        self._c = M.mosaic_kv_cache(_TYPES[k.dtype], kv_heads, dim, page, pages, table.shape[0], table.shape[1],
+                                    max(table.stride(0), table.shape[1]), k.stride(0), k.stride(1), k.stride(2),
+                                    *ptr)
+        self._ref = ctypes.byref(self._c)
+        self._ws = {}
+
+    @classmethod
+    def empty(cls, pages: int, kv_heads: int, page_size: int, head_dim: int, table, dtype=torch.bfloat16,
+              weights: bool = True):
+        """A new pool (head-major pages), with positions, and weights unless turned off."""
+        shape, dev = (pages, kv_heads, page_size), table.device
+        k, v = (torch.zeros(*shape, head_dim, dtype=dtype, device=dev) for _ in range(2))
+        return cls(k, v, table, torch.zeros(shape, dtype=torch.int32, device=dev),
+                   torch.zeros(shape, dtype=torch.float32, device=dev) if weights else None)
+
+    def _bytes(self, key, size) -> int:
+        n = self._ws.get(key)
+        if n is None:
+            n = self._ws[key] = size()
+        return n
+
+    def append(self, qkv, heads: int, seq, slot, index=None, rope: Rope | None = None, pos=None, out=None):
+        """Rotates row t of qkv (l x (heads + 2 kv_heads) head_dim fp32) and
+        stores its keys and values in slot[t] of sequence seq[t] (a negative
+        slot: not stored); returns the queries, l x heads x head_dim fp32."""
+        l, d = qkv.shape[0], self.head_dim
+        _need(qkv.dtype == torch.float32 and qkv.dim() == 2 and qkv.device == self.device
+              and qkv.shape[1] == (heads + 2 * self.kv_heads) * d and qkv.stride(1) == 1,
+              "qkv: float32, l x (heads + 2 kv_heads) head_dim, rows contiguous")
+        for t, name in ((seq, "seq"), (slot, "slot"), (index, "index")):
+            if t is not None:
+                _int32(t, name, (l,), self.device)
+        _need((rope is None) == (pos is None), "rope and pos go together")
+        q = torch.empty(l, heads, d, dtype=torch.float32, device=self.device) if out is None else out
+        _need(q.dtype == torch.float32 and tuple(q.shape) == (l, heads, d) and q.device == self.device
+              and q.stride(2) == 1 and (heads == 1 or q.stride(1) == d), "out: float32, l x heads x head_dim")
+        r = None
+        if rope is not None:
+            r = rope.at(pos)
+            _need((pos[None] if pos.dim() == 1 else pos).shape[1] == l, "pos: a position for every token")
+        M.mosaic_kv_append(self._ref, qkv, max(qkv.stride(0), qkv.shape[1]), l, heads, seq, slot, index,
+                           None if r is None else ctypes.byref(r), q, max(q.stride(0), heads * d))
+        return q
+
+    def attend(self, q, lens, max_len: int, first=None, scale: float | None = None, decay: float = 1.0, out=None):
+        """Attention of one query a sequence (q: seqs x heads x head_dim fp32)
+        over its first lens[i] <= max_len slots, without the slots whose
+        position is below first[i]; adds the attention weights to
+        ``weight`` (after scaling it by decay) if the cache keeps them."""
+        heads, d = q.shape[1], self.head_dim
+        _need(q.dtype == torch.float32 and tuple(q.shape) == (self.seqs, heads, d) and q.device == self.device
+              and q.stride(2) == 1 and (heads == 1 or q.stride(1) == d), "q: float32, seqs x heads x head_dim")
+        _int32(lens, "lens", (self.seqs,), self.device)
+        if first is not None:
+            _int32(first, "first", (self.seqs,), self.device)
+        o = torch.empty(self.seqs, heads, d, dtype=torch.float32, device=self.device) if out is None else out
+        _need(o.dtype == torch.float32 and o.shape == q.shape and o.device == self.device and o.stride(2) == 1
+              and (heads == 1 or o.stride(1) == d), "out: float32, seqs x heads x head_dim")
+        n = self._bytes((heads, max_len), lambda: M.mosaic_kv_attention_workspace(self._ref, heads, max_len))
+        ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+        M.mosaic_kv_attention(self._ref, q, max(q.stride(0), heads * d), heads, lens, max_len, first,
+                              d ** -0.5 if scale is None else scale, decay, o, max(o.stride(0), heads * d), ws)
+        return o
+
+    def evict(self, lens, max_len: int, keep: int, recent_from=None, new_lens=None):
+        """Cuts every sequence to ``keep`` slots by least gathered weight (ties:
+        the lower slot leaves), sparing positions >= recent_from[i]; returns
+        the new lengths."""
+        _int32(lens, "lens", (self.seqs,), self.device)
+        if recent_from is not None:
+            _int32(recent_from, "recent_from", (self.seqs,), self.device)
+        new = torch.empty_like(lens) if new_lens is None else new_lens
+        _int32(new, "new_lens", (self.seqs,), self.device)
+        n = self._bytes(("evict", max_len, keep), lambda: M.mosaic_kv_evict_workspace(self._ref, max_len, keep))
+        ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+        M.mosaic_kv_evict(self._ref, lens, max_len, keep, recent_from, new, ws)
+        return new
+
+
+class PageTable:
+    """Which page belongs to which sequence: the host's account and its copy
+    on the device (``table``).  Page 0 is nobody's (the table's filler)."""
+
+    def __init__(self, seqs: int, columns: int, pages: int, page_size: int, device="cuda"):
+        _need(pages >= 1 and page_size >= 1, "pages and page_size: at least 1")
+        self.page_size = page_size
+        self.free = list(range(pages - 1, 0, -1))
+        self.owned = [[] for _ in range(seqs)]
+        self.columns = columns
+        self.table = torch.zeros(seqs, columns, dtype=torch.int32, device=device)
+
+    def resize(self, seq: int, slots: int) -> None:
+        """Gives sequence ``seq`` the pages that ``slots`` slots need, and takes back what it has beyond."""
+        need, own = -(-slots // self.page_size), self.owned[seq]
+        _need(need <= self.columns, "the table has too few columns")
+        _need(need - len(own) <= len(self.free), "no free page")
+        while len(own) > need:
+            self.free.append(own.pop())
+        if len(own) < need:
+            at = len(own)
+            own += [self.free.pop() for _ in range(need - at)]
+            self.table[seq, at:need] = torch.tensor(own[at:], dtype=torch.int32)

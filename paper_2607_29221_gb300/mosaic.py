@@ -56,6 +56,22 @@ class mosaic_mask_io(ctypes.Structure):
                 ("pass_dev", ctypes.c_void_p), ("Ux_tm", ctypes.c_void_p), ("K_tm", ctypes.c_void_p)]
 
 
+KV_F32, KV_BF16, KV_F16 = 0, 1, 2
+
+
+class mosaic_kv_cache(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("type", "kv_heads", "head_dim", "page_size")]
+                + [(n, ctypes.c_int64) for n in ("pages", "seqs", "table_cols", "ld_table", "page_stride",
+                                                 "head_stride", "slot_stride")]
+                + [(n, ctypes.c_void_p) for n in ("k", "v", "table", "position", "weight")])
+
+
+class mosaic_rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("turns", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("ldp", ctypes.c_int64)]
+
+
 class mosaic_kernel_time(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 64), ("launches", ctypes.c_uint64), ("ms", ctypes.c_double)]
 
@@ -66,6 +82,8 @@ _P, _I64, _U32, _U64, _INT, _F32 = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_ui
 _SZ = ctypes.c_size_t
 _PP = ctypes.POINTER(mosaic_params)
 _PK = ctypes.POINTER(mosaic_key)
+_PC = ctypes.POINTER(mosaic_kv_cache)
+_PR = ctypes.POINTER(mosaic_rope)
 
 _SIGS = {
     "mosaic_default_params": ([_PP], None),
@@ -118,6 +136,12 @@ _SIGS = {
     "mosaic_freivalds_setup": ([_PP, _PK, _U64, _INT, _P, _I64, _I64, _I64, _P, _P, _P], _INT),
     "mosaic_freivalds_check": ([_INT, _P, _P, _I64, _I64, _I64, _P, _I64, _P, _I64, _P, _P, _P, _SZ,
                                 _P], _INT),
+    "mosaic_rope_turns": ([_I64, ctypes.c_double, _P], _INT),
+    "mosaic_kv_append": ([_PC, _P, _I64, _I64, _I64, _P, _P, _P, _PR, _P, _I64, _P], _INT),
+    "mosaic_kv_attention_workspace": ([_PC, _I64, _I64], _SZ),
+    "mosaic_kv_attention": ([_PC, _P, _I64, _I64, _P, _I64, _P, _F32, _F32, _P, _I64, _P, _SZ, _P], _INT),
+    "mosaic_kv_evict_workspace": ([_PC, _I64, _I64], _SZ),
+    "mosaic_kv_evict": ([_PC, _P, _I64, _I64, _P, _P, _P, _SZ, _P], _INT),
 }
 
 EXPORTS = tuple(_SIGS)
@@ -418,3 +442,34 @@ def mosaic_mask(kind, params, key, stream_id, rows, n_pad, l, io: dict, variant=
 
 def mosaic_advance_pass(pass_dev, delta=1, stream=None):
     _call("mosaic_advance_pass", _ptr(pass_dev), delta, _stream(stream))
+
+
+def mosaic_rope_turns(rot_dim, base):
+    """The frequencies of rot_dim / 2 rotary pairs in 2^-64 turns a position (numpy uint64)."""
+    import numpy as np
+    out = np.zeros(max(int(rot_dim) // 2, 1), np.uint64)
+    _call("mosaic_rope_turns", rot_dim, base, out.ctypes.data_as(ctypes.c_void_p))
+    return out
+
+
+def mosaic_kv_append(cache, qkv, ldx, l, heads, seq, slot, index, rope, q, ldq, stream=None):
+    _call("mosaic_kv_append", cache, _ptr(qkv), ldx, l, heads, _ptr(seq), _ptr(slot), _ptr(index), rope, _ptr(q),
+          ldq, _stream(stream))
+
+
+def mosaic_kv_attention_workspace(cache, heads, max_len) -> int:
+    return int(lib().mosaic_kv_attention_workspace(cache, heads, max_len))
+
+
+def mosaic_kv_attention(cache, q, ldq, heads, lens, max_len, first, scale, decay, out, ldo, ws, stream=None):
+    _call("mosaic_kv_attention", cache, _ptr(q), ldq, heads, _ptr(lens), max_len, _ptr(first), scale, decay,
+          _ptr(out), ldo, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+
+
+def mosaic_kv_evict_workspace(cache, max_len, keep) -> int:
+    return int(lib().mosaic_kv_evict_workspace(cache, max_len, keep))
+
+
+def mosaic_kv_evict(cache, lens, max_len, keep, recent_from, new_lens, ws, stream=None):
+    _call("mosaic_kv_evict", cache, _ptr(lens), max_len, keep, _ptr(recent_from), _ptr(new_lens), _ptr(ws),
+          0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
