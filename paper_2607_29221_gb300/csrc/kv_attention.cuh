@@ -1,0 +1,74 @@
+// Attention of one new token per sequence over the paged cache: the kernel,
+// its mathematics and its split; kv_attention.cu holds the entry point and
+// what follows it, kv_attention_<type>.cu the instances of one element type.
+//
+//   s_j = scale q . k_j,  p = softmax(s) over the live slots,  out = sum p_j v_j
+//
+// Bound by reading K and V once (8 query heads a key/value head: 8 operations
+// a byte of a 16-bit cache), so what matters is to keep enough bytes in
+// flight on every SM and to keep the rest out of their way:
+//
+//  * A warp is on its own: it copies tiles of 16 slots (K and V rows of one
+//    head) into its own ring in shared memory with asynchronous copies,
+//    multiplies, and keeps the running maximum and sum of its slots, with no
+//    block-wide barrier until the warps' results are merged.
+//  * S^T = K Q^T and O^T += V^T P^T on mma.sync with 8 query heads as the
+//    narrow side: K and V fill the 16 rows whatever the group's size, which
+//    no shape of tcgen05 does better here: at 8 operations a byte the tensor
+//    pipe is a few percent busy, and registers are where softmax wants S.
+//  * fp32 queries and probabilities against 16-bit K and V: each is split
+//    into terms of the cache's type (bf16: three terms, all 24 bits; fp16:
+//    two, 22 bits, scaled by a power of two), the products of which are exact;
+//    fp32 K and V into two tf32 terms (products of 22 bits).  Terms are summed
+//    from the least on, each chain starts from zero and its result is added
+//    in fp32 with rounding to nearest, since the tensor cores truncate.
+//  * Work is cut evenly: units of (4 warps x 16) slots of all (sequence, head)
+//    jobs in a row, a contiguous share for every block (one wave of blocks).
+//    A job that lies in one block is finished there; one cut by a block's end
+//    leaves partial sums that the join adds (at most two a block).
+#pragma once
+
+#include "kv_cache.cuh"
+
+namespace mosaic {
+
+// Blocks of one wave at most (the resident ones of an instance are fewer).
+constexpr int kAttendWave = 152 * 8;
+
+struct AttendArgs {
+    const float *q;
+    int64_t ldq;
+    const int32_t *lens, *first;
+    int64_t max_len;
+    int heads, group, hb;       // hb: jobs (blocks of query heads) of a key/value head
+    int whole;                  // a block a job, nothing is cut
+    int blocks;
+    float scale2, decay;        // scale * log2(e): scores are kept in the base-2 domain
+    float *out;
+    int64_t ldo;
+    // Partial sums of a block: slot 2c (its first job, begun elsewhere) and
+    // 2c + 1 (its last, ended elsewhere): maxima and sums, and outputs.
+    float *part_ml, *part_o;
+    int64_t *split;             // of block c: the job cut by its end (or -1), the last block with a part of
+                                // it, and the units of the whole call
+    float *stats;               // final maximum and sum of (sequence, head), for the weights
+    float *scores;              // (sequence, kv head) x score_rows x group, for the weights
+    int64_t score_rows;
+};
+
+// What the instance for a head_dim and a group has: query heads of a job,
+// padded head_dim (row length of part_o), slots of a unit; the blocks of one
+// wave on the current device (0: a CUDA error); and its launch.
+struct AttendShape {
+    int heads, dim, unit;
+};
+template <class T> AttendShape attend_shape(int head_dim, int group);
+template <class T> int attend_wave(int head_dim, int group);
+template <class T> mosaic_status attend_launch(const mosaic_kv_cache &c, const AttendArgs &a, cudaStream_t st);
+
+namespace {
+
+__device__ __forceinline__ float minus_inf() { return __int_as_float(0xff800000); }
+
+}  // namespace
+}  // namespace mosaic

@@ -1,0 +1,5 @@
+#include "kv_attention_impl.cuh"
+
+namespace mosaic {
+MOSAIC_ATTEND_TYPE(float)
+}
