@@ -11,55 +11,151 @@ namespace {
 constexpr int kMaxGroup = 64;
 // Up to here every job is one block's: nothing to join, one launch fewer.
 constexpr int64_t kWholeLen = 512;
+// What a job costs beside its slots, as bytes of cache read in that time.  48
+// sequences of 41 to 2000 slots on 32 heads of 128: 266 us at 0, 231 at 32 KB,
+// 140 at 128 KB, 135 at 192 KB, 139 at 256 KB, 153 at 512 KB; 64 of 256 to 16384
+// on 8 heads: 418, 410, 381, 371, 368, 372; 400 of 3 to 1500 on 8 heads of 64,
+// windowed: 147, 122, 95, 93, 90 (256 KB).
+constexpr int64_t kJobBytes = 256 * 1024;
 
 // Block (c, head): the job that block c's end cuts, one query head of it.
 __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a, AttendShape s, int dim) {
+    __shared__ float factor[kAttendWave], part[2][4];
     pdl_enter();
-    const int c = blockIdx.x, head = blockIdx.y;
+    const int c = blockIdx.x, head = blockIdx.y, n = a.blocks, tid = threadIdx.x;
     const int64_t job = a.split[3 * c], last = a.split[3 * c + 1], total = a.split[3 * c + 2];
     if (job < 0) return;
     const int per_seq = a.heads / a.group * a.hb, r = (int)(job % per_seq), h = r / a.hb, hb = r % a.hb;
     if (hb * s.heads + head >= a.group) return;
     const int64_t i = job / per_seq, qh = (int64_t)h * a.group + hb * s.heads + head;
-    const int n = a.blocks;
-    // Part k of the job: the cut block's second slot, then the first slots of the blocks after it.
-    auto slot = [&](int64_t k) { return (2 * k + (k == c)) * s.heads + head; };
-    auto has = [&](int64_t k) { return total * k / n < total * (k + 1) / n; };
+    // Part k of the job: the cut block's second slot, then the first slots of
+    // the blocks after it (some without a unit where units are fewer than blocks).
+    const int parts = (int)(last - c) + 1;
+    auto slot = [&](int k) { return (2 * (int64_t)(c + k) + (k == 0)) * s.heads + head; };
+    auto has = [&](int k) { return total >= n || total * (c + k) / n < total * (c + k + 1) / n; };
+    auto block_of = [&](float x, int which, auto op) {   // of all threads' values
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) x = op(x, __shfl_xor_sync(0xffffffffu, x, o));
+        if ((tid & 31) == 0) part[which][tid >> 5] = x;
+        __syncthreads();
+        return op(op(part[which][0], part[which][1]), op(part[which][2], part[which][3]));
+    };
     float top = minus_inf();
-    for (int64_t k = c; k <= last; ++k)
+    for (int k = tid; k < parts; k += 128)
         if (has(k)) top = fmaxf(top, a.part_ml[2 * slot(k)]);
+    top = block_of(top, 0, [](float x, float y) { return fmaxf(x, y); });
     const float ref = top == minus_inf() ? 0.0f : top;
-    for (int d = threadIdx.x; d < dim; d += 128) {
-        float sum = 0.0f, out = 0.0f;
-        for (int64_t k = c; k <= last; ++k) {
-            if (!has(k)) continue;
-            const float f = exp2f(a.part_ml[2 * slot(k)] - ref);
-            sum = fmaf(f, a.part_ml[2 * slot(k) + 1], sum);
-            out = fmaf(f, a.part_o[slot(k) * s.dim + d], out);
+    float sum = 0.0f;
+    for (int k = tid; k < parts; k += 128) {
+        const bool in = has(k);
+        const float f = in ? power2(a.part_ml[2 * slot(k)] - ref) : 0.0f;
+        factor[k] = in ? f : -1.0f;
+        if (in) sum = fmaf(f, a.part_ml[2 * slot(k) + 1], sum);
+    }
+    sum = block_of(sum, 1, [](float x, float y) { return x + y; });
+    // A warp every fourth part, a lane four channels (two rounds beyond 128).
+    __shared__ float4 rest[3][32];
+    for (int d0 = 0; d0 < s.dim; d0 += 128) {
+        const int d = d0 + 4 * (tid & 31), w = tid >> 5;
+        float4 out = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (d < s.dim) {
+#pragma unroll 4
+            for (int k = w; k < parts; k += 4) {
+                const float f = factor[k];
+                if (f == -1.0f) continue;
+                const float4 x = *reinterpret_cast<const float4 *>(a.part_o + slot(k) * s.dim + d);
+                out.x = fmaf(f, x.x, out.x), out.y = fmaf(f, x.y, out.y);
+                out.z = fmaf(f, x.z, out.z), out.w = fmaf(f, x.w, out.w);
+            }
         }
-        a.out[i * a.ldo + qh * dim + d] = sum == 0.0f ? 0.0f : out / sum;
-        if (a.scores && d == 0) a.stats[2 * (i * a.heads + qh)] = ref, a.stats[2 * (i * a.heads + qh) + 1] = sum;
+        if (w) rest[w - 1][tid & 31] = out;
+        __syncthreads();
+        if (w == 0) {
+            for (int x = 0; x < 3; ++x) {
+                const float4 y = rest[x][tid];
+                out.x += y.x, out.y += y.y, out.z += y.z, out.w += y.w;
+            }
+            const float o[4] = {out.x, out.y, out.z, out.w};
+            for (int x = 0; x < 4; ++x)
+                if (d + x < dim) a.out[i * a.ldo + qh * dim + d + x] = sum == 0.0f ? 0.0f : o[x] / sum;
+        }
+        __syncthreads();
+    }
+    if (a.scores && tid == 0) {
+        a.stats[2 * (i * a.heads + qh)] = ref;
+        a.stats[2 * (i * a.heads + qh) + 1] = sum == 0.0f ? 0.0f : 1.0f / sum;
     }
 }
 
-// A thread a slot of a (sequence, key/value head): the weight that it gathers.
-__global__ void __launch_bounds__(256) attend_weight_kernel(KvView kv, AttendArgs a, int64_t chunks) {
+// A thread four slots of a (sequence, key/value head): the weight that they
+// gather.  Bound by reading the scores (4 bytes a slot and query head); every
+// load of a thread is issued before its use.  vec: four slots share a page and
+// a 16-byte word of the weights.
+constexpr int kWeightSlots = 4 * 128;
+struct WeightWalk {
+    int64_t chunks, jobs_step, chunk_step;   // the grid's stride over (job, chunk of slots)
+    int vec;
+};
+__global__ void __launch_bounds__(128, 8) attend_weight_kernel(KvView kv, AttendArgs a, WeightWalk walk) {
     pdl_enter();
-    const int64_t jobs = kv.c.seqs * kv.c.kv_heads * chunks;
-    for (int64_t b = blockIdx.x; b < jobs; b += gridDim.x) {
-        const int64_t job = b / chunks, i = job / kv.c.kv_heads;
-        const int h = (int)(job % kv.c.kv_heads), s = (int)(b % chunks) * 256 + threadIdx.x;
-        if (s >= kv.length(a.lens, i, a.max_len)) continue;
+    const int64_t jobs = kv.c.seqs * kv.c.kv_heads;
+    int64_t job = blockIdx.x / walk.chunks, chunk = blockIdx.x % walk.chunks;
+    for (; job < jobs; job += walk.jobs_step, chunk += walk.chunk_step) {
+        if (chunk >= walk.chunks && (chunk -= walk.chunks, ++job) >= jobs) break;
+        const int64_t i = job / kv.c.kv_heads;
+        const int h = (int)(job - i * kv.c.kv_heads), s = (int)chunk * kWeightSlots + 4 * threadIdx.x;
+        const int len = kv.length(a.lens, i, a.max_len);
+        if (s >= len) continue;
+        float *at[4];
+        __align__(16) float old[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         uint32_t off;
         const int id = kv.page_of(i, (uint32_t)s, off);
-        if (id < 0) continue;
-        const float *sc = a.scores + (job * a.score_rows + s) * a.group;
-        const float *st = a.stats + 2 * (i * a.heads + (int64_t)h * a.group);
-        float w = 0.0f;
-        for (int g = 0; g < a.group; ++g)
-            if (st[2 * g + 1] != 0.0f) w += exp2f(sc[g] - st[2 * g]) / st[2 * g + 1];
-        float *p = kv.c.weight + kv.mark(id, h, off);
-        *p = *p * a.decay + w;
+        at[0] = id < 0 ? nullptr : kv.c.weight + kv.mark(id, h, off);
+        const bool quad = walk.vec && s + 4 <= len;
+        if (!quad) {
+#pragma unroll
+            for (int j = 1; j < 4; ++j) {
+                const int jd = s + j < len ? kv.page_of(i, (uint32_t)(s + j), off) : -1;
+                at[j] = jd < 0 ? nullptr : kv.c.weight + kv.mark(jd, h, off);
+            }
+        }
+        const int64_t head = i * a.heads + (int64_t)h * a.group;
+        const float *sc = a.scores + head * a.score_rows + s;
+        const float2 *st = reinterpret_cast<const float2 *>(a.stats) + head;
+        float w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int g0 = 0; g0 < a.group; g0 += 8) {
+            float4 x[8];
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+                if (g0 + g < a.group) x[g] = *reinterpret_cast<const float4 *>(sc + (g0 + g) * a.score_rows);
+            if (g0 == 0) {
+                if (quad) {
+                    if (at[0]) *reinterpret_cast<float4 *>(old) = *reinterpret_cast<const float4 *>(at[0]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (at[j]) old[j] = *at[j];
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+                if (g0 + g < a.group) {
+                    const float2 y = st[g0 + g];
+                    w[0] = fmaf(power2(x[g].x - y.x), y.y, w[0]);
+                    w[1] = fmaf(power2(x[g].y - y.x), y.y, w[1]);
+                    w[2] = fmaf(power2(x[g].z - y.x), y.y, w[2]);
+                    w[3] = fmaf(power2(x[g].w - y.x), y.y, w[3]);
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) old[j] = fmaf(old[j], a.decay, w[j]);
+        if (quad) {
+            if (at[0]) *reinterpret_cast<float4 *>(at[0]) = *reinterpret_cast<const float4 *>(old);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (at[j]) *at[j] = old[j];
+        }
     }
 }
 
@@ -156,6 +252,8 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
         if (wave <= 0) return MOSAIC_ERR_CUDA;
         a.blocks = (int)(cap < wave ? cap : wave);
     }
+    const int64_t unit_bytes = 2 * s.unit * D * kv_element_bytes(cache->type);
+    a.job_cost = (int)((kJobBytes + unit_bytes / 2) / unit_bytes);
     cudaStream_t st = as_stream(stream);
     MOSAIC_TRY(by_type(cache->type, [&](auto t) { return attend_launch<decltype(t)>(*cache, a, st); }));
     if (!a.whole) {
@@ -166,12 +264,14 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
         MOSAIC_TRY(launch_status());
     }
     if (!a.scores || max_len == 0) return MOSAIC_OK;
-    const int64_t chunks = (max_len + 255) / 256, all = cache->seqs * cache->kv_heads * chunks;
+    const int64_t chunks = (max_len + kWeightSlots - 1) / kWeightSlots, all = cache->seqs * cache->kv_heads * chunks;
     const KvView kv(*cache);
     {
         KernelSpan span("attend_weight", st);
-        pdl_launch(attend_weight_kernel, dim3((unsigned)(all < 152 * 8 ? all : 152 * 8)), dim3(256), 0, st, kv, a,
-                   chunks);
+        const int64_t grid = all < 152 * 8 ? all : 152 * 8;
+        const WeightWalk walk = {chunks, grid / chunks, grid % chunks,
+                                 cache->page_size % 4 == 0 && aligned16(cache->weight)};
+        pdl_launch(attend_weight_kernel, dim3((unsigned)grid), dim3(128), 0, st, kv, a, walk);
     }
     return launch_status();
 }

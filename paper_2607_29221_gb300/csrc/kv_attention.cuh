@@ -43,6 +43,7 @@ struct AttendArgs {
     int heads, group, hb;       // hb: jobs (blocks of query heads) of a key/value head
     int whole;                  // a block a job, nothing is cut
     int blocks;
+    int job_cost;
     float scale2, decay;        // scale * log2(e): scores are kept in the base-2 domain
     float *out;
     int64_t ldo;
@@ -51,8 +52,8 @@ struct AttendArgs {
     float *part_ml, *part_o;
     int64_t *split;             // of block c: the job cut by its end (or -1), the last block with a part of
                                 // it, and the units of the whole call
-    float *stats;               // final maximum and sum of (sequence, head), for the weights
-    float *scores;              // (sequence, kv head) x score_rows x group, for the weights
+    float *stats;               // final maximum and 1 / sum of (sequence, head), for the weights
+    float *scores;              // (sequence, head) x score_rows, for the weights
     int64_t score_rows;
 };
 
@@ -69,6 +70,12 @@ template <class T> mosaic_status attend_launch(const mosaic_kv_cache &c, const A
 namespace {
 
 __device__ __forceinline__ float minus_inf() { return __int_as_float(0xff800000); }
+// 2^x to 2^-22 relative; results below 2^-126 are zeros.
+__device__ __forceinline__ float power2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 }  // namespace
 }  // namespace mosaic

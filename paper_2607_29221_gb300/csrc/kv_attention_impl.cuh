@@ -70,11 +70,7 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&t)[N]) {
 // fp32 as two tf32 terms, the upper one rounded to nearest (the lower one then
 // has either sign, and what is left out averages out); the lower one's own tail
 // (2^-23) is cut by the tensor core.
-__device__ __forceinline__ uint32_t tf32_high(float x) {
-    uint32_t r;
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
-    return r;
-}
+__device__ __forceinline__ uint32_t tf32_high(float x) { return (__float_as_uint(x) + 0x1000u) & 0xffffe000u; }
 __device__ __forceinline__ uint32_t tf32_low(float x, uint32_t high) {
     return __float_as_uint(x - __uint_as_float(high));
 }
@@ -85,23 +81,31 @@ template <> constexpr int kTerms<__half> = 2;
 template <class T> constexpr float kShift = 0.0f;
 template <> constexpr float kShift<__half> = 12.0f;
 
+constexpr int kGroup = 128;   // slots whose page ids a warp looks up together (8 tiles)
+
 // DP: head_dim padded to 64, 128 or 256.  NT: tiles of 8 query heads.
 template <class T, int DP, int NT>
 struct Shape {
     static constexpr int kES = sizeof(T), kRow = DP * kES, kChunks = kRow / 16;
     static constexpr int kTile = 2 * 16 * kRow;                   // K and V of 16 slots
-    static constexpr int kWarps = kTile >= 32768 ? 2 : 4, kUnit = 16 * kWarps;
-    static constexpr int kStages = kTile <= 4096 ? 4 : 3;
+    // 8 warps an SM, as two blocks or (with twice the outputs and queries) one;
+    // fewer where tiles are large.
+    static constexpr bool kSix = kES == 4 && DP == 128 && NT == 1;
+    static constexpr int kWarps = kTile >= 32768 ? 2 : NT == 2 && kTile <= 8192 ? 8 : kSix ? 6 : 4, kUnit = 16 * kWarps;
+    static constexpr int kStages = kTile <= 4096 ? 4 : (NT == 2 && DP == 256) || kSix ? 2 : 3;
+    static constexpr int kSlots = kWarps == 2 || (NT == 2 && kTile >= 16384) ? 1 : 2;   // warps' results at a time
     static constexpr int kK = kES == 4 ? 8 : 16, kSteps = DP / kK;    // channels of a product step
     static constexpr int kHeads = 8 * NT, kPitch = DP + 4;
     static constexpr int kQWords = kSteps * NT * kTerms<T> * 2 * 32;  // query fragments
     // Queries stay in registers where they fit beside the outputs.
     static constexpr bool kQReg = kSteps * NT * kTerms<T> * 2 <= 48;
-    static constexpr int kMerge = 4 * kWarps * kHeads * (kPitch + 2);
+    // Shared memory: the rings, the results of some warps, the warps'
+    // page ids, the queries' fragments.
     static constexpr int kRing = kWarps * kStages * kTile;
-    static constexpr int kQBytes = kQReg ? 0 : 4 * kQWords;
-    static constexpr int kBytes = (kRing > kMerge ? kRing : kMerge) + kQBytes;
-    static_assert(kBytes <= 227 * 1024, "shared memory");
+    static constexpr int kMerge = 4 * kSlots * kHeads * (kPitch + 2);
+    static constexpr int kIds = 4 * kWarps * kGroup;
+    static constexpr int kBytes = kRing + kMerge + kIds + (kQReg ? 0 : 4 * kQWords);
+    static_assert(kBytes + 128 <= 227 * 1024, "shared memory");
 };
 
 // 16-byte chunk c of row r sits at chunk c ^ swizzle(r): 8 rows of a chunk are
@@ -135,10 +139,20 @@ struct Warp {
         for (int n = 0; n < NT; ++n) {
             const bool in = 8 * n + g < rows;
             const float *x = q + (int64_t)(8 * n + g) * D;
-            float mul = scale2;
+            float v[S::kSteps][S::kES == 4 ? 2 : 4];   // all loads before their use
+#pragma unroll
+            for (int k = 0; k < S::kSteps; ++k)
+#pragma unroll
+                for (int j = 0; j < (S::kES == 4 ? 2 : 4); ++j) {
+                    const int d = S::kES == 4 ? 8 * k + 4 * j + t : 16 * k + 8 * (j >> 1) + 2 * t + (j & 1);
+                    v[k][j] = in && d < D ? x[d] * scale2 : 0.0f;
+                }
             if constexpr (sizeof(T) == 2 && kTermsN == 2) {
                 float top = 0.0f;
-                for (int d = t; d < D; d += 4) top = fmaxf(top, in ? fabsf(x[d] * scale2) : 0.0f);
+#pragma unroll
+                for (int k = 0; k < S::kSteps; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(v[k][j]));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 // Largest |q| to [2^10, 2^11); nothing to scale in zeros, NaN and infinities.
@@ -146,30 +160,24 @@ struct Warp {
                 e = e == 128 || top == 0.0f ? 10 : e < -100 ? -100 : e;
                 const float up = __uint_as_float((uint32_t)(10 - e + 127) << 23);
                 const float down = __uint_as_float((uint32_t)(e - 10 + 127) << 23);
-                mul = up;
                 unscale[n][0] = __shfl_sync(0xffffffffu, down, 8 * t);
                 unscale[n][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
+#pragma unroll
+                for (int k = 0; k < S::kSteps; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[k][j] *= up;
             }
 #pragma unroll
             for (int k = 0; k < S::kSteps; ++k) {
                 uint32_t f[kTermsN][2];
-                if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const int d = 8 * k + 4 * b + t;
-                        const float v = in && d < D ? x[d] * scale2 : 0.0f;
-                        f[1][b] = tf32_high(v);
-                        f[0][b] = tf32_low(v, f[1][b]);
-                    }
-                } else {
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const int d = 16 * k + 8 * b + 2 * t;
-                        float v = 0.0f, w = 0.0f;
-                        if (in && d < D) v = x[d] * scale2, w = x[d + 1] * scale2;
-                        if constexpr (kTermsN == 2) v *= mul, w *= mul;
+                for (int b = 0; b < 2; ++b) {
+                    if constexpr (sizeof(T) == 4) {
+                        f[1][b] = tf32_high(v[k][b]);
+                        f[0][b] = tf32_low(v[k][b], f[1][b]);
+                    } else {
                         uint32_t s[kTermsN];
-                        split2<T, kTermsN>(v, w, s);
+                        split2<T, kTermsN>(v[k][2 * b], v[k][2 * b + 1], s);
 #pragma unroll
                         for (int i = 0; i < kTermsN; ++i) f[i][b] = s[i];
                     }
@@ -192,10 +200,10 @@ struct Warp {
     }
 
     // One tile of 16 slots, K rows at `tile` and V rows behind them; bit r of
-    // `live`: slot r counts.  `sc`: where the scores of slot 0 go (rows of
-    // `group` words, `heads` of which are the job's), or null; `left` rows exist.
-    __device__ __forceinline__ void tile(uint32_t tile, uint32_t live, const uint32_t *qs, float *sc, int group,
-                                         int heads, int left) {
+    // `live`: slot r counts.  `sc`: where the scores of slot 0 and the job's
+    // first head go (a row of `pitch` words a head, `heads` of them), or null.
+    __device__ __forceinline__ void tile(uint32_t tile, uint32_t live, const uint32_t *qs, float *sc, int64_t pitch,
+                                         int heads) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         float s[NT][4];
 #pragma unroll
@@ -242,8 +250,8 @@ struct Warp {
             if (sc) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int r = g + (j & 2) * 4, h = 8 * n + 2 * t + (j & 1);
-                    if (r < left && h < heads) sc[(int64_t)r * group + h] = s[n][j];
+                    const int h = 8 * n + 2 * t + (j & 1);   // 8 slots of 4 heads a store: whole sectors
+                    if (h < heads) sc[h * pitch + g + (j & 2) * 4] = s[n][j];
                 }
             }
 #pragma unroll
@@ -252,11 +260,11 @@ struct Warp {
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
                 top = fmaxf(top, m[n][j]);
-                alpha[n][j] = exp2f(m[n][j] - top);
+                alpha[n][j] = power2(m[n][j] - top);
                 m[n][j] = top;
                 const float ref = top - kShift<T>;
-                s[n][j] = exp2f(s[n][j] - ref);
-                s[n][2 + j] = exp2f(s[n][2 + j] - ref);
+                s[n][j] = power2(s[n][j] - ref);
+                s[n][2 + j] = power2(s[n][2 + j] - ref);
                 l[n][j] = fmaf(l[n][j], alpha[n][j], s[n][j] + s[n][2 + j]);
             }
             if constexpr (sizeof(T) == 2) {
@@ -333,22 +341,50 @@ struct Warp {
     }
 };
 
-// The block's place in the row of all units.
-struct Place {
-    int64_t i;    // sequence
-    int64_t at;   // units of it before the block's first
+// Work is counted in units; a job counts a.job_cost units more than it has, for
+// what its queries, its merge and its output take.
+//
+// The jobs of a block, one after the other: a stretch of `left` counted units,
+// from counted unit `at` of sequence i on.
+struct Jobs {
+    int64_t i, at, left;
+    int r, b0, b1, nb, len;   // the job: number in its sequence, its units here, all its units, the sequence's length
+    __device__ __forceinline__ bool next(const KvView &kv, const AttendArgs &a, int unit, int per_seq) {
+        while (left > 0) {
+            len = kv.length(a.lens, i, a.max_len);
+            nb = (len + unit - 1) / unit;
+            if (a.whole) {
+                r = (int)at, b0 = 0, b1 = nb, left = 0;
+                return true;
+            }
+            const int counted = nb + a.job_cost;
+            if (nb == 0 || at >= (int64_t)counted * per_seq) {
+                ++i, at = 0;
+                continue;
+            }
+            r = (int)((uint32_t)at / (uint32_t)counted);   // a sequence counts below 2^31 units
+            const int x0 = (int)at - r * counted, x1 = counted - x0 < left ? counted : x0 + (int)left;
+            left -= x1 - x0, at += x1 - x0;
+            b0 = max(0, x0 - a.job_cost), b1 = max(0, x1 - a.job_cost);
+            if (b0 < b1) return true;
+        }
+        return false;
+    }
+    __device__ __forceinline__ int first(int unit) const { return b0 * unit; }
+    __device__ __forceinline__ int last(int unit) const { return min(len, b1 * unit); }
 };
 
-// Units of the whole call (`total`), and sequence and offset of unit `u0`.
-// Every thread calls it; `sh` holds 2 x threads words.
+// Counted units of the whole call (`total`), the stretch of part `part` of
+// `parts`, and the sequence and offset of its beginning.  Every thread calls
+// it; `sh` holds a word a warp and two more.
 template <int THREADS>
 __device__ __forceinline__ void find_place(const KvView &kv, const AttendArgs &a, int unit, int64_t per_seq, int part,
-                                           int parts, int64_t &total, int64_t &u0, int64_t &u1, Place &p,
-                                           long long *sh) {
+                                           int parts, int64_t &total, int64_t &u1, Jobs &jobs, long long *sh) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int64_t seqs = kv.c.seqs;
     auto units = [&](int64_t i) -> long long {
-        return i < seqs ? (long long)((kv.length(a.lens, i, a.max_len) + unit - 1) / unit) * per_seq : 0;
+        const int nb = i < seqs ? (kv.length(a.lens, i, a.max_len) + unit - 1) / unit : 0;
+        return nb ? (long long)(nb + a.job_cost) * per_seq : 0;
     };
     long long mine = 0;
     for (int64_t i = tid; i < seqs; i += THREADS) mine += units(i);
@@ -359,7 +395,9 @@ __device__ __forceinline__ void find_place(const KvView &kv, const AttendArgs &a
     total = 0;
 #pragma unroll
     for (int k = 0; k < THREADS / 32; ++k) total += sh[k];
-    u0 = total * part / parts, u1 = total * (part + 1) / parts;
+    const long long u0 = total * part / parts;
+    u1 = total * (part + 1) / parts;
+    jobs.i = jobs.at = 0, jobs.left = u1 - u0;
     __syncthreads();
     if (u0 >= u1) return;
     long long before = 0;
@@ -385,97 +423,109 @@ __device__ __forceinline__ void find_place(const KvView &kv, const AttendArgs &a
         before += all;
         if (u0 < before) break;
     }
-    p.i = sh[THREADS / 32], p.at = sh[THREADS / 32 + 1];
+    jobs.i = sh[THREADS / 32], jobs.at = sh[THREADS / 32 + 1];
     __syncthreads();
 }
 
+// What a warp copies, tile by tile, through all jobs of the block.  Page ids
+// of 128 slots are looked up together, two groups (with a lower bound: and
+// the positions, one group) before their tiles are copied.
 template <class T, int DP, int NT>
-__global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps) attend_kernel(KvView kv, AttendArgs a) {
+struct Feed {
     using S = Shape<T, DP, NT>;
-    constexpr int W = S::kWarps, THREADS = 32 * W, NS = S::kStages;
-    extern __shared__ __align__(1024) char smem[];
-    __shared__ long long place_sh[W + 2];
-    uint32_t *qs = reinterpret_cast<uint32_t *>(smem + S::kBytes - S::kQBytes);
-    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-    const int D = kv.c.head_dim, KV = kv.c.kv_heads, per_seq = KV * a.hb;
-    pdl_enter();
+    struct Group {
+        int h, s, end, tiles, low;   // head, first slot, end of the job's slots, tiles of this warp, position bound
+        int64_t i;
+    };
+    const KvView &kv;
+    const AttendArgs &a;
+    const int per_seq, w, lane;
+    uint32_t ring;
+    int32_t *ids;       // shared: of the group being copied
+    Jobs jobs;
+    int job_tiles, job_at;   // tiles of this warp in the newest group's job, and how many have a group
+    Group now, mid, far;
+    int id_mid[4], id_far[4], pos_mid[4];
+    int at;             // tile of `now` that is copied next
+    int stage;
+    bool over;          // no further group
+    unsigned long long queue;   // live slots of the tiles in flight, 16 bits each, the oldest lowest
 
-    int64_t u0, u1, total;
-    Place p;
-    if (a.whole) {
-        p.i = blockIdx.x / per_seq;
-        u0 = 0, u1 = 1, total = 0;
-        p.at = 0;
-    } else {
-        find_place<THREADS>(kv, a, S::kUnit, per_seq, blockIdx.x, gridDim.x, total, u0, u1, p, place_sh);
-        // Sequences without a slot belong to nobody's units: their rows are shared out.
-        for (int64_t i = blockIdx.x; i < kv.c.seqs; i += gridDim.x)
-            if (kv.length(a.lens, i, a.max_len) == 0)
-                for (int x = tid; x < a.heads * D; x += THREADS) a.out[i * a.ldo + x] = 0.0f;
-        if (tid == 0) a.split[3 * blockIdx.x] = -1;
+    __device__ __forceinline__ Feed(const KvView &kv_, const AttendArgs &a_, int per_seq_, const Jobs &j, char *smem)
+        : kv(kv_), a(a_), per_seq(per_seq_), w(threadIdx.x >> 5), lane(threadIdx.x & 31), jobs(j) {
+        ring = shared_addr(smem) + w * S::kStages * S::kTile;
+        ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge) + w * kGroup;
+        job_tiles = job_at = at = stage = 0;
+        over = false, queue = 0;
+        now.tiles = mid.tiles = far.tiles = 0;
+        step(), step(), step();
     }
-
-    const char *kp = static_cast<const char *>(kv.c.k), *vp = static_cast<const char *>(kv.c.v);
-    const int chunks = D * S::kES / 16;
-    const uint32_t ring = shared_addr(smem) + w * NS * S::kTile;
-    Warp<T, DP, NT> wp;
-
-    while (u0 < u1) {
-        // The job of unit u0 and the block's slots [s0, s1) of it.
-        const int len = kv.length(a.lens, p.i, a.max_len);
-        const int nb = (len + S::kUnit - 1) / S::kUnit;
-        int r, b0, b1;
-        if (a.whole) {
-            r = blockIdx.x % per_seq, b0 = 0, b1 = nb;
-            u0 = u1;
-        } else {
-            if (nb == 0 || p.at >= (int64_t)nb * per_seq) {   // the next sequence
-                p.i += 1, p.at = 0;
-                continue;
+    __device__ __forceinline__ int slot(const Group &g, int e) const {   // entry e of the group
+        return g.s + (e >> 4) * S::kUnit + (e & 15);
+    }
+    // The next group becomes `now`, its ids in shared memory.
+    __device__ __forceinline__ void step() {
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (mid.tiles > 0) ids[32 * e + lane] = a.first && pos_mid[e] < mid.low ? -1 : id_mid[e];
+        now = mid, mid = far, at = 0;
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            id_mid[e] = id_far[e];
+            if (a.first && mid.tiles > 0 && id_mid[e] >= 0) {
+                const int s = slot(mid, 32 * e + lane);
+                pos_mid[e] = kv.c.position[kv.mark(id_mid[e], mid.h, (uint32_t)s - kv.page.div(s) * kv.page.d)];
             }
-            r = (int)(p.at / nb), b0 = (int)(p.at - (int64_t)r * nb);
-            const int64_t can = b0 + (u1 - u0);
-            b1 = can < nb ? (int)can : nb;
-            u0 += b1 - b0, p.at += b1 - b0;
         }
-        const int h = r / a.hb, hb = r % a.hb;
-        const int s0 = b0 * S::kUnit, s1 = min(len, b1 * S::kUnit);
-        const int rows = min(S::kHeads, a.group - hb * S::kHeads);
-        const int qh = h * a.group + hb * S::kHeads;
-        wp.clear();
-        const int low = a.first ? a.first[p.i] : 0;
-        const int tiles = (s1 - s0 + 15) / 16, mine = tiles > w ? (tiles - w + W - 1) / W : 0;
-        float *scores = a.scores ? a.scores + ((p.i * KV + h) * a.score_rows + s0) * a.group + hb * S::kHeads : nullptr;
-
-        // Copies run NS - 1 tiles ahead, page ids one tile further, and with a
-        // lower bound the positions in between.
-        const int64_t nothing = -1;
-        auto page_at = [&](int n, uint32_t &off) {
-            const int s = s0 + 16 * (w + n * W) + (lane & 15);
-            return n < mine && s < s1 ? kv.page_of(p.i, (uint32_t)s, off) : -1;
-        };
-        auto keep = [&](int id, uint32_t off) -> int64_t {   // element, or nothing if the slot is not live
-            if (id < 0) return nothing;
-            if (a.first && kv.c.position[kv.mark(id, h, off)] < low) return nothing;
-            return kv.element(id, h, off) * S::kES;
-        };
-        uint32_t off_next = 0;
-        int id_next = page_at(0, off_next);
-        int64_t row_next = keep(id_next, off_next);
-        id_next = page_at(1, off_next);
-        unsigned long long queue = 0;
-        auto issue = [&](int n, int depth) {
-            const int64_t at = row_next;
-            row_next = keep(id_next, off_next);
-            id_next = page_at(n + 2, off_next);
-            const uint32_t live = __ballot_sync(0xffffffffu, at >= 0) & 0xffffu;
+        // Jobs that leave this warp without a tile have no group.
+        far.tiles = 0;
+        while (!over && job_at >= job_tiles) {
+            if (!jobs.next(kv, a, S::kUnit, per_seq)) {
+                over = true;
+                break;
+            }
+            const int tiles = (jobs.last(S::kUnit) - jobs.first(S::kUnit) + 15) / 16;
+            job_tiles = tiles > w ? (tiles - w + S::kWarps - 1) / S::kWarps : 0;
+            job_at = 0;
+        }
+        if (job_at < job_tiles) {
+            far.i = jobs.i, far.h = jobs.r / a.hb, far.end = jobs.last(S::kUnit);
+            far.s = jobs.first(S::kUnit) + 16 * w + job_at * S::kUnit;
+            far.tiles = min(kGroup / 16, job_tiles - job_at);
+            far.low = a.first ? a.first[jobs.i] : 0;
+            if (job_at == 0 && w == 0) {   // the queries come from memory by the time the job begins
+                const float *q = a.q + jobs.i * a.ldq + (int64_t)(far.h * a.group + jobs.r % a.hb * S::kHeads) * kv.c.head_dim;
+                const int words = min(S::kHeads, a.group - jobs.r % a.hb * S::kHeads) * kv.c.head_dim;
+                for (int x = 32 * lane; x < words; x += 1024) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + x));
+            }
+            job_at += far.tiles;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int x = 32 * e + lane, s = slot(far, x);
+                uint32_t off;
+                id_far[e] = (x >> 4) < far.tiles && s < far.end ? kv.page_of(far.i, (uint32_t)s, off) : -1;
+            }
+        }
+    }
+    // Copies the next tile (an empty one at the end), `depth` tiles before its use.
+    __device__ __forceinline__ void issue(int depth) {
+        // No group is empty but those behind the last one.
+        if (at >= now.tiles && mid.tiles > 0) step();
+        if (at < now.tiles) {
+            const int id = ids[16 * at + (lane & 15)], s = now.s + at * S::kUnit + (lane & 15);
+            const uint32_t live = __ballot_sync(0xffffffffu, id >= 0) & 0xffffu;
             queue |= (unsigned long long)live << (16 * depth);
             if (live) {
-                const uint32_t to = ring + (n % NS) * S::kTile;
+                const int64_t row = id < 0 ? -1 : kv.element(id, now.h, (uint32_t)s - kv.page.div(s) * kv.page.d) * S::kES;
+                const char *kp = static_cast<const char *>(kv.c.k), *vp = static_cast<const char *>(kv.c.v);
+                const int chunks = kv.c.head_dim * S::kES / 16;
+                const uint32_t to = ring + stage * S::kTile;
 #pragma unroll
                 for (int x = 0; x < 16 * S::kChunks / 32; ++x) {
                     const int at16 = x * 32 + lane, rr = at16 / S::kChunks, c = at16 % S::kChunks;
-                    const int64_t e = __shfl_sync(0xffffffffu, at, rr);
+                    const int64_t e = __shfl_sync(0xffffffffu, row, rr);
                     const bool ok = e >= 0 && c < chunks;
                     const uint32_t dst = to + rr * S::kRow + ((c ^ swizzle(rr & 7)) << 4);
                     const int64_t src = ok ? e + c * 16 : 0;
@@ -483,86 +533,155 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps) attend_kernel(K
                     copy16(dst + 16 * S::kRow, vp + src, ok);
                 }
             }
-            copies_commit();
-        };
+            ++at;
+        }
+        copies_commit();
+        stage = stage + 1 == S::kStages ? 0 : stage + 1;
+    }
+};
+
+template <class T, int DP, int NT>
+__global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps) attend_kernel(KvView kv, AttendArgs a) {
+    using S = Shape<T, DP, NT>;
+    constexpr int W = S::kWarps, THREADS = 32 * W, NS = S::kStages, MS = S::kSlots;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ long long place_sh[W + 2];
+    float *mo = reinterpret_cast<float *>(smem + S::kRing), *mm = mo + MS * S::kHeads * S::kPitch,
+          *ml = mm + MS * S::kHeads;
+    uint32_t *qs = reinterpret_cast<uint32_t *>(smem + S::kRing + S::kMerge + S::kIds);
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int D = kv.c.head_dim, KV = kv.c.kv_heads, per_seq = KV * a.hb;
+    pdl_enter();
+
+    Jobs jobs;
+    int64_t total = 0, end = 0;
+    if (a.whole) {
+        jobs.i = blockIdx.x / per_seq, jobs.at = blockIdx.x % per_seq, jobs.left = 1;
+    } else {
+        find_place<THREADS>(kv, a, S::kUnit, per_seq, blockIdx.x, gridDim.x, total, end, jobs, place_sh);
+        // Sequences without a slot belong to nobody's units: their rows are shared out.
+        for (int64_t i = blockIdx.x; i < kv.c.seqs; i += gridDim.x)
+            if (kv.length(a.lens, i, a.max_len) == 0)
+                for (int x = tid; x < a.heads * D; x += THREADS) a.out[i * a.ldo + x] = 0.0f;
+        if (tid == 0) a.split[3 * blockIdx.x] = -1;
+    }
+    Feed<T, DP, NT> feed(kv, a, per_seq, jobs, smem);
 #pragma unroll
-        for (int n = 0; n < NS - 1; ++n) issue(n, n);
-        wp.queries(a.q + p.i * a.ldq + (int64_t)qh * D, D, rows, a.scale2, qs);
+    for (int n = 0; n < NS - 1; ++n) feed.issue(n);
+
+    Warp<T, DP, NT> wp;
+    int use = 0;   // ring stage of the next tile
+    while (jobs.next(kv, a, S::kUnit, per_seq)) {
+        const int s0 = jobs.first(S::kUnit), s1 = jobs.last(S::kUnit);
+        const int h = jobs.r / a.hb, hb = jobs.r % a.hb;
+        const int rows = min(S::kHeads, a.group - hb * S::kHeads);
+        const int64_t i = jobs.i, qh = (int64_t)h * a.group + hb * S::kHeads;
+        const int tiles = (s1 - s0 + 15) / 16, mine = tiles > w ? (tiles - w + W - 1) / W : 0;
+        float *scores = a.scores ? a.scores + (i * a.heads + qh) * a.score_rows + s0 : nullptr;
+        wp.clear();
+        wp.queries(a.q + i * a.ldq + qh * D, D, rows, a.scale2, qs);
         if constexpr (!S::kQReg) __syncthreads();
         for (int n = 0; n < mine; ++n) {
             copies_wait<NS - 2>();
             __syncwarp();
-            const uint32_t live = (uint32_t)queue & 0xffffu;
-            queue >>= 16;
-            issue(n + NS - 1, NS - 2);
-            const int s = 16 * (w + n * W);
-            if (live)
-                wp.tile(ring + (n % NS) * S::kTile, live, qs, scores ? scores + (int64_t)s * a.group : nullptr, a.group,
-                        rows, s1 - s0 - s);
-            else if (scores) {   // no slot counts: the weights read that
-                for (int x = lane; x < 16 * rows; x += 32)
-                    if (s + x / rows < s1 - s0) scores[(int64_t)(s + x / rows) * a.group + x % rows] = minus_inf();
+            const uint32_t live = (uint32_t)feed.queue & 0xffffu;
+            feed.queue >>= 16;
+            feed.issue(NS - 2);
+            float *sc = scores ? scores + 16 * (w + n * W) : nullptr;   // rows of 16 slots exist in whole
+            if (live) wp.tile(feed.ring + use * S::kTile, live, qs, sc, a.score_rows, rows);
+            else if (sc) {   // no slot counts: the weights read that
+                for (int x = lane; x < 16 * rows; x += 32) sc[(x >> 4) * a.score_rows + (x & 15)] = minus_inf();
             }
+            use = use + 1 == NS ? 0 : use + 1;
         }
-        copies_wait<0>();
 
-        // Merge of the warps.
-        __syncthreads();
-        float *mo = reinterpret_cast<float *>(smem), *mm = mo + W * S::kHeads * S::kPitch, *ml = mm + W * S::kHeads;
-        const int g = lane >> 2, t = lane & 3;
+        // Merge of the warps through shared memory, the uppermost kSlots into
+        // the next ones, and so on; the lowest ones' to whoever writes.
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float l = wp.l[n][j];
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-                const int head = w * S::kHeads + 8 * n + 2 * t + j;
-                if (g == 0) mm[head] = wp.m[n][j] - kShift<T>, ml[head] = l;
-#pragma unroll
-                for (int i = 0; i < DP / 16; ++i) {
-                    mo[head * S::kPitch + 16 * i + g] = wp.o[n][i][j];
-                    mo[head * S::kPitch + 16 * i + g + 8] = wp.o[n][i][2 + j];
-                }
+                for (int x = 4; x < 32; x <<= 1) wp.l[n][j] += __shfl_xor_sync(0xffffffffu, wp.l[n][j], x);
+                wp.m[n][j] -= kShift<T>;
             }
-        __syncthreads();
-        const bool whole = b0 == 0 && b1 == nb;
-        const int64_t slot = 2 * (int64_t)blockIdx.x + (b0 == 0 ? 1 : 0);
+        auto put = [&](int slot) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int head = slot * S::kHeads + 8 * n + 2 * t + j;
+                    if (8 * n + 2 * t + j >= rows) continue;
+                    if (g == 0) mm[head] = wp.m[n][j], ml[head] = wp.l[n][j];
+#pragma unroll
+                    for (int x = 0; x < DP / 16; ++x) {
+                        mo[head * S::kPitch + 16 * x + g] = wp.o[n][x][j];
+                        mo[head * S::kPitch + 16 * x + g + 8] = wp.o[n][x][2 + j];
+                    }
+                }
+        };
+        auto take = [&](int slot) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int head = slot * S::kHeads + 8 * n + 2 * t + j;
+                    if (8 * n + 2 * t + j >= rows) continue;
+                    const float m = mm[head], top = fmaxf(m, wp.m[n][j]), ref = top == minus_inf() ? 0.0f : top;
+                    const float f = power2(wp.m[n][j] - ref), e = power2(m - ref);
+                    wp.m[n][j] = top;
+                    wp.l[n][j] = fmaf(e, ml[head], f * wp.l[n][j]);
+#pragma unroll
+                    for (int x = 0; x < DP / 16; ++x) {
+                        wp.o[n][x][j] = fmaf(e, mo[head * S::kPitch + 16 * x + g], f * wp.o[n][x][j]);
+                        wp.o[n][x][2 + j] = fmaf(e, mo[head * S::kPitch + 16 * x + g + 8], f * wp.o[n][x][2 + j]);
+                    }
+                }
+            __syncwarp();
+        };
+        for (int top = W; top > 0; top -= MS) {   // a warp takes from and puts into the same slot
+            if (w >= top - MS && w < top) put(w - (top - MS));
+            __syncthreads();
+            if (w >= top - 2 * MS && w < top - MS) take(w - (top - 2 * MS));
+        }
+        const bool whole = jobs.b0 == 0 && jobs.b1 == jobs.nb;
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (jobs.b0 == 0 ? 1 : 0);
         for (int x = tid; x < rows * DP; x += THREADS) {
             const int head = x / DP, d = x % DP;
             float top = minus_inf(), sum = 0.0f, out = 0.0f;
 #pragma unroll
-            for (int k = 0; k < W; ++k) top = fmaxf(top, mm[k * S::kHeads + head]);
+            for (int k = 0; k < MS; ++k) top = fmaxf(top, mm[k * S::kHeads + head]);
             const float ref = top == minus_inf() ? 0.0f : top;
 #pragma unroll
-            for (int k = 0; k < W; ++k) {
-                const float f = exp2f(mm[k * S::kHeads + head] - ref);
+            for (int k = 0; k < MS; ++k) {
+                const float f = power2(mm[k * S::kHeads + head] - ref);
                 sum = fmaf(f, ml[k * S::kHeads + head], sum);
                 out = fmaf(f, mo[(k * S::kHeads + head) * S::kPitch + d], out);
             }
             if (whole) {
-                if (d < D) a.out[p.i * a.ldo + (int64_t)(qh + head) * D + d] = sum == 0.0f ? 0.0f : out / sum;
+                if (d < D) a.out[i * a.ldo + (qh + head) * D + d] = sum == 0.0f ? 0.0f : out / sum;
                 if (a.scores && d == 0) {
-                    float *st = a.stats + 2 * (p.i * a.heads + qh + head);
-                    st[0] = ref, st[1] = sum;
+                    float *st = a.stats + 2 * (i * a.heads + qh + head);
+                    st[0] = ref, st[1] = sum == 0.0f ? 0.0f : 1.0f / sum;
                 }
             } else {
                 a.part_o[(slot * S::kHeads + head) * DP + d] = out;
                 if (d == 0) a.part_ml[2 * (slot * S::kHeads + head)] = top, a.part_ml[2 * (slot * S::kHeads + head) + 1] = sum;
             }
         }
-        if (!whole && b0 == 0 && tid == 0) {   // this block's end cuts the job: who else has a part of it?
-            // Unit u is block c's if total c / blocks <= u < total (c + 1) / blocks (rounded down).
-            const int64_t last = u1 + (nb - b1) - 1, n = gridDim.x;
+        if (!whole && jobs.b0 == 0 && tid == 0) {   // this block's end cuts the job: who has the rest of it?
+            // Counted unit u is block c's if total c / blocks <= u < total (c + 1) / blocks (rounded down).
+            const int64_t last = end + (jobs.nb - jobs.b1) - 1, n = gridDim.x;
             int64_t c = last * n / total;
             while (total * (c + 1) / n <= last) ++c;
             while (total * c / n > last) --c;
-            a.split[3 * blockIdx.x] = p.i * per_seq + r;
+            a.split[3 * blockIdx.x] = i * per_seq + jobs.r;
             a.split[3 * blockIdx.x + 1] = c;
             a.split[3 * blockIdx.x + 2] = total;
         }
         __syncthreads();
     }
+    copies_wait<0>();
 }
 
 template <class T, int DP, int NT>
