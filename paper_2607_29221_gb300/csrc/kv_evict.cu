@@ -1,16 +1,29 @@
 // Eviction from the paged cache by gathered attention weight.
 //
 // Per (sequence, head): the rank of a slot is its weight as an ordered 32-bit
-// key; the E = len - keep least (key, slot) leave.  A radix selection finds
-// the E-th least key, one ordered pass the holes below keep and the stayers
-// from keep on, and the k-th hole takes the k-th stayer's row.  Only rows
-// that have to move do, and no row is both read and written.
+// key; the E = len - keep least (key, slot) leave.  The E-th least key is
+// found by narrowing [least, greatest] 2048-fold a pass with a histogram
+// (three passes at most: the keys of positive weights are their logarithms,
+// piecewise, so they spread over the bins).  The k-th hole below keep then
+// takes the k-th stayer from keep on: only rows that have to move do, and no
+// row is both read and written.
+//
+// Selection: bound by its trips to memory (length, page, weight) and barriers,
+// not by bytes.  A cluster of blocks takes a (sequence, head), each block a
+// stretch of slots whose keys it keeps in shared memory, with histograms and
+// counts summed through the cluster's shared memory.  Moves: bound by HBM, a
+// warp takes 32 and copies four rows at a time.
+#include <cooperative_groups.h>
+
 #include "kv_cache.cuh"
 
 namespace mosaic {
 namespace {
 
-constexpr int kSelectThreads = 1024;
+namespace cg = cooperative_groups;
+
+constexpr int kBins = 2048;
+constexpr int kMaxKeys = 48 * 1024;   // keys in shared memory; those beyond are looked up again each pass
 
 // Weights as unsigned keys in ascending order; NaN as -inf, -0 as 0.
 __device__ __forceinline__ uint32_t order_key(float w) {
@@ -18,13 +31,14 @@ __device__ __forceinline__ uint32_t order_key(float w) {
     const uint32_t u = __float_as_uint(w + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-constexpr uint32_t kKeyInf = 0xff800000u;   // order_key(+inf)
+constexpr uint32_t kKeyInf = 0xff800000u;   // order_key(+inf), the greatest
 
 struct EvictArgs {
     const int32_t *lens, *recent_from;
     int32_t *new_lens;
     int64_t max_len, keep, cap;   // cap: most moves of a (sequence, head)
     int32_t *count, *from, *to;
+    int keys;                     // keys a block has room for
 };
 
 __device__ __forceinline__ uint32_t slot_key(const KvView &kv, const EvictArgs &a, int64_t i, int h, int s, int from) {
@@ -32,89 +46,196 @@ __device__ __forceinline__ uint32_t slot_key(const KvView &kv, const EvictArgs &
     const int id = kv.page_of(i, (uint32_t)s, off);
     if (id < 0) return kKeyInf;
     const int64_t at = kv.mark(id, h, off);
+    const float w = kv.c.weight[at];
     if (a.recent_from && kv.c.position[at] >= from) return kKeyInf;
-    return order_key(kv.c.weight[at]);
+    return order_key(w);
 }
 
-// Exclusive sum of `v` over the block and its total (all threads call it).
-__device__ __forceinline__ int block_scan(int v, int *part, int &total) {
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    int x = v;
+template <int THREADS>
+struct SelectShared {
+    int hist[2][kBins];
+    int warp[3][THREADS / 32];
+    uint32_t low, high;   // this block's least and greatest key below kKeyInf
+    int finite, total[3];
+    uint32_t pick_low, pick_high;
+    int pick_rank;
+};
+
+// Exclusive sum over the block's warps of a warp-uniform value (one lane a
+// warp passes it); `total` gets the block's.
+template <int THREADS>
+__device__ __forceinline__ int warp_base(int v, int *part, int &total) {
+    const int w = threadIdx.x >> 5;
+    if ((threadIdx.x & 31) == 0) part[w] = v;
+    __syncthreads();
+    int before = 0;
+    total = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
+    for (int k = 0; k < THREADS / 32; ++k) {
+        const int x = part[k];
+        before += k < w ? x : 0;
+        total += x;
     }
-    if (lane == 31) part[w] = x;
-    __syncthreads();
-    int before = 0, all = 0;
-    for (int k = 0; k < kSelectThreads / 32; ++k) {
-        if (k < w) before += part[k];
-        all += part[k];
-    }
-    __syncthreads();
-    total = all;
-    return before + x - v;
+    return before;
 }
 
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(KvView kv, EvictArgs a) {
-    __shared__ int hist[256], part[kSelectThreads / 32];
-    __shared__ uint32_t prefix;
-    __shared__ int left;
-    const int h = blockIdx.x % kv.c.kv_heads;
-    const int64_t i = blockIdx.x / kv.c.kv_heads;
-    const int len = kv.length(a.lens, i, a.max_len), keep = (int)a.keep;
-    if (len <= keep) {
-        if (threadIdx.x == 0) a.count[blockIdx.x] = 0;
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView kv, EvictArgs a) {
+    extern __shared__ uint32_t keys[];
+    __shared__ SelectShared<THREADS> sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    const int64_t job = blockIdx.x / C, i = job / kv.c.kv_heads;
+    const int h = (int)(job % kv.c.kv_heads);
+    auto sync = [&] {
+        if (C > 1) cluster.sync();
+        else __syncthreads();
+    };
+    pdl_enter();
+    const int len = kv.length(a.lens, i, a.max_len), keep = (int)(a.keep < 0x7fffffff ? a.keep : 0x7fffffff);
+    if (len <= keep) {   // the whole cluster's
+        if (rank == 0 && tid == 0) a.count[job] = 0;
         return;
     }
     const int from = a.recent_from ? a.recent_from[i] : 0;
-    if (threadIdx.x == 0) prefix = 0, left = len - keep;
-    // The E-th least key, 8 bits a pass; `left`: its rank among the keys with this prefix.
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (threadIdx.x < 256) hist[threadIdx.x] = 0;
-        __syncthreads();
-        const uint32_t pre = prefix;
-        for (int s = threadIdx.x; s < len; s += kSelectThreads) {
-            const uint32_t k = slot_key(kv, a, i, h, s, from);
-            if (shift == 24 || (k >> (shift + 8)) == (pre >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+    const int per = (len + C - 1) / C, s0 = min(len, rank * per), n = min(len, s0 + per) - s0;
+    if (tid == 0) sh.low = 0xffffffffu, sh.high = 0, sh.finite = 0;
+    for (int b = tid; b < kBins; b += THREADS) sh.hist[0][b] = 0;
+    __syncthreads();
+    {
+        uint32_t low = 0xffffffffu, high = 0;
+        int finite = 0;
+#pragma unroll 4
+        for (int x = tid; x < n; x += THREADS) {
+            const uint32_t k = slot_key(kv, a, i, h, s0 + x, from);
+            if (x < a.keys) keys[x] = k;
+            if (k < kKeyInf) low = min(low, k), high = max(high, k), ++finite;
+        }
+        low = __reduce_min_sync(0xffffffffu, low);
+        high = __reduce_max_sync(0xffffffffu, high);
+        finite = __reduce_add_sync(0xffffffffu, finite);
+        if (lane == 0) atomicMin(&sh.low, low), atomicMax(&sh.high, high), atomicAdd(&sh.finite, finite);
+    }
+    auto key = [&](int x) { return x < a.keys ? keys[x] : slot_key(kv, a, i, h, s0 + x, from); };
+    sync();
+    uint32_t low = 0xffffffffu, high = 0;
+    int finite = 0;
+    for (int q = 0; q < C; ++q) {
+        const SelectShared<THREADS> *o = C > 1 ? cluster.map_shared_rank(&sh, q) : &sh;
+        low = min(low, o->low), high = max(high, o->high), finite += o->finite;
+    }
+    int left = len - keep;   // of the keys in [low, high], so many least ones leave
+    if (left > finite) low = high = kKeyInf, left -= finite;
+    for (int pass = 0; low < high; ++pass) {
+        int *hist = sh.hist[pass & 1];
+        const int shift = max(0, 21 - __clz((int)(high - low)));
+        for (int x = tid; x < n; x += THREADS) {
+            const uint32_t k = key(x);
+            if (k >= low && k <= high) atomicAdd(&hist[(k - low) >> shift], 1);
+        }
+        sync();
+        // The other histogram has been read by everyone (they passed this barrier).
+        for (int b = tid; b < kBins; b += THREADS) sh.hist[~pass & 1][b] = 0;
+        constexpr int kOwn = kBins / THREADS;
+        int own[kOwn], sum = 0;
+#pragma unroll
+        for (int b = 0; b < kOwn; ++b) own[b] = 0;
+        for (int q = 0; q < C; ++q) {
+            const int *o = C > 1 ? cluster.map_shared_rank(hist, q) : hist;
+#pragma unroll
+            for (int b = 0; b < kOwn; ++b) own[b] += o[tid * kOwn + b];
+        }
+#pragma unroll
+        for (int b = 0; b < kOwn; ++b) sum += own[b];
+        int incl = sum, all;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        const int of_warp = __shfl_sync(0xffffffffu, incl, 31);
+        int before = warp_base<THREADS>(of_warp, sh.warp[0], all) + incl - sum;
+        if (before < left && left <= before + sum) {
+#pragma unroll
+            for (int b = 0; b < kOwn; ++b) {
+                if (before < left && left <= before + own[b]) {
+                    const uint32_t to = low + ((uint32_t)(tid * kOwn + b) << shift);
+                    sh.pick_low = to;
+                    sh.pick_high = min(high, to + ((1u << shift) - 1));
+                    sh.pick_rank = left - before;
+                }
+                before += own[b];
+            }
         }
         __syncthreads();
-        if (threadIdx.x == 0) {
-            int r = left, b = 0;
-            while (hist[b] < r) r -= hist[b++];
-            prefix = pre | ((uint32_t)b << shift);
-            left = r;
-        }
+        low = sh.pick_low, high = sh.pick_high, left = sh.pick_rank;
         __syncthreads();
     }
-    const uint32_t least = prefix;
-    const int ties = left;   // of the slots with that key, so many leave
-    int32_t *to = a.to + (int64_t)blockIdx.x * a.cap, *src = a.from + (int64_t)blockIdx.x * a.cap;
-    int seen = 0, holes = 0, stays = 0, total;
-    for (int s0 = 0; s0 < len; s0 += kSelectThreads) {
-        const int s = s0 + threadIdx.x;
-        const bool in = s < len;
-        const uint32_t k = in ? slot_key(kv, a, i, h, s, from) : 0xffffffffu;
-        const bool tie = in && k == least;
-        const int rank = seen + block_scan(tie, part, total);
-        seen += total;
-        const bool out = in && (k < least || (tie && rank < ties));
-        const bool hole = out && s < keep, stay = in && !out && s >= keep;
-        int at = holes + block_scan(hole, part, total);
-        holes += total;
-        if (hole && at < a.cap) to[at] = s;
-        at = stays + block_scan(stay, part, total);
-        stays += total;
-        if (stay && at < a.cap) src[at] = s;
+    const uint32_t least = low;
+    const int ties = left;   // of the slots with that key, the first so many leave
+
+    // A warp a stretch: ties, then holes and stayers, before each.
+    const int run = ((n + THREADS / 32 - 1) / (THREADS / 32) + 31) / 32 * 32;
+    const int x0 = min(n, w * run), x1 = min(n, x0 + run);
+    auto before_block = [&](int which) {
+        int v = 0;
+        if (C > 1)
+            for (int q = 0; q < rank; ++q) v += cluster.map_shared_rank(&sh, q)->total[which];
+        return v;
+    };
+    int count = 0, all;
+    for (int x = x0 + lane; x < x1; x += 32) count += key(x) == least;
+    count = __reduce_add_sync(0xffffffffu, count);
+    int seen = warp_base<THREADS>(count, sh.warp[0], all);
+    if (tid == 0) sh.total[0] = all;
+    sync();
+    seen += before_block(0);
+    // Every lane's slot: whether it leaves, given the ties before the warp's 32.
+    auto leaves = [&](int x, int &ties_before) {
+        const bool in = x < x1;
+        const uint32_t k = in ? key(x) : 0xffffffffu;
+        const uint32_t same = __ballot_sync(0xffffffffu, in && k == least);
+        const int mine = ties_before + __popc(same & ((1u << lane) - 1));
+        ties_before += __popc(same);
+        return in && (k < least || (k == least && mine < ties));
+    };
+    int holes = 0, stays = 0;
+    {
+        int t = seen;
+        for (int b = x0; b < x1; b += 32) {
+            const int x = b + lane, s = s0 + x;
+            const bool out = leaves(x, t);
+            holes += __popc(__ballot_sync(0xffffffffu, out && s < keep));
+            stays += __popc(__ballot_sync(0xffffffffu, x < x1 && !out && s >= keep));
+        }
     }
-    if (threadIdx.x == 0) a.count[blockIdx.x] = holes < a.cap ? holes : (int)a.cap;
+    int hole = warp_base<THREADS>(holes, sh.warp[1], all);
+    if (tid == 0) sh.total[1] = all;
+    int stay = warp_base<THREADS>(stays, sh.warp[2], all);
+    if (tid == 0) sh.total[2] = all;
+    sync();
+    hole += before_block(1), stay += before_block(2);
+    if (rank == C - 1 && tid == 0) a.count[job] = before_block(1) + sh.total[1];   // at most a.cap
+    int32_t *to = a.to + job * a.cap, *src = a.from + job * a.cap;
+    for (int b = x0; b < x1; b += 32) {
+        const int x = b + lane, s = s0 + x;
+        const bool out = leaves(x, seen);
+        const uint32_t hm = __ballot_sync(0xffffffffu, out && s < keep);
+        const uint32_t sm = __ballot_sync(0xffffffffu, x < x1 && !out && s >= keep);
+        const uint32_t under = (1u << lane) - 1;
+        if (hm >> lane & 1) to[hole + __popc(hm & under)] = s;
+        if (sm >> lane & 1) src[stay + __popc(sm & under)] = s;
+        hole += __popc(hm), stay += __popc(sm);
+    }
+    if (C > 1) cluster.sync();   // the others have read this block's counts
 }
 
-// A warp a move: key and value row, position and weight.
+// A warp 32 moves at a time: key and value row, position and weight.
 __global__ void __launch_bounds__(256) evict_move_kernel(KvView kv, EvictArgs a, int chunks) {
+    pdl_enter();
     const int64_t job = blockIdx.x / chunks;
-    const int part = blockIdx.x % chunks;
+    const int part = (int)(blockIdx.x % chunks);
     const int h = (int)(job % kv.c.kv_heads), lane = threadIdx.x & 31;
     const int64_t i = job / kv.c.kv_heads;
     if (part == 0 && h == 0 && threadIdx.x == 0) {
@@ -123,20 +244,37 @@ __global__ void __launch_bounds__(256) evict_move_kernel(KvView kv, EvictArgs a,
     }
     const int count = a.count[job];
     const int es = kv.c.type == MOSAIC_KV_F32 ? 4 : 2, quads = kv.c.head_dim * es / 16;
-    for (int m = part * 8 + (threadIdx.x >> 5); m < count; m += chunks * 8) {
-        uint32_t so, to;
-        const int sid = kv.page_of(i, (uint32_t)a.from[job * a.cap + m], so);
-        const int tid = kv.page_of(i, (uint32_t)a.to[job * a.cap + m], to);
-        if (sid < 0 || tid < 0) continue;
-        const int64_t se = kv.element(sid, h, so) * es, te = kv.element(tid, h, to) * es;
-        for (int b = lane; b < 2 * quads; b += 32) {
-            char *pool = static_cast<char *>(b < quads ? kv.c.k : kv.c.v);
-            const int o = 16 * (b < quads ? b : b - quads);
-            *reinterpret_cast<uint4 *>(pool + te + o) = *reinterpret_cast<const uint4 *>(pool + se + o);
+    char *const kp = static_cast<char *>(kv.c.k), *const vp = static_cast<char *>(kv.c.v);
+    for (int m0 = 32 * (part * 8 + (threadIdx.x >> 5)); m0 < count; m0 += chunks * 256) {
+        int64_t se = -1, te = 0;
+        if (m0 + lane < count) {
+            uint32_t so, to;
+            const int sid = kv.page_of(i, (uint32_t)a.from[job * a.cap + m0 + lane], so);
+            const int tid = kv.page_of(i, (uint32_t)a.to[job * a.cap + m0 + lane], to);
+            if (sid >= 0 && tid >= 0) {
+                se = kv.element(sid, h, so) * es, te = kv.element(tid, h, to) * es;
+                const int64_t sm = kv.mark(sid, h, so), tm = kv.mark(tid, h, to);
+                kv.c.weight[tm] = kv.c.weight[sm];
+                if (kv.c.position) kv.c.position[tm] = kv.c.position[sm];
+            }
         }
-        const int64_t sm = kv.mark(sid, h, so), tm = kv.mark(tid, h, to);
-        if (lane == 0) kv.c.weight[tm] = kv.c.weight[sm];
-        if (lane == 1 && kv.c.position) kv.c.position[tm] = kv.c.position[sm];
+        for (int j0 = 0; j0 < 32 && m0 + j0 < count; j0 += 4) {
+            int64_t s[4], t[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                s[j] = __shfl_sync(0xffffffffu, se, j0 + j), t[j] = __shfl_sync(0xffffffffu, te, j0 + j);
+            for (int b = lane; b < 2 * quads; b += 32) {
+                char *pool = b < quads ? kp : vp;
+                const int o = 16 * (b < quads ? b : b - quads);
+                uint4 x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (s[j] >= 0) x[j] = *reinterpret_cast<const uint4 *>(pool + s[j] + o);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (s[j] >= 0) *reinterpret_cast<uint4 *>(pool + t[j] + o) = x[j];
+            }
+        }
     }
 }
 
@@ -145,6 +283,26 @@ int64_t most_moves(int64_t max_len, int64_t keep) {
     return over <= 0 ? 0 : over < keep ? over : keep;
 }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+template <int THREADS>
+mosaic_status select_launch(const KvView &kv, const EvictArgs &a, int64_t blocks, int cluster, cudaStream_t st) {
+    static std::atomic<unsigned long long> done{0};
+    if (!ensure_smem_limit(done, evict_select_kernel<THREADS>, 4 * kMaxKeys)) return MOSAIC_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = 4 * (size_t)a.keys;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    KernelSpan span("evict_select", st);
+    cudaLaunchKernelEx(&cfg, evict_select_kernel<THREADS>, kv, a);   // a failure is read by launch_status
+    return launch_status();
+}
 
 }  // namespace
 }  // namespace mosaic
@@ -168,28 +326,35 @@ mosaic_status mosaic_kv_evict(const mosaic_kv_cache *cache, const int32_t *lens,
     if (cache->seqs == 0) return MOSAIC_OK;
     if (!lens || !new_lens || !cache->weight || (recent_from && !cache->position)) return MOSAIC_ERR_ARG;
     const int64_t jobs = cache->seqs * cache->kv_heads;
-    if (jobs > 0x7fffffff) return MOSAIC_ERR_SHAPE;
+    if (jobs > 0x7fffffff / 8) return MOSAIC_ERR_SHAPE;
     if (ws_bytes < mosaic_kv_evict_workspace(cache, max_len, keep)) return MOSAIC_ERR_WORKSPACE;
     if (!ws) return MOSAIC_ERR_ARG;
     if (reinterpret_cast<uintptr_t>(ws) % 4) return MOSAIC_ERR_ALIGN;
-    EvictArgs a = {lens, recent_from, new_lens, max_len, keep, most_moves(max_len, keep), nullptr, nullptr, nullptr};
+    EvictArgs a = {lens, recent_from, new_lens, max_len, keep, most_moves(max_len, keep), nullptr, nullptr, nullptr, 0};
     char *w = static_cast<char *>(ws);
     a.count = reinterpret_cast<int32_t *>(w);
     a.from = reinterpret_cast<int32_t *>(w + up256(4 * (size_t)jobs));
     a.to = a.from + up256(4 * (size_t)(jobs * a.cap)) / 4;
     cudaStream_t st = as_stream(stream);
     const KvView kv(*cache);
-    {
-        KernelSpan span("evict_select", st);
-        evict_select_kernel<<<(unsigned)jobs, kSelectThreads, 0, st>>>(kv, a);
-    }
-    MOSAIC_TRY(launch_status());
-    int64_t chunks = (a.cap + 63) / 64;
+    // As many blocks a job as there are SMs for, of 2048 slots at least.
+    int cluster = 1;
+    while (cluster < 8 && jobs * cluster * 2 <= 152 && max_len / (cluster * 2) >= 2048) cluster *= 2;
+    while (cluster < 8 && (max_len + cluster - 1) / cluster > kMaxKeys) cluster *= 2;
+    const int64_t per = (max_len + cluster - 1) / cluster;
+    a.keys = (int)(per < kMaxKeys ? per : kMaxKeys);
+    if (per > 8192) MOSAIC_TRY(select_launch<1024>(kv, a, jobs * cluster, cluster, st));
+    else MOSAIC_TRY(select_launch<512>(kv, a, jobs * cluster, cluster, st));
+    // One wave of blocks for the moves (32 a warp, 256 a block).
+    constexpr int64_t kWave = 152 * 8;
+    int64_t chunks = (a.cap + 255) / 256;
+    if (chunks * jobs > kWave) chunks = kWave / jobs;
     if (chunks < 1) chunks = 1;
-    while (chunks > 1 && chunks * jobs > 16384) chunks = (chunks + 1) / 2;
     {
         KernelSpan span("evict_move", st);
-        evict_move_kernel<<<(unsigned)(chunks * jobs), 256, 0, st>>>(kv, a, (int)chunks);
+        const dim3 grid((unsigned)(chunks * jobs));
+        if (chunks * jobs <= kWave) pdl_launch(evict_move_kernel, grid, dim3(256), 0, st, kv, a, (int)chunks);
+        else evict_move_kernel<<<grid, 256, 0, st>>>(kv, a, (int)chunks);
     }
     return launch_status();
 }
