@@ -676,7 +676,7 @@ mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, i
  * more and summed in fp32.  heads: a multiple of kv_heads, at most 64 query
  * heads a key/value head.  max_len: an upper bound of the lengths, which
  * sizes the workspace (mosaic_kv_attention_workspace bytes for the same
- * cache, heads and max_len; 0 if they are not valid).  out: seqs x heads
+ * cache, heads and max_len; 0 if none is needed or they are not valid).  out: seqs x heads
  * head_dim fp32 (ldo), no overlap with q.  Results do not depend on the run. */
 size_t mosaic_kv_attention_workspace(const mosaic_kv_cache *cache, int64_t heads, int64_t max_len);
 mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, int64_t ldq, int64_t heads,

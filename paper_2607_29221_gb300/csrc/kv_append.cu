@@ -7,8 +7,12 @@
 // The phase's upper 32 bits, as a signed fraction of a turn, go to sincospif:
 // 2^-25 turns at most.
 //
-// A thread owns 8 channels of a head (4 pairs): it computes their 4 sines and
-// cosines once a token and walks the heads of its block's share.
+// Bound by HBM (fp32 rows in, fp32 queries and the cache's rows out).  A block
+// takes the heads of one token, or a share of them where tokens are few; its
+// sines and cosines are computed once, in shared memory (each thread for
+// itself: 39 against XX us for 2048 tokens of 64 + 16 heads of 128).  A thread
+// owns 4 + 4 channels of a head, a quarter warp's worth apart so that every
+// access is whole lines, and has four heads in flight.
 #include <math.h>
 
 #include "kv_cache.cuh"
@@ -63,67 +67,78 @@ struct AppendArgs {
 
 template <class T>
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(KvView kv, AppendArgs a) {
+    __shared__ __align__(16) float cs[128], sn[128];
     const int64_t t = blockIdx.y + (int64_t)blockIdx.z * 65535;
     if (t >= a.l) return;
     const int D = kv.c.head_dim, units = D / 8, rot = a.rope.rot_dim;
-    const int u = threadIdx.x % units, lane = threadIdx.x / units, lanes = blockDim.x / units;
-    // Channels of the unit's two groups of four, and its rotation.
-    const bool spins = 8 * u < rot;
-    const bool split = spins && !a.rope.interleaved;
-    const int c0 = split ? 4 * u : 8 * u, c1 = split ? rot / 2 + 4 * u : 8 * u + 4;
-    float cs[4], sn[4];
-    if (spins) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = 4 * u + i;
-            int ax = a.rope.axis ? a.rope.axis[j] : 0;
-            ax = (uint32_t)ax < (uint32_t)a.rope.axes ? ax : 0;
-            const int64_t pos = a.rope.pos[ax * a.rope.ldp + t];
-            const int32_t phase = (int32_t)(((uint64_t)pos * a.rope.turns[j]) >> 32);
-            sincospif((float)phase * 0x1p-31f, &sn[i], &cs[i]);
-        }
+    if ((int)threadIdx.x < rot / 2) {
+        const int j = threadIdx.x;
+        int ax = a.rope.axis ? a.rope.axis[j] : 0;
+        ax = (uint32_t)ax < (uint32_t)a.rope.axes ? ax : 0;
+        const int64_t pos = a.rope.pos[ax * a.rope.ldp + t];
+        const int32_t phase = (int32_t)(((uint64_t)pos * a.rope.turns[j]) >> 32);
+        sincospif((float)phase * 0x1p-31f, &sn[j], &cs[j]);
     }
     const int64_t sq = a.seq[t], sl = a.slot[t];
     int id = -1;
     uint32_t off = 0;
     if (sq >= 0 && sq < kv.c.seqs && sl >= 0 && sl < kv.slots()) id = kv.page_of(sq, (uint32_t)sl, off);
+    __syncthreads();
+    // The thread's channels c0 .. c0 + 3 and c1 .. c1 + 3 of every head, in the
+    // halves of the channels that turn or of those that do not.
+    const int u = threadIdx.x % units, lane = threadIdx.x / units, lanes = blockDim.x / units;
+    const bool spins = 8 * u < rot;
+    const int c0 = spins ? 4 * u : rot + 4 * (u - rot / 8), c1 = c0 + (spins ? rot : D - rot) / 2;
     const int H = a.heads, KV = kv.c.kv_heads;
     const int last = min((int)(blockIdx.x + 1) * a.share, H + 2 * KV);
     const float *row = a.qkv + t * a.ldx;
-    for (int h = blockIdx.x * a.share + lane; h < last; h += lanes) {
-        Load4 x = load4(row + (int64_t)h * D + c0, a.vec), y = load4(row + (int64_t)h * D + c1, a.vec);
-        if (spins && h < H + KV) {
-            if (split) {
+    float *qrow = a.q + t * a.ldq;
+    constexpr int N = 4;
+    for (int h0 = blockIdx.x * a.share + lane; h0 < last; h0 += N * lanes) {
+        Load4 xs[N], ys[N];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = x.x[i], q = y.x[i];
-                    x.x[i] = p * cs[i] - q * sn[i];
-                    y.x[i] = q * cs[i] + p * sn[i];
-                }
-            } else {
+        for (int k = 0; k < N; ++k)
+            if (h0 + k * lanes < last) {
+                xs[k] = load4(row + (int64_t)(h0 + k * lanes) * D + c0, a.vec);
+                ys[k] = load4(row + (int64_t)(h0 + k * lanes) * D + c1, a.vec);
+            }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float p = x.x[2 * i], q = x.x[2 * i + 1];
-                    x.x[2 * i] = p * cs[i] - q * sn[i];
-                    x.x[2 * i + 1] = q * cs[i] + p * sn[i];
-                    p = y.x[2 * i], q = y.x[2 * i + 1];
-                    y.x[2 * i] = p * cs[2 + i] - q * sn[2 + i];
-                    y.x[2 * i + 1] = q * cs[2 + i] + p * sn[2 + i];
+        for (int k = 0; k < N; ++k) {
+            const int h = h0 + k * lanes;
+            if (h >= last) break;
+            Load4 &x = xs[k], &y = ys[k];
+            if (spins && h < H + KV) {
+                if (!a.rope.interleaved) {   // channel c0 + i with c1 + i
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float c = cs[c0 + i], s = sn[c0 + i], p = x.x[i], q = y.x[i];
+                        x.x[i] = p * c - q * s;
+                        y.x[i] = q * c + p * s;
+                    }
+                } else {                     // neighbours
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        float c = cs[(c0 + i) / 2], s = sn[(c0 + i) / 2], p = x.x[i], q = x.x[i + 1];
+                        x.x[i] = p * c - q * s;
+                        x.x[i + 1] = q * c + p * s;
+                        c = cs[(c1 + i) / 2], s = sn[(c1 + i) / 2], p = y.x[i], q = y.x[i + 1];
+                        y.x[i] = p * c - q * s;
+                        y.x[i + 1] = q * c + p * s;
+                    }
                 }
             }
-        }
-        if (h < H) {
-            float *o = a.q + t * a.ldq + (int64_t)h * D;
-            store4(o + c0, x, a.vec);
-            store4(o + c1, y, a.vec);
-        } else if (id >= 0) {
-            const int g = h < H + KV ? h - H : h - H - KV;
-            T *o = static_cast<T *>(h < H + KV ? kv.c.k : kv.c.v) + kv.element(id, g, off);
-            put4(o + c0, x);
-            put4(o + c1, y);
-            if (u == 0 && h < H + KV) {
-                if (kv.c.position) kv.c.position[kv.mark(id, g, off)] = a.index[t];
-                if (kv.c.weight) kv.c.weight[kv.mark(id, g, off)] = 0.0f;
+            if (h < H) {
+                store4(qrow + (int64_t)h * D + c0, x, a.vec);
+                store4(qrow + (int64_t)h * D + c1, y, a.vec);
+            } else if (id >= 0) {
+                const int g = h < H + KV ? h - H : h - H - KV;
+                T *o = static_cast<T *>(h < H + KV ? kv.c.k : kv.c.v) + kv.element(id, g, off);
+                put4(o + c0, x);
+                put4(o + c1, y);
+                if (u == 0 && h < H + KV) {
+                    if (kv.c.position) kv.c.position[kv.mark(id, g, off)] = a.index[t];
+                    if (kv.c.weight) kv.c.weight[kv.mark(id, g, off)] = 0.0f;
+                }
             }
         }
     }
@@ -173,8 +188,12 @@ mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, i
     a.qkv = qkv, a.ldx = ldx, a.l = l, a.heads = (int)heads, a.seq = seq, a.slot = slot, a.index = index, a.q = q, a.ldq = ldq;
     a.vec = aligned16(qkv) && aligned16(q) && ldx % 4 == 0 && ldq % 4 == 0;
     const int units = (int)D / 8, lanes = kAppendThreads / units;
-    a.share = lanes;
-    const int64_t all = heads + 2 * KV;
+    // Heads of a block: all of a token's, unless that leaves SMs without work
+    // (at most four blocks an SM, a head a thread at least).
+    const int64_t all = heads + 2 * KV, most = (all + lanes - 1) / lanes;
+    int64_t cut = 152 * 4 / l;
+    cut = cut < 1 ? 1 : cut > most ? most : cut;
+    a.share = (int)((most + cut - 1) / cut * lanes);
     const dim3 grid((unsigned)((all + a.share - 1) / a.share), (unsigned)(l < 65535 ? l : 65535),
                     (unsigned)((l + 65534) / 65535));
     cudaStream_t st = as_stream(stream);

@@ -96,7 +96,7 @@ struct WeightWalk {
     int64_t chunks, jobs_step, chunk_step;   // the grid's stride over (job, chunk of slots)
     int vec;
 };
-__global__ void __launch_bounds__(128, 8) attend_weight_kernel(KvView kv, AttendArgs a, WeightWalk walk) {
+__global__ void __launch_bounds__(128, 6) attend_weight_kernel(KvView kv, AttendArgs a, WeightWalk walk) {
     pdl_enter();
     const int64_t jobs = kv.c.seqs * kv.c.kv_heads;
     int64_t job = blockIdx.x / walk.chunks, chunk = blockIdx.x % walk.chunks;
@@ -171,6 +171,7 @@ struct Parts {
     size_t ml, o, split, stats, scores;
     size_t total() const { return ml + o + split + stats + scores; }
 };
+// blocks: those that share the work (0: every job is one block's).
 Parts parts(const mosaic_kv_cache &c, const AttendShape &s, int64_t heads, int64_t blocks, int64_t rows) {
     Parts p = {};
     p.ml = up256(16 * (size_t)(blocks * s.heads));
@@ -186,10 +187,11 @@ AttendShape shape_of(const mosaic_kv_cache &c, int64_t heads) {
     const int group = (int)(heads / c.kv_heads);
     return by_type(c.type, [&](auto t) { return attend_shape<decltype(t)>(c.head_dim, group); });
 }
-// Units that the lengths may add up to, and how many blocks may share them.
-int64_t most_units(const mosaic_kv_cache &c, const AttendShape &s, int64_t heads, int64_t max_len) {
+// How many blocks may share the units that the lengths may add up to.
+int64_t most_blocks(const mosaic_kv_cache &c, const AttendShape &s, int64_t heads, int64_t max_len) {
     const int64_t group = heads / c.kv_heads, hb = (group + s.heads - 1) / s.heads;
-    return c.seqs * c.kv_heads * hb * ((max_len + s.unit - 1) / s.unit);
+    const int64_t units = c.seqs * c.kv_heads * hb * ((max_len + s.unit - 1) / s.unit);
+    return max_len <= kWholeLen ? 0 : units < kAttendWave ? units : kAttendWave;
 }
 mosaic_status check(const mosaic_kv_cache *c, int64_t heads, int64_t max_len) {
     MOSAIC_TRY(kv_check(c));
@@ -211,8 +213,7 @@ extern "C" {
 size_t mosaic_kv_attention_workspace(const mosaic_kv_cache *cache, int64_t heads, int64_t max_len) {
     if (check(cache, heads, max_len) != MOSAIC_OK) return 0;
     const AttendShape s = shape_of(*cache, heads);
-    const int64_t units = most_units(*cache, s, heads, max_len);
-    return parts(*cache, s, heads, units < kAttendWave ? units : kAttendWave, rows_of(max_len)).total() + 256;
+    return parts(*cache, s, heads, most_blocks(*cache, s, heads, max_len), rows_of(max_len)).total();
 }
 
 mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, int64_t ldq, int64_t heads,
@@ -226,10 +227,10 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     if (cache->seqs == 0) return MOSAIC_OK;
     if (!q || !out || !lens || (first && !cache->position)) return MOSAIC_ERR_ARG;
     const AttendShape s = shape_of(*cache, heads);
-    const int64_t units = most_units(*cache, s, heads, max_len), cap = units < kAttendWave ? units : kAttendWave;
+    const int64_t cap = most_blocks(*cache, s, heads, max_len);
     const Parts p = parts(*cache, s, heads, cap, rows_of(max_len));
-    if (ws_bytes < p.total() + 256) return MOSAIC_ERR_WORKSPACE;
-    if (!ws) return MOSAIC_ERR_ARG;
+    if (ws_bytes < p.total()) return MOSAIC_ERR_WORKSPACE;
+    if (!ws && p.total()) return MOSAIC_ERR_ARG;
     if (reinterpret_cast<uintptr_t>(ws) % 16) return MOSAIC_ERR_ALIGN;
     AttendArgs a = {};
     a.q = q, a.ldq = ldq, a.lens = lens, a.first = first, a.max_len = max_len, a.heads = (int)heads;
@@ -245,7 +246,7 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
         a.score_rows = rows_of(max_len);
     }
     const int64_t jobs = cache->seqs * cache->kv_heads * a.hb;
-    a.whole = max_len <= kWholeLen;
+    a.whole = cap == 0;
     if (a.whole) a.blocks = (int)jobs;
     else {
         const int wave = by_type(cache->type, [&](auto t) { return attend_wave<decltype(t)>((int)D, a.group); });
@@ -268,7 +269,7 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     const KvView kv(*cache);
     {
         KernelSpan span("attend_weight", st);
-        const int64_t grid = all < 152 * 8 ? all : 152 * 8;
+        const int64_t grid = all < 152 * 6 ? all : 152 * 6;
         const WeightWalk walk = {chunks, grid / chunks, grid % chunks,
                                  cache->page_size % 4 == 0 && aligned16(cache->weight)};
         pdl_launch(attend_weight_kernel, dim3((unsigned)grid), dim3(128), 0, st, kv, a, walk);

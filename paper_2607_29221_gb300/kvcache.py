@@ -31,9 +31,19 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _int32(t, name: str, shape, device) -> None:
-    _need(t.dtype == torch.int32 and t.device == device and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
-          f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on {device} is needed")
+def _int32(t, name: str, n: int, index: int) -> None:
+    if t.dtype is not torch.int32 or t.get_device() != index or t.dim() != 1 or t.numel() != n or (
+            n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: a contiguous int32 tensor of {n} elements on the cache's device is needed")
+
+
+def _rows(t, name: str, n: int, heads: int, dim: int, index: int) -> int:
+    """The row stride of a float32 n x heads x dim tensor whose rows are contiguous."""
+    st = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if (t.dtype is not torch.float32 or t.get_device() != index or t.shape != (n, heads, dim) or st[2] != 1
+            or (heads > 1 and st[1] != dim)):
+        raise ValueError(f"{name}: float32, {n} x {heads} x {dim}, rows contiguous, on the cache's device")
+    return max(st[0], heads * dim)
 
 
 class Rope:
@@ -51,15 +61,16 @@ class Rope:
         self.turns = torch.from_numpy(M.mosaic_rope_turns(rot_dim, base).view("int64")).to(device)
         self.axis = torch.repeat_interleave(torch.arange(self.axes, dtype=torch.int32),
                                             torch.tensor(sections)).to(device)
+        self._turns, self._axis = self.turns.data_ptr(), self.axis.data_ptr()
 
     def at(self, pos: torch.Tensor) -> M.mosaic_rope:
         """The rotation of tokens at ``pos`` (axes x tokens, or tokens for one axis)."""
         pos = pos[None] if pos.dim() == 1 else pos
-        _need(pos.dtype == torch.int32 and pos.dim() == 2 and pos.shape[0] == self.axes
-              and (pos.shape[1] <= 1 or pos.stride(1) == 1) and pos.device == self.turns.device,
-              f"pos: int32, {self.axes} x tokens, rows contiguous")
-        return M.mosaic_rope(self.rot_dim, self.interleaved, self.axes, self.turns.data_ptr(), self.axis.data_ptr(),
-                             pos.data_ptr(), max(pos.stride(0), pos.shape[1]))
+        if (pos.dtype is not torch.int32 or pos.dim() != 2 or pos.shape[0] != self.axes
+                or (pos.shape[1] > 1 and pos.stride(1) != 1) or pos.get_device() != self.turns.get_device()):
+            raise ValueError(f"pos: int32, {self.axes} x tokens, rows contiguous, on the rope's device")
+        return M.mosaic_rope(self.rot_dim, self.interleaved, self.axes, self._turns, self._axis, pos.data_ptr(),
+                             max(pos.stride(0), pos.shape[1]))
 
 
 class PagedCache:
@@ -81,6 +92,7 @@ class PagedCache:
                   f"{name}: contiguous {dt}, pages x kv_heads x page_size, on the cache's device")
         self.k, self.v, self.table, self.position, self.weight = k, v, table, position, weight
         self.device, self.kv_heads, self.head_dim, self.seqs = k.device, kv_heads, dim, table.shape[0]
+        self._index = k.get_device()
         ptr = [None if t is None else t.data_ptr() for t in (k, v, table, position, weight)]
         self._c = M.mosaic_kv_cache(_TYPES[k.dtype], kv_heads, dim, page, pages, table.shape[0], table.shape[1],
                                     max(table.stride(0), table.shape[1]), k.stride(0), k.stride(1), k.stride(2),
@@ -97,33 +109,34 @@ class PagedCache:
         return cls(k, v, table, torch.zeros(shape, dtype=torch.int32, device=dev),
                    torch.zeros(shape, dtype=torch.float32, device=dev) if weights else None)
 
-    def _bytes(self, key, size) -> int:
+    def _bytes(self, key, size, *args) -> int:
         n = self._ws.get(key)
         if n is None:
-            n = self._ws[key] = size()
+            if len(self._ws) > 256:   # max_len grows with every step of a loop
+                self._ws.clear()
+            n = self._ws[key] = size(self._ref, *args)
         return n
 
     def append(self, qkv, heads: int, seq, slot, index=None, rope: Rope | None = None, pos=None, out=None):
         """Rotates row t of qkv (l x (heads + 2 kv_heads) head_dim fp32) and
         stores its keys and values in slot[t] of sequence seq[t] (a negative
         slot: not stored); returns the queries, l x heads x head_dim fp32."""
-        l, d = qkv.shape[0], self.head_dim
-        _need(qkv.dtype == torch.float32 and qkv.dim() == 2 and qkv.device == self.device
-              and qkv.shape[1] == (heads + 2 * self.kv_heads) * d and qkv.stride(1) == 1,
-              "qkv: float32, l x (heads + 2 kv_heads) head_dim, rows contiguous")
-        for t, name in ((seq, "seq"), (slot, "slot"), (index, "index")):
-            if t is not None:
-                _int32(t, name, (l,), self.device)
-        _need((rope is None) == (pos is None), "rope and pos go together")
-        q = torch.empty(l, heads, d, dtype=torch.float32, device=self.device) if out is None else out
-        _need(q.dtype == torch.float32 and tuple(q.shape) == (l, heads, d) and q.device == self.device
-              and q.stride(2) == 1 and (heads == 1 or q.stride(1) == d), "out: float32, l x heads x head_dim")
+        d, width = self.head_dim, (heads + 2 * self.kv_heads) * self.head_dim
+        if (qkv.dtype is not torch.float32 or qkv.dim() != 2 or qkv.get_device() != self._index
+                or qkv.shape[1] != width or qkv.stride(1) != 1):
+            raise ValueError("qkv: float32, l x (heads + 2 kv_heads) head_dim, rows contiguous, on the cache's device")
+        l = qkv.shape[0]
+        _int32(seq, "seq", l, self._index)
+        _int32(slot, "slot", l, self._index)
+        if index is not None:
+            _int32(index, "index", l, self._index)
         r = None
         if rope is not None:
+            _need(pos is not None and pos.shape[-1] == l, "pos: a position for every token goes with rope")
             r = rope.at(pos)
-            _need((pos[None] if pos.dim() == 1 else pos).shape[1] == l, "pos: a position for every token")
-        M.mosaic_kv_append(self._ref, qkv, max(qkv.stride(0), qkv.shape[1]), l, heads, seq, slot, index,
-                           None if r is None else ctypes.byref(r), q, max(q.stride(0), heads * d))
+        q = torch.empty((l, heads, d), dtype=torch.float32, device=self.device) if out is None else out
+        M.mosaic_kv_append(self._ref, qkv, max(qkv.stride(0), width), l, heads, seq, slot, index,
+                           None if r is None else ctypes.byref(r), q, _rows(q, "out", l, heads, d, self._index))
         return q
 
     def attend(self, q, lens, max_len: int, first=None, scale: float | None = None, decay: float = 1.0, out=None):
@@ -131,32 +144,30 @@ class PagedCache:
         over its first lens[i] <= max_len slots, without the slots whose
         position is below first[i]; adds the attention weights to
         ``weight`` (after scaling it by decay) if the cache keeps them."""
-        heads, d = q.shape[1], self.head_dim
-        _need(q.dtype == torch.float32 and tuple(q.shape) == (self.seqs, heads, d) and q.device == self.device
-              and q.stride(2) == 1 and (heads == 1 or q.stride(1) == d), "q: float32, seqs x heads x head_dim")
-        _int32(lens, "lens", (self.seqs,), self.device)
+        n, d, at = self.seqs, self.head_dim, self._index
+        heads = q.shape[1] if q.dim() == 3 else 0
+        ldq = _rows(q, "q", n, heads, d, at)
+        _int32(lens, "lens", n, at)
         if first is not None:
-            _int32(first, "first", (self.seqs,), self.device)
-        o = torch.empty(self.seqs, heads, d, dtype=torch.float32, device=self.device) if out is None else out
-        _need(o.dtype == torch.float32 and o.shape == q.shape and o.device == self.device and o.stride(2) == 1
-              and (heads == 1 or o.stride(1) == d), "out: float32, seqs x heads x head_dim")
-        n = self._bytes((heads, max_len), lambda: M.mosaic_kv_attention_workspace(self._ref, heads, max_len))
-        ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
-        M.mosaic_kv_attention(self._ref, q, max(q.stride(0), heads * d), heads, lens, max_len, first,
-                              d ** -0.5 if scale is None else scale, decay, o, max(o.stride(0), heads * d), ws)
+            _int32(first, "first", n, at)
+        o = torch.empty((n, heads, d), dtype=torch.float32, device=self.device) if out is None else out
+        need = self._bytes((heads, max_len), M.mosaic_kv_attention_workspace, heads, max_len)
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        M.mosaic_kv_attention(self._ref, q, ldq, heads, lens, max_len, first, d ** -0.5 if scale is None else scale,
+                              decay, o, _rows(o, "out", n, heads, d, at), ws)
         return o
 
     def evict(self, lens, max_len: int, keep: int, recent_from=None, new_lens=None):
         """Cuts every sequence to ``keep`` slots by least gathered weight (ties:
         the lower slot leaves), sparing positions >= recent_from[i]; returns
         the new lengths."""
-        _int32(lens, "lens", (self.seqs,), self.device)
+        _int32(lens, "lens", self.seqs, self._index)
         if recent_from is not None:
-            _int32(recent_from, "recent_from", (self.seqs,), self.device)
+            _int32(recent_from, "recent_from", self.seqs, self._index)
         new = torch.empty_like(lens) if new_lens is None else new_lens
-        _int32(new, "new_lens", (self.seqs,), self.device)
-        n = self._bytes(("evict", max_len, keep), lambda: M.mosaic_kv_evict_workspace(self._ref, max_len, keep))
-        ws = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+        _int32(new, "new_lens", self.seqs, self._index)
+        need = self._bytes(("evict", max_len, keep), M.mosaic_kv_evict_workspace, max_len, keep)
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
         M.mosaic_kv_evict(self._ref, lens, max_len, keep, recent_from, new, ws)
         return new
 
