@@ -204,6 +204,13 @@ mosaic_status check(const mosaic_kv_cache *c, int64_t heads, int64_t max_len) {
 int64_t rows_of(int64_t max_len) { return (max_len + 15) / 16 * 16; }
 
 }  // namespace
+
+// Reads and clears the timeout words of the attention kernels (after a stream sync).
+mosaic_status kv_status() {
+    const mosaic_status a = attend_status<float>(), b = attend_status<__nv_bfloat16>(), c = attend_status<__half>();
+    return a != MOSAIC_OK ? a : b != MOSAIC_OK ? b : c;
+}
+
 }  // namespace mosaic
 
 using namespace mosaic;
@@ -247,16 +254,11 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     }
     const int64_t jobs = cache->seqs * cache->kv_heads * a.hb;
     a.whole = cap == 0;
-    if (a.whole) a.blocks = (int)jobs;
-    else {
-        const int wave = by_type(cache->type, [&](auto t) { return attend_wave<decltype(t)>((int)D, a.group); });
-        if (wave <= 0) return MOSAIC_ERR_CUDA;
-        a.blocks = (int)(cap < wave ? cap : wave);
-    }
+    a.blocks = (int)(a.whole ? jobs : cap);
     const int64_t unit_bytes = 2 * s.unit * D * kv_element_bytes(cache->type);
     a.job_cost = (int)((kJobBytes + unit_bytes / 2) / unit_bytes);
     cudaStream_t st = as_stream(stream);
-    MOSAIC_TRY(by_type(cache->type, [&](auto t) { return attend_launch<decltype(t)>(*cache, a, st); }));
+    MOSAIC_TRY(by_type(cache->type, [&](auto t) { return attend_launch<decltype(t)>(*cache, a, a.blocks, st); }));
     if (!a.whole) {
         {
             KernelSpan span("attend_join", st);

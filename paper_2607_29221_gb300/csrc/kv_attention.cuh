@@ -44,6 +44,7 @@ struct AttendArgs {
     int whole;                  // a block a job, nothing is cut
     int blocks;
     int job_cost;
+    int token_major;            // of the tensor maps: heads lie closer than slots
     float scale2, decay;        // scale * log2(e): scores are kept in the base-2 domain
     float *out;
     int64_t ldo;
@@ -57,15 +58,17 @@ struct AttendArgs {
     int64_t score_rows;
 };
 
-// What the instance for a head_dim and a group has: query heads of a job,
-// padded head_dim (row length of part_o), slots of a unit; the blocks of one
-// wave on the current device (0: a CUDA error); and its launch.
+// What the instance for a head_dim and a group has (query heads of a job,
+// padded head_dim = row length of part_o, slots of a unit); its launch on
+// a.blocks blocks or one wave (`blocks`: how many); and whether a bounded wait
+// of it ran out since the last call (after a stream sync).
 struct AttendShape {
     int heads, dim, unit;
 };
 template <class T> AttendShape attend_shape(int head_dim, int group);
-template <class T> int attend_wave(int head_dim, int group);
-template <class T> mosaic_status attend_launch(const mosaic_kv_cache &c, const AttendArgs &a, cudaStream_t st);
+template <class T>
+mosaic_status attend_launch(const mosaic_kv_cache &c, const AttendArgs &a, int &blocks, cudaStream_t st);
+template <class T> mosaic_status attend_status();
 
 namespace {
 

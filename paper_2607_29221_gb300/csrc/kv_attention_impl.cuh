@@ -1,12 +1,15 @@
 // The split kernel of kv_attention.cuh for one element type.
 #pragma once
 
+#include "async_copy.cuh"
 #include "kv_attention.cuh"
 
 namespace mosaic {
 namespace {
 
-__device__ __forceinline__ uint32_t shared_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// Set when a bounded wait ran out (read by attend_status).
+__device__ unsigned int g_attend_error;
+
 // 16 bytes, or zeros where !ok (nothing is read then).
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool ok) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
@@ -34,37 +37,62 @@ __device__ __forceinline__ float lds(uint32_t a) {
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(a) : "memory");
     return x;
 }
-// d += a b, 16 x 8 x 16 (16-bit types) or 16 x 8 x 8 (tf32).
+// d += a b (mma0: d = a b), 16 x 8 x 16 (16-bit types) or 16 x 8 x 8 (tf32).
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma0(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma0(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float) {
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack(__nv_bfloat16 x, __nv_bfloat16 y) {
-    return __bfloat16_as_ushort(x) | (uint32_t)__bfloat16_as_ushort(y) << 16;
+__device__ __forceinline__ void mma0(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float) {
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3},{%4,%5,%6,%7},{%8,%9},{%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
-__device__ __forceinline__ uint32_t pack(__half x, __half y) {
-    return __half_as_ushort(x) | (uint32_t)__half_as_ushort(y) << 16;
+// x, y rounded to the type and packed (x lower); and back.
+__device__ __forceinline__ uint32_t pack2(float x, float y, __nv_bfloat16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&v);
 }
-
+__device__ __forceinline__ uint32_t pack2(float x, float y, __half) {
+    const __half2 v = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ float2 unpack2(uint32_t v, __nv_bfloat16) {
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+__device__ __forceinline__ float2 unpack2(uint32_t v, __half) {
+    return __half22float2(*reinterpret_cast<const __half2 *>(&v));
+}
 // x, y -> terms t[0] (the least) .. t[N-1] (the greatest), packed.
 template <class T, int N>
 __device__ __forceinline__ void split2(float x, float y, uint32_t (&t)[N]) {
 #pragma unroll
     for (int i = N - 1; i >= 0; --i) {
-        const T a = Elem<T>::from(x), b = Elem<T>::from(y);
-        t[i] = pack(a, b);
-        x -= Elem<T>::to(a), y -= Elem<T>::to(b);
+        t[i] = pack2(x, y, T());
+        if (i) {
+            const float2 v = unpack2(t[i], T());
+            x -= v.x, y -= v.y;
+        }
     }
 }
 // fp32 as two tf32 terms, the upper one rounded to nearest (the lower one then
@@ -81,6 +109,7 @@ template <> constexpr int kTerms<__half> = 2;
 template <class T> constexpr float kShift = 0.0f;
 template <> constexpr float kShift<__half> = 12.0f;
 
+constexpr int kTogether = 4;   // chains of products at a time
 constexpr int kGroup = 128;   // slots whose page ids a warp looks up together (8 tiles)
 
 // DP: head_dim padded to 64, 128 or 256.  NT: tiles of 8 query heads.
@@ -104,13 +133,20 @@ struct Shape {
     static constexpr int kRing = kWarps * kStages * kTile;
     static constexpr int kMerge = 4 * kSlots * kHeads * (kPitch + 2);
     static constexpr int kIds = 4 * kWarps * kGroup;
-    static constexpr int kBytes = kRing + kMerge + kIds + (kQReg ? 0 : 4 * kQWords);
-    static_assert(kBytes + 128 <= 227 * 1024, "shared memory");
+    static constexpr int kMisc = 8 * kWarps * kStages + 8 * (kWarps + 2) + 8;   // barriers, place, abort flag
+    static constexpr int kQAt = kRing + kMerge + kIds, kMiscAt = kQAt + (kQReg ? 0 : 4 * kQWords);
+    static constexpr int kBytes = kMiscAt + kMisc;
+    static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kBlocks = kFit < 3 ? kFit : 3;   // blocks an SM
+    static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
-// 16-byte chunk c of row r sits at chunk c ^ swizzle(r): 8 rows of a chunk are
-// conflict-free (ldmatrix), and so are 8 words of 4 rows r, r + 1, r + 2, r + 3.
-__device__ __forceinline__ int swizzle(int r) { return (r & 3) << 1 | (r >> 2 & 1); }
+// A tile: K, then V; each in blocks of 128 bytes of 16 rows, 16-byte chunk c of
+// row r at chunk c ^ (r % 8) of its block (the tensor copies' 128-byte
+// swizzle).  8 rows of a chunk are conflict-free (ldmatrix), and so are 8
+// words of rows r, r + 2, r + 4 and r + 6.
+__device__ __forceinline__ uint32_t chunk_at(int r, int c) {
+    return (uint32_t)((c >> 3) * 2048 + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+}
 
 template <class T, int DP, int NT>
 struct Warp {
@@ -206,36 +242,53 @@ struct Warp {
                                          int heads) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         float s[NT][4];
+        const uint32_t base = tile + chunk_at(lane & 15, lane >> 4);
+        // kTogether independent chains at a time (one alone waits out the latency
+        // of each of its products), each over two steps, the least terms first.
+        constexpr int KT = kTogether / NT, KB = 2 * KT < S::kSteps ? 2 * KT : S::kSteps;
+        static_assert(S::kSteps % KB == 0 && KB % KT == 0, "steps");
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int k0 = 0; k0 < S::kSteps; k0 += KB) {
+            uint32_t a[KB][4];
+            float c[KT][NT][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[n][j] = 0.0f;
-        const int row = lane & 15, sw = swizzle(row & 7);   // swizzle depends on the row modulo 8
-        const uint32_t base = tile + row * S::kRow;
+            for (int k = 0; k < KB; ++k) ldm4(a[k], (base ^ (2 * (k0 + k) % 8 << 4)) + (2 * (k0 + k) / 8) * 2048);
+            auto product = [&](bool first, int k, const uint32_t (&x)[4], int i) {
 #pragma unroll
-        for (int k = 0; k < S::kSteps; ++k) {
-            uint32_t a[4];
-            ldm4(a, base + (((2 * k + (lane >> 4)) ^ sw) << 4));
+                for (int n = 0; n < NT; ++n) {
+                    const uint32_t b0 = query(qs, k0 + k, n, i, 0), b1 = query(qs, k0 + k, n, i, 1);
+                    if (first) mma0(c[k % KT][n], x, b0, b1, T());
+                    else mma(c[k % KT][n], x, b0, b1, T());
+                }
+            };
+            if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if constexpr (sizeof(T) == 4) {
-                    uint32_t hi[4], lo[4];
+                for (int k = 0; k < KB; ++k) {
+                    uint32_t lo[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        hi[i] = tf32_high(__uint_as_float(a[i]));
-                        lo[i] = tf32_low(__uint_as_float(a[i]), hi[i]);
+                        const float v = __uint_as_float(a[k][i]);
+                        a[k][i] = tf32_high(v);
+                        lo[i] = tf32_low(v, a[k][i]);
                     }
-                    mma(c, lo, query(qs, k, n, 1, 0), query(qs, k, n, 1, 1), T());
-                    mma(c, hi, query(qs, k, n, 0, 0), query(qs, k, n, 0, 1), T());
-                    mma(c, hi, query(qs, k, n, 1, 0), query(qs, k, n, 1, 1), T());
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kTermsN; ++i) mma(c, a, query(qs, k, n, i, 0), query(qs, k, n, i, 1), T());
+                    product(k < KT, k, lo, 1);
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[n][j] += c[j];
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int k = 0; k < KB; ++k) product(false, k, a[k], i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kTermsN; ++i)
+#pragma unroll
+                    for (int k = 0; k < KB; ++k) product(i == 0 && k < KT, k, a[k], i);
             }
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[n][j] = k0 + k == 0 ? c[k][n][j] : s[n][j] + c[k][n][j];
         }
         const bool up = live >> g & 1, dn = live >> (g + 8) & 1;
         uint32_t p16[NT][kTermsN][2];   // 16-bit types: terms of P^T, as the product wants them
@@ -278,64 +331,91 @@ struct Warp {
         const uint32_t vbase = tile + 16 * S::kRow;
         if constexpr (sizeof(T) == 2) {
             // Slots (lane / 16) * 8 + lane % 8, channels 16 i + 8 (lane / 8 % 2).
-            const int vr = (lane >> 4) * 8 + (lane & 7), vsw = swizzle(vr & 7);
+            const uint32_t at = vbase + chunk_at((lane >> 4) * 8 + (lane & 7), lane >> 3 & 1);
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
-                uint32_t a[4];
-                ldm4t(a, vbase + vr * S::kRow + (((2 * i + (lane >> 3 & 1)) ^ vsw) << 4));
+            for (int i0 = 0; i0 < DP / 16; i0 += KT) {
+                uint32_t a[KT][4];
+                float c[KT][NT][4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int x = 0; x < kTermsN; ++x) mma(c, a, p16[n][x][0], p16[n][x][1], T());
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[n][i][j] = fmaf(o[n][i][j], alpha[n][j & 1], c[j]);
+                for (int i = 0; i < KT; ++i) {
+                    ldm4t(a[i], (at ^ (2 * (i0 + i) % 8 << 4)) + (2 * (i0 + i) / 8) * 2048);
                 }
+#pragma unroll
+                for (int x = 0; x < kTermsN; ++x)
+#pragma unroll
+                    for (int i = 0; i < KT; ++i)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            if (x == 0) mma0(c[i][n], a[i], p16[n][x][0], p16[n][x][1], T());
+                            else mma(c[i][n], a[i], p16[n][x][0], p16[n][x][1], T());
+                        }
+#pragma unroll
+                for (int i = 0; i < KT; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            o[n][i0 + i][j] = fmaf(o[n][i0 + i][j], alpha[n][j & 1], c[i][n][j]);
             }
         } else {
-            uint32_t ph[NT][2][2], pl[NT][2][2];   // by step of 8 slots
+            // By step of 8 slots; the step's row t is slot 2t, row t + 4 slot 2t + 1.
+            uint32_t ph[NT][2][2], pl[NT][2][2];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        const int from = (t + 4 * b) * 4 + (g >> 1);
+                        const int from = (2 * t + b) * 4 + (g >> 1);
                         const float x = __shfl_sync(0xffffffffu, s[n][2 * k], from);
                         const float y = __shfl_sync(0xffffffffu, s[n][2 * k + 1], from);
                         const float v = g & 1 ? y : x;
                         ph[n][k][b] = tf32_high(v);
                         pl[n][k][b] = tf32_low(v, ph[n][k][b]);
                     }
+            constexpr int IT = kTogether / NT / 2;   // two chains (steps) each
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
-                float c[NT][4];
+            for (int i0 = 0; i0 < DP / 16; i0 += IT) {
+                float c[IT][NT][2][4];
+                uint32_t hi[IT][2][4], lo[IT][2][4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int i = 0; i < IT; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) c[n][j] = 0.0f;
-                uint32_t hi[2][4], lo[2][4];
+                    for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                        for (int j = 0; j < 4; ++j) {
+                            const int r = 8 * k + 2 * t + (j >> 1), ch = 4 * (i0 + i) + (g >> 2) + 2 * (j & 1);
+                            hi[i][k][j] = __float_as_uint(lds(vbase + chunk_at(r, ch) + (g & 3) * 4));
+                        }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int r = 8 * k + t + 2 * (j & 2), d = 16 * i + g + 8 * (j & 1);
-                        const float v = lds(vbase + r * S::kRow + (((d >> 2) ^ swizzle(r & 7)) << 4) + (d & 3) * 4);
-                        hi[k][j] = tf32_high(v);
-                        lo[k][j] = tf32_low(v, hi[k][j]);
-                    }
+                for (int i = 0; i < IT; ++i)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
+                    for (int k = 0; k < 2; ++k)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        mma(c[n], lo[k], ph[n][k][0], ph[n][k][1], T());
-                        mma(c[n], hi[k], pl[n][k][0], pl[n][k][1], T());
-                    }
+                        for (int j = 0; j < 4; ++j) {
+                            const float v = __uint_as_float(hi[i][k][j]);
+                            hi[i][k][j] = tf32_high(v);
+                            lo[i][k][j] = tf32_low(v, hi[i][k][j]);
+                        }
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) mma(c[n], hi[k], ph[n][k][0], ph[n][k][1], T());
+                for (int x = 0; x < 3; ++x)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) o[n][i][j] = fmaf(o[n][i][j], alpha[n][j & 1], c[n][j]);
-                }
+                    for (int i = 0; i < IT; ++i)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                if (x == 0) mma0(c[i][n][k], lo[i][k], ph[n][k][0], ph[n][k][1], T());
+                                else if (x == 1) mma(c[i][n][k], hi[i][k], pl[n][k][0], pl[n][k][1], T());
+                                else mma(c[i][n][k], hi[i][k], ph[n][k][0], ph[n][k][1], T());
+                            }
+#pragma unroll
+                for (int i = 0; i < IT; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            o[n][i0 + i][j] = fmaf(o[n][i0 + i][j], alpha[n][j & 1], c[i][n][0][j] + c[i][n][1][j]);
             }
         }
     }
@@ -429,8 +509,10 @@ __device__ __forceinline__ void find_place(const KvView &kv, const AttendArgs &a
 
 // What a warp copies, tile by tile, through all jobs of the block.  Page ids
 // of 128 slots are looked up together, two groups (with a lower bound: and
-// the positions, one group) before their tiles are copied.
-template <class T, int DP, int NT>
+// the positions, one group) before their tiles are copied.  TMA: a tile lies in
+// one page (page_size is a multiple of 16) and comes by tensor copies, a few
+// instructions of one lane; else by 16-byte copies of every lane.
+template <class T, int DP, int NT, bool TMA>
 struct Feed {
     using S = Shape<T, DP, NT>;
     struct Group {
@@ -439,26 +521,34 @@ struct Feed {
     };
     const KvView &kv;
     const AttendArgs &a;
+    const CUtensorMap *mk, *mv;
     const int per_seq, w, lane;
-    uint32_t ring;
+    char *ring;
     int32_t *ids;       // shared: of the group being copied
+    uint64_t *full;     // shared: a barrier a stage
+    volatile int *aborted;
     Jobs jobs;
     int job_tiles, job_at;   // tiles of this warp in the newest group's job, and how many have a group
     Group now, mid, far;
     int id_mid[4], id_far[4], pos_mid[4];
     int at;             // tile of `now` that is copied next
     int stage;
+    uint32_t phase, flying;   // of the stages' barriers: parity, and whether a copy is under way
     bool over;          // no further group
     unsigned long long queue;   // live slots of the tiles in flight, 16 bits each, the oldest lowest
 
-    __device__ __forceinline__ Feed(const KvView &kv_, const AttendArgs &a_, int per_seq_, const Jobs &j, char *smem)
-        : kv(kv_), a(a_), per_seq(per_seq_), w(threadIdx.x >> 5), lane(threadIdx.x & 31), jobs(j) {
-        ring = shared_addr(smem) + w * S::kStages * S::kTile;
+    __device__ __forceinline__ Feed(const KvView &kv_, const AttendArgs &a_, const CUtensorMap *mk_,
+                                    const CUtensorMap *mv_, int per_seq_, const Jobs &j, char *smem, uint64_t *bars,
+                                    volatile int *aborted_)
+        : kv(kv_), a(a_), mk(mk_), mv(mv_), per_seq(per_seq_), w(threadIdx.x >> 5), lane(threadIdx.x & 31),
+          aborted(aborted_), jobs(j) {
+        ring = smem + w * S::kStages * S::kTile;
         ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge) + w * kGroup;
+        full = bars + w * S::kStages;
         job_tiles = job_at = at = stage = 0;
+        phase = flying = 0;
         over = false, queue = 0;
-        now.tiles = mid.tiles = far.tiles = 0;
-        step(), step(), step();
+        now.tiles = mid.tiles = far.tiles = 0;   // filled by the first steps
     }
     __device__ __forceinline__ int slot(const Group &g, int e) const {   // entry e of the group
         return g.s + (e >> 4) * S::kUnit + (e & 15);
@@ -511,46 +601,105 @@ struct Feed {
     }
     // Copies the next tile (an empty one at the end), `depth` tiles before its use.
     __device__ __forceinline__ void issue(int depth) {
-        // No group is empty but those behind the last one.
-        if (at >= now.tiles && mid.tiles > 0) step();
+        // Empty groups: before the first one and behind the last.
+        while (at >= now.tiles && (mid.tiles > 0 || far.tiles > 0 || !over)) step();
         if (at < now.tiles) {
             const int id = ids[16 * at + (lane & 15)], s = now.s + at * S::kUnit + (lane & 15);
             const uint32_t live = __ballot_sync(0xffffffffu, id >= 0) & 0xffffu;
             queue |= (unsigned long long)live << (16 * depth);
             if (live) {
-                const int64_t row = id < 0 ? -1 : kv.element(id, now.h, (uint32_t)s - kv.page.div(s) * kv.page.d) * S::kES;
-                const char *kp = static_cast<const char *>(kv.c.k), *vp = static_cast<const char *>(kv.c.v);
-                const int chunks = kv.c.head_dim * S::kES / 16;
-                const uint32_t to = ring + stage * S::kTile;
+                char *to = ring + stage * S::kTile;
+                const uint32_t off = (uint32_t)s - kv.page.div(s) * kv.page.d;
+                if constexpr (TMA) {
+                    const int any = __shfl_sync(0xffffffffu, id, __ffs(live) - 1);
+                    if (lane == 0) {
+                        uint64_t *bar = full + stage;
+                        mbar_expect_tx(bar, S::kTile);
+                        const int c1 = a.token_major ? now.h : (int)off, c2 = a.token_major ? (int)off : now.h;
 #pragma unroll
-                for (int x = 0; x < 16 * S::kChunks / 32; ++x) {
-                    const int at16 = x * 32 + lane, rr = at16 / S::kChunks, c = at16 % S::kChunks;
-                    const int64_t e = __shfl_sync(0xffffffffu, row, rr);
-                    const bool ok = e >= 0 && c < chunks;
-                    const uint32_t dst = to + rr * S::kRow + ((c ^ swizzle(rr & 7)) << 4);
-                    const int64_t src = ok ? e + c * 16 : 0;
-                    copy16(dst, kp + src, ok);
-                    copy16(dst + 16 * S::kRow, vp + src, ok);
+                        for (int b = 0; b < S::kRow / 128; ++b) {
+                            tma_load_4d(to + b * 2048, mk, bar, b * 128 / S::kES, c1, c2, any);
+                            tma_load_4d(to + 16 * S::kRow + b * 2048, mv, bar, b * 128 / S::kES, c1, c2, any);
+                        }
+                    }
+                    flying |= 1u << stage;
+                } else {
+                    const int64_t row = id < 0 ? -1 : kv.element(id, now.h, off) * S::kES;
+                    const char *kp = static_cast<const char *>(kv.c.k), *vp = static_cast<const char *>(kv.c.v);
+                    const int chunks = kv.c.head_dim * S::kES / 16;
+                    const uint32_t at0 = smem_u32(to);
+#pragma unroll
+                    for (int x = 0; x < 16 * S::kChunks / 32; ++x) {
+                        const int at16 = x * 32 + lane, rr = at16 / S::kChunks, c = at16 % S::kChunks;
+                        const int64_t e = __shfl_sync(0xffffffffu, row, rr);
+                        const bool ok = e >= 0 && c < chunks;
+                        const uint32_t dst = at0 + chunk_at(rr, c);
+                        const int64_t src = ok ? e + c * 16 : 0;
+                        copy16(dst, kp + src, ok);
+                        copy16(dst + 16 * S::kRow, vp + src, ok);
+                    }
                 }
             }
             ++at;
         }
-        copies_commit();
+        if constexpr (!TMA) copies_commit();
         stage = stage + 1 == S::kStages ? 0 : stage + 1;
+    }
+    // Waits for the tile in stage `use` (live != 0) and clears the values of
+    // slots that do not count: a weight of zero does not make up for a NaN.
+    __device__ __forceinline__ void ready(int use, uint32_t live) {
+        if constexpr (TMA) {
+            if (!mbar_wait(full + use, phase >> use & 1u, aborted)) {
+                *aborted = 1;   // results are void; the device status says so
+                if (lane == 0) atomicExch(&g_attend_error, 1u);
+            } else {
+                flying &= ~(1u << use);
+            }
+            phase ^= 1u << use;
+            if (live != 0xffffu) {
+                char *v = ring + use * S::kTile + 16 * S::kRow;
+                for (int x = lane; x < 16 * S::kChunks; x += 32)
+                    if (!(live >> (x / S::kChunks) & 1u))
+                        *reinterpret_cast<uint4 *>(v + chunk_at(x / S::kChunks, x % S::kChunks)) = make_uint4(0, 0, 0, 0);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // before the stage's next copy
+                __syncwarp();
+            }
+        }
+    }
+    // Nothing in flight may outlive the block.
+    __device__ __forceinline__ void finish() {
+        if constexpr (TMA) {
+            if (*aborted)
+                for (int s = 0; s < S::kStages; ++s)
+                    if (flying >> s & 1u) mbar_drain(full + s, phase >> s & 1u);
+        } else {
+            copies_wait<0>();
+        }
     }
 };
 
-template <class T, int DP, int NT>
-__global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps) attend_kernel(KvView kv, AttendArgs a) {
+template <class T, int DP, int NT, bool TMA>
+__global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps, Shape<T, DP, NT>::kBlocks)
+    attend_kernel(KvView kv, AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
     using S = Shape<T, DP, NT>;
     constexpr int W = S::kWarps, THREADS = 32 * W, NS = S::kStages, MS = S::kSlots;
-    extern __shared__ __align__(128) char smem[];
-    __shared__ long long place_sh[W + 2];
+    extern __shared__ __align__(1024) char smem[];
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + S::kMiscAt);
+    long long *place_sh = reinterpret_cast<long long *>(bars + W * NS);
+    volatile int *aborted = reinterpret_cast<volatile int *>(place_sh + W + 2);
     float *mo = reinterpret_cast<float *>(smem + S::kRing), *mm = mo + MS * S::kHeads * S::kPitch,
           *ml = mm + MS * S::kHeads;
-    uint32_t *qs = reinterpret_cast<uint32_t *>(smem + S::kRing + S::kMerge + S::kIds);
+    uint32_t *qs = reinterpret_cast<uint32_t *>(smem + S::kQAt);
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, g = lane >> 2, t = lane & 3;
     const int D = kv.c.head_dim, KV = kv.c.kv_heads, per_seq = KV * a.hb;
+    if (tid == 0) {
+        *aborted = 0;
+        if (TMA) {
+            for (int x = 0; x < W * NS; ++x) mbar_init(bars + x, 1);
+            mbar_init_fence();
+        }
+    }
+    __syncthreads();
     pdl_enter();
 
     Jobs jobs;
@@ -565,8 +714,8 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps) attend_kernel(K
                 for (int x = tid; x < a.heads * D; x += THREADS) a.out[i * a.ldo + x] = 0.0f;
         if (tid == 0) a.split[3 * blockIdx.x] = -1;
     }
-    Feed<T, DP, NT> feed(kv, a, per_seq, jobs, smem);
-#pragma unroll
+    Feed<T, DP, NT, TMA> feed(kv, a, &mk, &mv, per_seq, jobs, smem, bars, aborted);
+#pragma unroll 1
     for (int n = 0; n < NS - 1; ++n) feed.issue(n);
 
     Warp<T, DP, NT> wp;
@@ -582,14 +731,16 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps) attend_kernel(K
         wp.queries(a.q + i * a.ldq + qh * D, D, rows, a.scale2, qs);
         if constexpr (!S::kQReg) __syncthreads();
         for (int n = 0; n < mine; ++n) {
-            copies_wait<NS - 2>();
+            if constexpr (!TMA) copies_wait<NS - 2>();
             __syncwarp();
             const uint32_t live = (uint32_t)feed.queue & 0xffffu;
             feed.queue >>= 16;
             feed.issue(NS - 2);
             float *sc = scores ? scores + 16 * (w + n * W) : nullptr;   // rows of 16 slots exist in whole
-            if (live) wp.tile(feed.ring + use * S::kTile, live, qs, sc, a.score_rows, rows);
-            else if (sc) {   // no slot counts: the weights read that
+            if (live) {
+                feed.ready(use, live);
+                wp.tile(smem_u32(feed.ring + use * S::kTile), live, qs, sc, a.score_rows, rows);
+            } else if (sc) {   // no slot counts: the weights read that
                 for (int x = lane; x < 16 * rows; x += 32) sc[(x >> 4) * a.score_rows + (x & 15)] = minus_inf();
             }
             use = use + 1 == NS ? 0 : use + 1;
@@ -681,19 +832,19 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps) attend_kernel(K
         }
         __syncthreads();
     }
-    copies_wait<0>();
+    feed.finish();
 }
 
-template <class T, int DP, int NT>
+template <class T, int DP, int NT, bool TMA>
 int resident() {
     static std::atomic<int> known[64];
     int dev = 0, n = 0;
     static std::atomic<unsigned long long> done{0};
     using S = Shape<T, DP, NT>;
-    if (!ensure_smem_limit(done, attend_kernel<T, DP, NT>, S::kBytes, &dev)) return 0;
+    if (!ensure_smem_limit(done, attend_kernel<T, DP, NT, TMA>, S::kBytes, &dev)) return 0;
     std::atomic<int> &at = known[dev & 63];
     if ((n = at.load(std::memory_order_relaxed)) > 0) return n;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<T, DP, NT>, 32 * S::kWarps, S::kBytes) !=
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<T, DP, NT, TMA>, 32 * S::kWarps, S::kBytes) !=
         cudaSuccess)
         return 0;
     n *= sm_count(dev);
@@ -701,23 +852,60 @@ int resident() {
     return n;
 }
 
+// A pool as a tensor of (channel, slot, head, page), or (channel, head, slot,
+// page) where heads are the closer ones; box: 128 bytes of 16 slots.  False
+// where the strides do not nest (or no tile lies in one page): the lanes copy.
+template <class T>
+bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int *token_major) {
+    if (c.page_size % 16) return false;
+    constexpr int kES = sizeof(T);
+    const cuuint64_t D = (cuuint64_t)c.head_dim * kES, slots = (cuuint64_t)c.page_size, heads = (cuuint64_t)c.kv_heads;
+    cuuint64_t slot = (cuuint64_t)c.slot_stride * kES, head = (cuuint64_t)c.head_stride * kES;
+    cuuint64_t page = (cuuint64_t)c.page_stride * kES;
+    if (heads == 1) head = slot * slots;
+    const bool tm = head < slot;
+    const cuuint64_t inner = tm ? head : slot, outer = tm ? slot : head;
+    if (c.pages == 1) page = outer * (tm ? slots : heads);
+    const cuuint64_t most = (cuuint64_t)1 << 40;
+    if (inner < D || outer < inner || page < outer || outer % inner || page % outer || page >= most) return false;
+    auto fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, tm ? heads : slots, tm ? slots : heads, (cuuint64_t)c.pages};
+    const cuuint64_t strides[3] = {inner, outer, page};
+    const cuuint32_t box[4] = {128 / kES, tm ? 1u : 16u, tm ? 16u : 1u, 1}, each[4] = {1, 1, 1, 1};
+    const CUtensorMapDataType type = kES == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                     : kTerms<T> == 3 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    *token_major = tm;
+    return fn(map, type, 4, pool, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <class T, int DP, int NT>
 struct Instance {
     using S = Shape<T, DP, NT>;
     static AttendShape shape() { return {S::kHeads, DP, S::kUnit}; }
-    static int wave() { return resident<T, DP, NT>(); }
-    static mosaic_status launch(const mosaic_kv_cache &c, const AttendArgs &a, cudaStream_t st) {
-        if (resident<T, DP, NT>() == 0) return MOSAIC_ERR_CUDA;   // sets the shared-memory limit
-        const KvView kv(c);
+    template <bool TMA>
+    static mosaic_status go(const KvView &kv, AttendArgs a, const CUtensorMap &mk, const CUtensorMap &mv,
+                            int &blocks, cudaStream_t st) {
+        const int wave = resident<T, DP, NT, TMA>();
+        if (wave <= 0) return MOSAIC_ERR_CUDA;
+        if (!a.whole && a.blocks > wave) a.blocks = wave;
+        blocks = a.blocks;
         {
             KernelSpan span("attend", st);
             const dim3 grid((unsigned)a.blocks), block(32 * S::kWarps);
             // More than one wave (whole jobs) must not stack up early.
-            if (a.blocks <= resident<T, DP, NT>())
-                pdl_launch(attend_kernel<T, DP, NT>, grid, block, S::kBytes, st, kv, a);
-            else attend_kernel<T, DP, NT><<<grid, block, S::kBytes, st>>>(kv, a);
+            if (a.blocks <= wave) pdl_launch(attend_kernel<T, DP, NT, TMA>, grid, block, S::kBytes, st, kv, a, mk, mv);
+            else attend_kernel<T, DP, NT, TMA><<<grid, block, S::kBytes, st>>>(kv, a, mk, mv);
         }
         return launch_status();
+    }
+    static mosaic_status launch(const mosaic_kv_cache &c, AttendArgs a, int &blocks, cudaStream_t st) {
+        const KvView kv(c);
+        alignas(64) CUtensorMap mk = {}, mv = {};
+        if (pool_map<T>(&mk, c, c.k, &a.token_major) && pool_map<T>(&mv, c, c.v, &a.token_major))
+            return go<true>(kv, a, mk, mv, blocks, st);
+        return go<false>(kv, a, mk, mv, blocks, st);
     }
 };
 
@@ -736,16 +924,22 @@ auto with_instance(int head_dim, int group, F f) {
 
 }  // namespace
 
-#define MOSAIC_ATTEND_TYPE(T)                                                                         \
-    template <> AttendShape attend_shape<T>(int head_dim, int group) {                                \
-        return with_instance<T>(head_dim, group, [&](auto i) { return decltype(i)::shape(); });       \
-    }                                                                                                 \
-    template <> int attend_wave<T>(int head_dim, int group) {                                         \
-        return with_instance<T>(head_dim, group, [&](auto i) { return decltype(i)::wave(); });        \
-    }                                                                                                 \
-    template <>                                                                                       \
-    mosaic_status attend_launch<T>(const mosaic_kv_cache &c, const AttendArgs &a, cudaStream_t st) {  \
-        return with_instance<T>(c.head_dim, a.group, [&](auto i) { return decltype(i)::launch(c, a, st); }); \
+#define MOSAIC_ATTEND_TYPE(T)                                                                             \
+    template <> AttendShape attend_shape<T>(int head_dim, int group) {                                    \
+        return with_instance<T>(head_dim, group, [&](auto i) { return decltype(i)::shape(); });           \
+    }                                                                                                     \
+    template <>                                                                                           \
+    mosaic_status attend_launch<T>(const mosaic_kv_cache &c, const AttendArgs &a, int &blocks,            \
+                                   cudaStream_t st) {                                                     \
+        return with_instance<T>(c.head_dim, a.group,                                                      \
+                                [&](auto i) { return decltype(i)::launch(c, a, blocks, st); });           \
+    }                                                                                                     \
+    template <> mosaic_status attend_status<T>() {                                                        \
+        unsigned int e = 0, zero = 0;                                                                     \
+        if (cudaMemcpyFromSymbol(&e, g_attend_error, sizeof(e)) != cudaSuccess) return MOSAIC_ERR_CUDA;   \
+        if (!e) return MOSAIC_OK;                                                                         \
+        if (cudaMemcpyToSymbol(g_attend_error, &zero, sizeof(zero)) != cudaSuccess) return MOSAIC_ERR_CUDA; \
+        return MOSAIC_ERR_TIMEOUT;                                                                        \
     }
 
 }  // namespace mosaic

@@ -386,6 +386,9 @@ mosaic_status unmask_few(int64_t l, int64_t m, const uint32_t *Z, int64_t ldz, i
 mosaic_status sparse_rowgather(const uint32_t *P, int64_t ldp, const SparseLevel *lev, int nlev,
                                int64_t m, int64_t ncols, const uint32_t *a, int64_t lda,
                                uint32_t *out, int64_t ldo, cudaStream_t st);
+// Reads and clears the timeout words of the cache's attention (after a stream sync).
+mosaic_status kv_status();
+
 // Layout helper.
 mosaic_status transpose_u32(const uint32_t *a, int64_t lda, int64_t rows, int64_t cols, uint32_t *out,
                             int64_t ldo, cudaStream_t st);
