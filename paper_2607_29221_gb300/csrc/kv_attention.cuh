@@ -44,7 +44,7 @@ struct AttendArgs {
     int whole;                  // a block a job, nothing is cut
     int blocks;
     int job_cost;
-    int token_major;            // of the tensor maps: heads lie closer than slots
+    int token_major, box;       // of the tensor maps: heads lie closer than slots; slots of a box
     float scale2, decay;        // scale * log2(e): scores are kept in the base-2 domain
     float *out;
     int64_t ldo;

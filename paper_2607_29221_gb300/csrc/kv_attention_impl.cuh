@@ -14,10 +14,10 @@ __device__ unsigned int g_attend_error;
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool ok) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+__device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// Arrives (for this lane, one of the barrier's count) when the lane's copies so far have landed.
+__device__ __forceinline__ void copies_arrive(uint64_t *bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t a) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -110,48 +110,49 @@ template <class T> constexpr float kShift = 0.0f;
 template <> constexpr float kShift<__half> = 12.0f;
 
 constexpr int kTogether = 4;   // chains of products at a time
-constexpr int kGroup = 128;   // slots whose page ids a warp looks up together (8 tiles)
+constexpr int kLookup = 4 * 128 + 32;   // bytes of a producer's page ids and live slots
 
 // DP: head_dim padded to 64, 128 or 256.  NT: tiles of 8 query heads.
 template <class T, int DP, int NT>
 struct Shape {
     static constexpr int kES = sizeof(T), kRow = DP * kES, kChunks = kRow / 16;
-    static constexpr int kTile = 2 * 16 * kRow;                   // K and V of 16 slots
-    // 8 warps an SM, as two blocks or (with twice the outputs and queries) one;
-    // fewer where tiles are large.
-    static constexpr bool kSix = kES == 4 && DP == 128 && NT == 1;
-    static constexpr int kWarps = kTile >= 32768 ? 2 : NT == 2 && kTile <= 8192 ? 8 : kSix ? 6 : 4, kUnit = 16 * kWarps;
-    static constexpr int kStages = kTile <= 4096 ? 4 : (NT == 2 && DP == 256) || kSix ? 2 : 3;
-    static constexpr int kSlots = kWarps == 2 || (NT == 2 && kTile >= 16384) ? 1 : 2;   // warps' results at a time
+    // A stage holds a unit: K and V of 16 slots a consumer warp.  8 consumer
+    // warps an SM, as two blocks or (with twice the outputs and queries) one;
+    // fewer where rows are long.
+    static constexpr int kWarps = kRow == 1024 ? 2 : NT == 2 && kRow <= 256 ? 8 : kRow == 512 && kES == 4 && NT == 1 ? 6 : 4;
+    static constexpr int kUnit = 16 * kWarps, kStage = 2 * kUnit * kRow;
+    static constexpr int kStages = kRow == 128 ? 4 : (NT == 2 && DP == 256) || kWarps == 6 ? 2 : 3;
+    static constexpr int kSlots = kWarps == 2 || (NT == 2 && kRow >= 512) ? 1 : 2;   // warps' results at a time
     static constexpr int kK = kES == 4 ? 8 : 16, kSteps = DP / kK;    // channels of a product step
     static constexpr int kHeads = 8 * NT, kPitch = DP + 4;
     static constexpr int kQWords = kSteps * NT * kTerms<T> * 2 * 32;  // query fragments
     // Queries stay in registers where they fit beside the outputs.
     static constexpr bool kQReg = kSteps * NT * kTerms<T> * 2 <= 48;
-    // Shared memory: the rings, the results of some warps, the warps'
-    // page ids, the queries' fragments.
-    static constexpr int kRing = kWarps * kStages * kTile;
+    // Shared memory: the ring, the results of some warps, page ids and live
+    // slots of the producers' groups, the queries' fragments, barriers and so on.
+    static constexpr int kRing = kStages * kStage;
     static constexpr int kMerge = 4 * kSlots * kHeads * (kPitch + 2);
-    static constexpr int kIds = 4 * kWarps * kGroup;
-    static constexpr int kMisc = 8 * kWarps * kStages + 8 * (kWarps + 2) + 8;   // barriers, place, abort flag
+    static constexpr int kIds = 2 * kLookup;
     static constexpr int kQAt = kRing + kMerge + kIds, kMiscAt = kQAt + (kQReg ? 0 : 4 * kQWords);
-    static constexpr int kBytes = kMiscAt + kMisc;
+    static constexpr int kBytes = kMiscAt + 512;
     static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kBlocks = kFit < 3 ? kFit : 3;   // blocks an SM
     static_assert(kBytes <= 227 * 1024, "shared memory");
 };
+constexpr int kProducers = 2;   // warps that copy
 
-// A tile: K, then V; each in blocks of 128 bytes of 16 rows, 16-byte chunk c of
-// row r at chunk c ^ (r % 8) of its block (the tensor copies' 128-byte
-// swizzle).  8 rows of a chunk are conflict-free (ldmatrix), and so are 8
-// words of rows r, r + 2, r + 4 and r + 6.
+// A stage: K, then V of a unit; each in blocks of 128 bytes of all its rows,
+// 16-byte chunk c of row r at chunk c ^ (r % 8) of its block (the tensor copies'
+// 128-byte swizzle).  8 rows of a chunk are conflict-free (ldmatrix), and so are
+// 8 words of rows r, r + 2, r + 4 and r + 6.
+template <int BLOCK>   // bytes of a block of all rows
 __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
-    return (uint32_t)((c >> 3) * 2048 + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+    return (uint32_t)((c >> 3) * BLOCK + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 
 template <class T, int DP, int NT>
 struct Warp {
     using S = Shape<T, DP, NT>;
-    static constexpr int kTermsN = kTerms<T>;
+    static constexpr int kTermsN = kTerms<T>, kBlock = 128 * S::kUnit;
     float m[NT][2], l[NT][2], o[NT][DP / 16][4];   // of heads 2t, 2t + 1 of each tile
     uint32_t qr[S::kQReg ? S::kSteps * NT * kTermsN * 2 : 1];
     float unscale[NT][2];                          // fp16: what undoes the queries' scaling
@@ -235,14 +236,14 @@ struct Warp {
         else return qs[at * 32 + (threadIdx.x & 31)];
     }
 
-    // One tile of 16 slots, K rows at `tile` and V rows behind them; bit r of
+    // One tile of 16 slots, K rows at `tile` and V rows at `vbase`; bit r of
     // `live`: slot r counts.  `sc`: where the scores of slot 0 and the job's
     // first head go (a row of `pitch` words a head, `heads` of them), or null.
-    __device__ __forceinline__ void tile(uint32_t tile, uint32_t live, const uint32_t *qs, float *sc, int64_t pitch,
+    __device__ __forceinline__ void tile(uint32_t tile, uint32_t vbase, uint32_t live, const uint32_t *qs, float *sc, int64_t pitch,
                                          int heads) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         float s[NT][4];
-        const uint32_t base = tile + chunk_at(lane & 15, lane >> 4);
+        const uint32_t base = tile + chunk_at<kBlock>(lane & 15, lane >> 4);
         // kTogether independent chains at a time (one alone waits out the latency
         // of each of its products), each over two steps, the least terms first.
         constexpr int KT = kTogether / NT, KB = 2 * KT < S::kSteps ? 2 * KT : S::kSteps;
@@ -252,7 +253,7 @@ struct Warp {
             uint32_t a[KB][4];
             float c[KT][NT][4];
 #pragma unroll
-            for (int k = 0; k < KB; ++k) ldm4(a[k], (base ^ (2 * (k0 + k) % 8 << 4)) + (2 * (k0 + k) / 8) * 2048);
+            for (int k = 0; k < KB; ++k) ldm4(a[k], (base ^ (2 * (k0 + k) % 8 << 4)) + (2 * (k0 + k) / 8) * kBlock);
             auto product = [&](bool first, int k, const uint32_t (&x)[4], int i) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
@@ -328,17 +329,16 @@ struct Warp {
                 for (int i = 0; i < kTermsN; ++i) p16[n][i][0] = transpose8(x[i]), p16[n][i][1] = transpose8(y[i]);
             }
         }
-        const uint32_t vbase = tile + 16 * S::kRow;
         if constexpr (sizeof(T) == 2) {
             // Slots (lane / 16) * 8 + lane % 8, channels 16 i + 8 (lane / 8 % 2).
-            const uint32_t at = vbase + chunk_at((lane >> 4) * 8 + (lane & 7), lane >> 3 & 1);
+            const uint32_t at = vbase + chunk_at<kBlock>((lane >> 4) * 8 + (lane & 7), lane >> 3 & 1);
 #pragma unroll
             for (int i0 = 0; i0 < DP / 16; i0 += KT) {
                 uint32_t a[KT][4];
                 float c[KT][NT][4];
 #pragma unroll
                 for (int i = 0; i < KT; ++i) {
-                    ldm4t(a[i], (at ^ (2 * (i0 + i) % 8 << 4)) + (2 * (i0 + i) / 8) * 2048);
+                    ldm4t(a[i], (at ^ (2 * (i0 + i) % 8 << 4)) + (2 * (i0 + i) / 8) * kBlock);
                 }
 #pragma unroll
                 for (int x = 0; x < kTermsN; ++x)
@@ -385,7 +385,7 @@ struct Warp {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const int r = 8 * k + 2 * t + (j >> 1), ch = 4 * (i0 + i) + (g >> 2) + 2 * (j & 1);
-                            hi[i][k][j] = __float_as_uint(lds(vbase + chunk_at(r, ch) + (g & 3) * 4));
+                            hi[i][k][j] = __float_as_uint(lds(vbase + chunk_at<kBlock>(r, ch) + (g & 3) * 4));
                         }
 #pragma unroll
                 for (int i = 0; i < IT; ++i)
@@ -507,197 +507,280 @@ __device__ __forceinline__ void find_place(const KvView &kv, const AttendArgs &a
     __syncthreads();
 }
 
-// What a warp copies, tile by tile, through all jobs of the block.  Page ids
-// of 128 slots are looked up together, two groups (with a lower bound: and
-// the positions, one group) before their tiles are copied.  TMA: a tile lies in
-// one page (page_size is a multiple of 16) and comes by tensor copies, a few
-// instructions of one lane; else by 16-byte copies of every lane.
-template <class T, int DP, int NT, bool TMA>
-struct Feed {
+// What producers and consumers share beside the ring.
+template <class T, int DP, int NT>
+struct Pipe {
     using S = Shape<T, DP, NT>;
+    uint64_t full[S::kStages], empty[S::kStages];
+    uint16_t live[S::kStages][8];   // slots of the stage's tiles that count
+    int unit[S::kStages];           // the stage's unit in its job; + kLastUnit: the job's last one here
+    long long place[12];
+    int aborted;
+};
+constexpr int kLastUnit = 1 << 30;
+
+// A producer warp: copies unit by unit, through all jobs of the block.  Pages
+// are looked up a group of slots at a time, two groups (with a lower bound: and
+// the positions, one group) before their units are copied; units without a
+// live slot are left out (but for a job's last, which ends it).
+// TMA: tensor copies of a.box slots that share a page, a lane's to issue, the
+// first warp K and the second V; a lane looks up 8 slots.  Else every lane
+// copies 16 bytes at a time, each warp half of a unit's rows, and looks up
+// four single slots.
+template <class T, int DP, int NT, bool TMA>
+struct Producer {
+    using S = Shape<T, DP, NT>;
+    static constexpr int kEach = TMA ? 1 : 4;                  // look-ups of a lane
+    static constexpr int kSpan = TMA ? 256 : 128;              // slots of a group
+    static constexpr int kUnits = kSpan / S::kUnit, kHalves = S::kUnit / 16;
     struct Group {
-        int h, s, end, tiles, low;   // head, first slot, end of the job's slots, tiles of this warp, position bound
+        int h, hb, s, end, units, low;   // head, first slot, end of the job's slots, units, position bound
+        int unit;                        // number of its first unit in the job
+        bool last;                       // the job's last group
         int64_t i;
     };
     const KvView &kv;
     const AttendArgs &a;
-    const CUtensorMap *mk, *mv;
-    const int per_seq, w, lane;
-    char *ring;
-    int32_t *ids;       // shared: of the group being copied
-    uint64_t *full;     // shared: a barrier a stage
-    volatile int *aborted;
+    const CUtensorMap *map;
+    Pipe<T, DP, NT> &pipe;
+    char *smem;
+    const int per_seq, pw, lane;
+    int32_t *ids;       // shared, this warp's: pages of the group being copied
+    uint8_t *live;      // and its live slots, a bit each
     Jobs jobs;
-    int job_tiles, job_at;   // tiles of this warp in the newest group's job, and how many have a group
+    int job_units, job_at;   // units of the newest group's job, and how many have a group
     Group now, mid, far;
-    int id_mid[4], id_far[4], pos_mid[4];
-    int at;             // tile of `now` that is copied next
-    int stage;
-    uint32_t phase, flying;   // of the stages' barriers: parity, and whether a copy is under way
-    bool over;          // no further group
-    unsigned long long queue;   // live slots of the tiles in flight, 16 bits each, the oldest lowest
+    int id_mid[kEach], id_far[kEach];
+    int4 pos_mid[TMA ? 2 : 1];
+    int count;          // units copied
+    bool over;          // no further job
 
-    __device__ __forceinline__ Feed(const KvView &kv_, const AttendArgs &a_, const CUtensorMap *mk_,
-                                    const CUtensorMap *mv_, int per_seq_, const Jobs &j, char *smem, uint64_t *bars,
-                                    volatile int *aborted_)
-        : kv(kv_), a(a_), mk(mk_), mv(mv_), per_seq(per_seq_), w(threadIdx.x >> 5), lane(threadIdx.x & 31),
-          aborted(aborted_), jobs(j) {
-        ring = smem + w * S::kStages * S::kTile;
-        ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge) + w * kGroup;
-        full = bars + w * S::kStages;
-        job_tiles = job_at = at = stage = 0;
-        phase = flying = 0;
-        over = false, queue = 0;
-        now.tiles = mid.tiles = far.tiles = 0;   // filled by the first steps
+    __device__ __forceinline__ Producer(const KvView &kv_, const AttendArgs &a_, const CUtensorMap *mk,
+                                        const CUtensorMap *mv, Pipe<T, DP, NT> &pipe_, int per_seq_, const Jobs &j,
+                                        char *smem_, int pw_)
+        : kv(kv_), a(a_), map(pw_ ? mv : mk), pipe(pipe_), smem(smem_), per_seq(per_seq_), pw(pw_),
+          lane(threadIdx.x & 31), jobs(j) {
+        ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge + pw * kLookup);
+        live = reinterpret_cast<uint8_t *>(ids + 128);
+        job_units = job_at = count = 0;
+        over = false;
+        now.units = mid.units = far.units = 0;
     }
-    __device__ __forceinline__ int slot(const Group &g, int e) const {   // entry e of the group
-        return g.s + (e >> 4) * S::kUnit + (e & 15);
+    __device__ __forceinline__ uint32_t offset(int s) const { return (uint32_t)s - kv.page.div(s) * kv.page.d; }
+    __device__ __forceinline__ int first_slot(const Group &g, int e) const {   // of the lane's look-up e
+        return g.s + (TMA ? 8 * lane : 32 * e + lane);
     }
-    // The next group becomes `now`, its ids in shared memory.
+    // The next group becomes `now`, its pages and live slots in shared memory.
     __device__ __forceinline__ void step() {
         __syncwarp();
+        if (mid.units > 0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (mid.tiles > 0) ids[32 * e + lane] = a.first && pos_mid[e] < mid.low ? -1 : id_mid[e];
-        now = mid, mid = far, at = 0;
-        __syncwarp();
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            id_mid[e] = id_far[e];
-            if (a.first && mid.tiles > 0 && id_mid[e] >= 0) {
-                const int s = slot(mid, 32 * e + lane);
-                pos_mid[e] = kv.c.position[kv.mark(id_mid[e], mid.h, (uint32_t)s - kv.page.div(s) * kv.page.d)];
-            }
-        }
-        // Jobs that leave this warp without a tile have no group.
-        far.tiles = 0;
-        while (!over && job_at >= job_tiles) {
-            if (!jobs.next(kv, a, S::kUnit, per_seq)) {
-                over = true;
-                break;
-            }
-            const int tiles = (jobs.last(S::kUnit) - jobs.first(S::kUnit) + 15) / 16;
-            job_tiles = tiles > w ? (tiles - w + S::kWarps - 1) / S::kWarps : 0;
-            job_at = 0;
-        }
-        if (job_at < job_tiles) {
-            far.i = jobs.i, far.h = jobs.r / a.hb, far.end = jobs.last(S::kUnit);
-            far.s = jobs.first(S::kUnit) + 16 * w + job_at * S::kUnit;
-            far.tiles = min(kGroup / 16, job_tiles - job_at);
-            far.low = a.first ? a.first[jobs.i] : 0;
-            if (job_at == 0 && w == 0) {   // the queries come from memory by the time the job begins
-                const float *q = a.q + jobs.i * a.ldq + (int64_t)(far.h * a.group + jobs.r % a.hb * S::kHeads) * kv.c.head_dim;
-                const int words = min(S::kHeads, a.group - jobs.r % a.hb * S::kHeads) * kv.c.head_dim;
-                for (int x = 32 * lane; x < words; x += 1024) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + x));
-            }
-            job_at += far.tiles;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int x = 32 * e + lane, s = slot(far, x);
-                uint32_t off;
-                id_far[e] = (x >> 4) < far.tiles && s < far.end ? kv.page_of(far.i, (uint32_t)s, off) : -1;
-            }
-        }
-    }
-    // Copies the next tile (an empty one at the end), `depth` tiles before its use.
-    __device__ __forceinline__ void issue(int depth) {
-        // Empty groups: before the first one and behind the last.
-        while (at >= now.tiles && (mid.tiles > 0 || far.tiles > 0 || !over)) step();
-        if (at < now.tiles) {
-            const int id = ids[16 * at + (lane & 15)], s = now.s + at * S::kUnit + (lane & 15);
-            const uint32_t live = __ballot_sync(0xffffffffu, id >= 0) & 0xffffu;
-            queue |= (unsigned long long)live << (16 * depth);
-            if (live) {
-                char *to = ring + stage * S::kTile;
-                const uint32_t off = (uint32_t)s - kv.page.div(s) * kv.page.d;
+            for (int e = 0; e < kEach; ++e) {
                 if constexpr (TMA) {
-                    const int any = __shfl_sync(0xffffffffu, id, __ffs(live) - 1);
-                    if (lane == 0) {
-                        uint64_t *bar = full + stage;
-                        mbar_expect_tx(bar, S::kTile);
-                        const int c1 = a.token_major ? now.h : (int)off, c2 = a.token_major ? (int)off : now.h;
-#pragma unroll
-                        for (int b = 0; b < S::kRow / 128; ++b) {
-                            tma_load_4d(to + b * 2048, mk, bar, b * 128 / S::kES, c1, c2, any);
-                            tma_load_4d(to + 16 * S::kRow + b * 2048, mv, bar, b * 128 / S::kES, c1, c2, any);
+                    uint32_t on = 0;
+                    if (id_mid[0] >= 0) {
+                        on = 0xffu >> max(0, 8 - (mid.end - first_slot(mid, 0)));
+                        if (a.first) {
+                            const int4 x = pos_mid[0], y = pos_mid[1];
+                            const int low = mid.low;
+                            on &= (x.x >= low) | (x.y >= low) << 1 | (x.z >= low) << 2 | (x.w >= low) << 3 |
+                                  (y.x >= low) << 4 | (y.y >= low) << 5 | (y.z >= low) << 6 | (y.w >= low) << 7;
                         }
                     }
-                    flying |= 1u << stage;
+                    ids[lane] = id_mid[0];
+                    live[lane] = (uint8_t)on;
                 } else {
-                    const int64_t row = id < 0 ? -1 : kv.element(id, now.h, off) * S::kES;
-                    const char *kp = static_cast<const char *>(kv.c.k), *vp = static_cast<const char *>(kv.c.v);
-                    const int chunks = kv.c.head_dim * S::kES / 16;
-                    const uint32_t at0 = smem_u32(to);
-#pragma unroll
-                    for (int x = 0; x < 16 * S::kChunks / 32; ++x) {
-                        const int at16 = x * 32 + lane, rr = at16 / S::kChunks, c = at16 % S::kChunks;
-                        const int64_t e = __shfl_sync(0xffffffffu, row, rr);
-                        const bool ok = e >= 0 && c < chunks;
-                        const uint32_t dst = at0 + chunk_at(rr, c);
-                        const int64_t src = ok ? e + c * 16 : 0;
-                        copy16(dst, kp + src, ok);
-                        copy16(dst + 16 * S::kRow, vp + src, ok);
-                    }
+                    const int p = e == 0 ? pos_mid[0].x : e == 1 ? pos_mid[0].y : e == 2 ? pos_mid[0].z : pos_mid[0].w;
+                    const uint32_t on = __ballot_sync(0xffffffffu, id_mid[e] >= 0 && !(a.first && p < mid.low));
+                    ids[32 * e + lane] = id_mid[e];
+                    if (lane == 0) reinterpret_cast<uint32_t *>(live)[e] = on;
                 }
             }
-            ++at;
         }
-        if constexpr (!TMA) copies_commit();
-        stage = stage + 1 == S::kStages ? 0 : stage + 1;
-    }
-    // Waits for the tile in stage `use` (live != 0) and clears the values of
-    // slots that do not count: a weight of zero does not make up for a NaN.
-    __device__ __forceinline__ void ready(int use, uint32_t live) {
-        if constexpr (TMA) {
-            if (!mbar_wait(full + use, phase >> use & 1u, aborted)) {
-                *aborted = 1;   // results are void; the device status says so
-                if (lane == 0) atomicExch(&g_attend_error, 1u);
+        now = mid, mid = far;
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            id_mid[e] = id_far[e];
+            if (!a.first || mid.units == 0 || id_mid[e] < 0) continue;
+            const int32_t *p = kv.c.position + kv.mark(id_mid[e], mid.h, offset(first_slot(mid, e)));
+            if constexpr (TMA) {   // 8 slots of a page whose size is a multiple of 8
+                pos_mid[0] = reinterpret_cast<const int4 *>(p)[0], pos_mid[1] = reinterpret_cast<const int4 *>(p)[1];
             } else {
-                flying &= ~(1u << use);
+                (e == 0 ? pos_mid[0].x : e == 1 ? pos_mid[0].y : e == 2 ? pos_mid[0].z : pos_mid[0].w) = *p;
             }
-            phase ^= 1u << use;
-            if (live != 0xffffu) {
-                char *v = ring + use * S::kTile + 16 * S::kRow;
-                for (int x = lane; x < 16 * S::kChunks; x += 32)
-                    if (!(live >> (x / S::kChunks) & 1u))
-                        *reinterpret_cast<uint4 *>(v + chunk_at(x / S::kChunks, x % S::kChunks)) = make_uint4(0, 0, 0, 0);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // before the stage's next copy
-                __syncwarp();
+        }
+        far.units = 0;
+        if (job_at >= job_units && !over) {
+            if (!jobs.next(kv, a, S::kUnit, per_seq)) over = true;
+            // A job without a slot (whole jobs only) is one unit without a live one.
+            else job_units = max(1, jobs.b1 - jobs.b0), job_at = 0;
+        }
+        if (job_at < job_units) {
+            far.i = jobs.i, far.h = jobs.r / a.hb, far.hb = jobs.r % a.hb, far.end = jobs.last(S::kUnit);
+            far.s = jobs.first(S::kUnit) + job_at * S::kUnit;
+            far.units = min(kUnits, job_units - job_at), far.unit = job_at;
+            far.low = a.first ? a.first[jobs.i] : 0;
+            if (job_at == 0 && pw == 0) {   // the queries come from memory by the time the job begins
+                const int qh = far.h * a.group + far.hb * S::kHeads;
+                const int words = min(S::kHeads, a.group - far.hb * S::kHeads) * kv.c.head_dim;
+                const float *q = a.q + far.i * a.ldq + (int64_t)qh * kv.c.head_dim;
+                for (int x = 32 * lane; x < words; x += 1024) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + x));
+            }
+            job_at += far.units;
+            far.last = job_at == job_units;
+            const int end = min(far.end, far.s + far.units * S::kUnit);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const int s = first_slot(far, e);
+                uint32_t off;
+                id_far[e] = s < end ? kv.page_of(far.i, (uint32_t)s, off) : -1;
             }
         }
     }
-    // Nothing in flight may outlive the block.
-    __device__ __forceinline__ void finish() {
+    // Scores of a unit that nobody multiplies, for the weights.
+    __device__ __forceinline__ void no_scores(int s) const {
+        const int rows = min(S::kHeads, a.group - now.hb * S::kHeads), n = min((now.end - s + 15) / 16 * 16, S::kUnit);
+        float *sc = a.scores + (now.i * a.heads + (int64_t)now.h * a.group + now.hb * S::kHeads) * a.score_rows + s;
+        for (int r = 0; r < rows; ++r)
+            for (int x = lane; x < n; x += 32) sc[r * a.score_rows + x] = minus_inf();
+    }
+    // All units of the block; false when a bounded wait ran out.
+    __device__ __forceinline__ bool run() {
+        for (;;) {
+            while (now.units == 0) {
+                if (over && mid.units == 0 && far.units == 0) return true;
+                step();
+            }
+            for (int u = 0; u < now.units; ++u) {
+                const int s = now.s + u * S::kUnit;
+                // Lane k: the live slots of tile k.
+                const uint32_t on = lane < kHalves ? reinterpret_cast<const uint16_t *>(live)[u * kHalves + lane] : 0;
+                const uint32_t any = __ballot_sync(0xffffffffu, on != 0);
+                const bool last = now.last && u + 1 == now.units;
+                if (!any && !last) {
+                    if (a.scores && pw == 0) no_scores(s);
+                    continue;
+                }
+                const int stage = count % S::kStages;
+                if (count >= S::kStages &&
+                    !mbar_wait(pipe.empty + stage, (count / S::kStages - 1) & 1, &pipe.aborted))
+                    return false;
+                __syncwarp();
+                if (pw == 0) {
+                    if (lane < kHalves) pipe.live[stage][lane] = (uint16_t)on;
+                    if (lane == 0) pipe.unit[stage] = (now.unit + u) | (last ? kLastUnit : 0);
+                    __syncwarp();
+                }
+                if constexpr (TMA) {
+                    if (a.box == 8) boxes<8>(u, s, stage);
+                    else if (a.box == 16) boxes<16>(u, s, stage);
+                    else if (a.box == 32) boxes<32>(u, s, stage);
+                    else boxes<64>(u, s, stage);
+                } else {
+                    rows(u, s, stage);
+                }
+                ++count;
+            }
+            now.units = 0;
+        }
+    }
+    // Straight code: a lane issues a copy in about 100 cycles, 200 in a loop over boxes.
+    template <int BOX>
+    __device__ __forceinline__ void boxes(int u, int s, int stage) {
+        if constexpr (S::kUnit % BOX == 0) {
+            constexpr int N = S::kUnit / BOX;
+            const uint8_t *on = live + u * (S::kUnit / 8);
+            bool has = false;
+            if (lane < N) {
+#pragma unroll
+                for (int x = 0; x < BOX / 8; ++x) has |= on[lane * (BOX / 8) + x] != 0;
+            }
+            const uint32_t mask = __ballot_sync(0xffffffffu, has);
+            if (lane == 0) {
+                uint64_t *bar = pipe.full + stage;
+                mbar_expect_tx(bar, (uint32_t)(__popc(mask) * BOX) * S::kRow);
+                int page[N];
+#pragma unroll
+                for (int b = 0; b < N; ++b) page[b] = ids[(u * S::kUnit + b * BOX) / 8];
+                char *to = smem + stage * S::kStage + pw * (S::kStage / 2);
+                int off = (int)offset(s);
+#pragma unroll
+                for (int b = 0; b < N; ++b) {
+                    if (mask >> b & 1u) {
+                        const int c1 = a.token_major ? now.h : off, c2 = a.token_major ? off : now.h;
+#pragma unroll
+                        for (int k = 0; k < S::kRow / 128; ++k)
+                            tma_load_4d(to + b * BOX * 128 + k * 128 * S::kUnit, map, bar, k * 128 / S::kES, c1, c2,
+                                        page[b]);
+                    }
+                    off += BOX;
+                    if (off == (int)kv.page.d) off = 0;
+                }
+            }
+            __syncwarp();
+        }
+    }
+    __device__ __forceinline__ void rows(int u, int s, int stage) {
+        constexpr int kMine = S::kUnit / kProducers;
+        const char *kp = static_cast<const char *>(kv.c.k), *vp = static_cast<const char *>(kv.c.v);
+        const int chunks = kv.c.head_dim * S::kES / 16;
+        const uint32_t to = smem_u32(smem + stage * S::kStage);
+        for (int r0 = pw * kMine; r0 < (pw + 1) * kMine; r0 += 16) {
+            const int e = u * S::kUnit + r0 + (lane & 15);
+            const bool on = live[e >> 3] >> (e & 7) & 1u;
+            const int64_t row = on ? kv.element(ids[e], now.h, offset(s + r0 + (lane & 15))) * S::kES : -1;
+            if (!__any_sync(0xffffffffu, on)) continue;
+#pragma unroll 8
+            for (int x = 0; x < 16 * S::kChunks / 32; ++x) {
+                const int at16 = x * 32 + lane, rr = at16 / S::kChunks, c = at16 % S::kChunks;
+                const int64_t from = __shfl_sync(0xffffffffu, row, rr);
+                const bool ok = from >= 0 && c < chunks;
+                const uint32_t dst = to + chunk_at<128 * S::kUnit>(r0 + rr, c);
+                const int64_t src = ok ? from + c * 16 : 0;
+                copy16(dst, kp + src, ok);
+                copy16(dst + S::kStage / 2, vp + src, ok);
+            }
+        }
+        copies_arrive(pipe.full + stage);
+        if (pw == 0 && lane == 0) mbar_arrive(pipe.full + stage);   // with the stage's live slots and unit
+    }
+    // After an abort: nothing in flight may outlive the block.
+    __device__ __forceinline__ void drain() {
         if constexpr (TMA) {
-            if (*aborted)
-                for (int s = 0; s < S::kStages; ++s)
-                    if (flying >> s & 1u) mbar_drain(full + s, phase >> s & 1u);
+            for (int c = max(0, count - S::kStages); c < count; ++c)
+                mbar_drain(pipe.full + c % S::kStages, c / S::kStages & 1);
         } else {
-            copies_wait<0>();
+            copies_wait_all();
         }
     }
 };
 
+template <int THREADS>
+__device__ __forceinline__ void consumers_sync() {
+    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+}
+
 template <class T, int DP, int NT, bool TMA>
-__global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps, Shape<T, DP, NT>::kBlocks)
+__global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers), Shape<T, DP, NT>::kBlocks)
     attend_kernel(KvView kv, AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
     using S = Shape<T, DP, NT>;
-    constexpr int W = S::kWarps, THREADS = 32 * W, NS = S::kStages, MS = S::kSlots;
+    constexpr int W = S::kWarps, THREADS = 32 * W, ALL = THREADS + 32 * kProducers, MS = S::kSlots;
     extern __shared__ __align__(1024) char smem[];
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + S::kMiscAt);
-    long long *place_sh = reinterpret_cast<long long *>(bars + W * NS);
-    volatile int *aborted = reinterpret_cast<volatile int *>(place_sh + W + 2);
+    static_assert(sizeof(Pipe<T, DP, NT>) <= 512, "pipe");
+    Pipe<T, DP, NT> &pipe = *reinterpret_cast<Pipe<T, DP, NT> *>(smem + S::kMiscAt);
     float *mo = reinterpret_cast<float *>(smem + S::kRing), *mm = mo + MS * S::kHeads * S::kPitch,
           *ml = mm + MS * S::kHeads;
     uint32_t *qs = reinterpret_cast<uint32_t *>(smem + S::kQAt);
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, g = lane >> 2, t = lane & 3;
     const int D = kv.c.head_dim, KV = kv.c.kv_heads, per_seq = KV * a.hb;
     if (tid == 0) {
-        *aborted = 0;
-        if (TMA) {
-            for (int x = 0; x < W * NS; ++x) mbar_init(bars + x, 1);
-            mbar_init_fence();
+        pipe.aborted = 0;
+        for (int x = 0; x < S::kStages; ++x) {
+            mbar_init(pipe.full + x, TMA ? kProducers : 32 * kProducers + 1);
+            mbar_init(pipe.empty + x, W);
         }
+        mbar_init_fence();
     }
     __syncthreads();
     pdl_enter();
@@ -707,43 +790,61 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps, Shape<T, DP, NT
     if (a.whole) {
         jobs.i = blockIdx.x / per_seq, jobs.at = blockIdx.x % per_seq, jobs.left = 1;
     } else {
-        find_place<THREADS>(kv, a, S::kUnit, per_seq, blockIdx.x, gridDim.x, total, end, jobs, place_sh);
+        find_place<ALL>(kv, a, S::kUnit, per_seq, blockIdx.x, gridDim.x, total, end, jobs, pipe.place);
         // Sequences without a slot belong to nobody's units: their rows are shared out.
         for (int64_t i = blockIdx.x; i < kv.c.seqs; i += gridDim.x)
             if (kv.length(a.lens, i, a.max_len) == 0)
-                for (int x = tid; x < a.heads * D; x += THREADS) a.out[i * a.ldo + x] = 0.0f;
+                for (int x = tid; x < a.heads * D; x += ALL) a.out[i * a.ldo + x] = 0.0f;
         if (tid == 0) a.split[3 * blockIdx.x] = -1;
     }
-    Feed<T, DP, NT, TMA> feed(kv, a, &mk, &mv, per_seq, jobs, smem, bars, aborted);
-#pragma unroll 1
-    for (int n = 0; n < NS - 1; ++n) feed.issue(n);
+    if (w >= W) {
+        Producer<T, DP, NT, TMA> producer(kv, a, &mk, &mv, pipe, per_seq, jobs, smem, w - W);
+        if (!producer.run()) {
+            *(volatile int *)&pipe.aborted = 1;   // results are void; the device status says so
+            if (lane == 0) atomicExch(&g_attend_error, 1u);
+            producer.drain();
+        }
+        return;
+    }
 
     Warp<T, DP, NT> wp;
-    int use = 0;   // ring stage of the next tile
+    int stage = 0, parity = 0;
     while (jobs.next(kv, a, S::kUnit, per_seq)) {
         const int s0 = jobs.first(S::kUnit), s1 = jobs.last(S::kUnit);
         const int h = jobs.r / a.hb, hb = jobs.r % a.hb;
         const int rows = min(S::kHeads, a.group - hb * S::kHeads);
         const int64_t i = jobs.i, qh = (int64_t)h * a.group + hb * S::kHeads;
-        const int tiles = (s1 - s0 + 15) / 16, mine = tiles > w ? (tiles - w + W - 1) / W : 0;
         float *scores = a.scores ? a.scores + (i * a.heads + qh) * a.score_rows + s0 : nullptr;
         wp.clear();
         wp.queries(a.q + i * a.ldq + qh * D, D, rows, a.scale2, qs);
-        if constexpr (!S::kQReg) __syncthreads();
-        for (int n = 0; n < mine; ++n) {
-            if constexpr (!TMA) copies_wait<NS - 2>();
-            __syncwarp();
-            const uint32_t live = (uint32_t)feed.queue & 0xffffu;
-            feed.queue >>= 16;
-            feed.issue(NS - 2);
-            float *sc = scores ? scores + 16 * (w + n * W) : nullptr;   // rows of 16 slots exist in whole
+        if constexpr (!S::kQReg) consumers_sync<THREADS>();
+        for (int n = max(1, jobs.b1 - jobs.b0); n > 0; --n) {   // at most; the job's last unit ends it
+            if (!mbar_wait(pipe.full + stage, parity, &pipe.aborted)) {
+                *(volatile int *)&pipe.aborted = 1;
+                if (lane == 0) atomicExch(&g_attend_error, 1u);
+                break;
+            }
+            const uint32_t live = pipe.live[stage][w];
+            const int unit = pipe.unit[stage], at = (unit & (kLastUnit - 1)) * S::kUnit + 16 * w;
+            char *k = smem + stage * S::kStage + 16 * w * 128, *v = k + S::kStage / 2;
+            float *sc = scores && s0 + at < s1 ? scores + at : nullptr;   // rows of 16 slots exist in whole
             if (live) {
-                feed.ready(use, live);
-                wp.tile(smem_u32(feed.ring + use * S::kTile), live, qs, sc, a.score_rows, rows);
+                if (live != 0xffffu) {   // a weight of zero does not make up for a NaN in a slot that does not count
+                    for (int x = lane; x < 16 * S::kChunks; x += 32)
+                        if (!(live >> (x / S::kChunks) & 1u))
+                            *reinterpret_cast<uint4 *>(v + chunk_at<128 * S::kUnit>(x / S::kChunks, x % S::kChunks)) =
+                                make_uint4(0, 0, 0, 0);
+                    if (TMA) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // before the next copy
+                    __syncwarp();
+                }
+                wp.tile(smem_u32(k), smem_u32(v), live, qs, sc, a.score_rows, rows);
             } else if (sc) {   // no slot counts: the weights read that
                 for (int x = lane; x < 16 * rows; x += 32) sc[(x >> 4) * a.score_rows + (x & 15)] = minus_inf();
             }
-            use = use + 1 == NS ? 0 : use + 1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(pipe.empty + stage);
+            if (++stage == S::kStages) stage = 0, parity ^= 1;
+            if (unit & kLastUnit) break;
         }
 
         // Merge of the warps through shared memory, the uppermost kSlots into
@@ -792,7 +893,7 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps, Shape<T, DP, NT
         };
         for (int top = W; top > 0; top -= MS) {   // a warp takes from and puts into the same slot
             if (w >= top - MS && w < top) put(w - (top - MS));
-            __syncthreads();
+            consumers_sync<THREADS>();
             if (w >= top - 2 * MS && w < top - MS) take(w - (top - 2 * MS));
         }
         const bool whole = jobs.b0 == 0 && jobs.b1 == jobs.nb;
@@ -830,9 +931,8 @@ __global__ void __launch_bounds__(32 * Shape<T, DP, NT>::kWarps, Shape<T, DP, NT
             a.split[3 * blockIdx.x + 1] = c;
             a.split[3 * blockIdx.x + 2] = total;
         }
-        __syncthreads();
+        consumers_sync<THREADS>();
     }
-    feed.finish();
 }
 
 template <class T, int DP, int NT, bool TMA>
@@ -844,7 +944,7 @@ int resident() {
     if (!ensure_smem_limit(done, attend_kernel<T, DP, NT, TMA>, S::kBytes, &dev)) return 0;
     std::atomic<int> &at = known[dev & 63];
     if ((n = at.load(std::memory_order_relaxed)) > 0) return n;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<T, DP, NT, TMA>, 32 * S::kWarps, S::kBytes) !=
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<T, DP, NT, TMA>, 32 * (S::kWarps + kProducers), S::kBytes) !=
         cudaSuccess)
         return 0;
     n *= sm_count(dev);
@@ -853,11 +953,10 @@ int resident() {
 }
 
 // A pool as a tensor of (channel, slot, head, page), or (channel, head, slot,
-// page) where heads are the closer ones; box: 128 bytes of 16 slots.  False
-// where the strides do not nest (or no tile lies in one page): the lanes copy.
+// page) where heads are the closer ones; box: 128 bytes of `slots_box` slots.
+// False where the strides do not nest: the lanes copy.
 template <class T>
-bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int *token_major) {
-    if (c.page_size % 16) return false;
+bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int slots_box, int *token_major) {
     constexpr int kES = sizeof(T);
     const cuuint64_t D = (cuuint64_t)c.head_dim * kES, slots = (cuuint64_t)c.page_size, heads = (cuuint64_t)c.kv_heads;
     cuuint64_t slot = (cuuint64_t)c.slot_stride * kES, head = (cuuint64_t)c.head_stride * kES;
@@ -872,7 +971,7 @@ bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int *token
     if (!fn) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, tm ? heads : slots, tm ? slots : heads, (cuuint64_t)c.pages};
     const cuuint64_t strides[3] = {inner, outer, page};
-    const cuuint32_t box[4] = {128 / kES, tm ? 1u : 16u, tm ? 16u : 1u, 1}, each[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {128 / kES, tm ? 1u : (cuuint32_t)slots_box, tm ? (cuuint32_t)slots_box : 1u, 1}, each[4] = {1, 1, 1, 1};
     const CUtensorMapDataType type = kES == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                      : kTerms<T> == 3 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     *token_major = tm;
@@ -893,7 +992,7 @@ struct Instance {
         blocks = a.blocks;
         {
             KernelSpan span("attend", st);
-            const dim3 grid((unsigned)a.blocks), block(32 * S::kWarps);
+            const dim3 grid((unsigned)a.blocks), block(32 * (S::kWarps + kProducers));
             // More than one wave (whole jobs) must not stack up early.
             if (a.blocks <= wave) pdl_launch(attend_kernel<T, DP, NT, TMA>, grid, block, S::kBytes, st, kv, a, mk, mv);
             else attend_kernel<T, DP, NT, TMA><<<grid, block, S::kBytes, st>>>(kv, a, mk, mv);
@@ -903,7 +1002,12 @@ struct Instance {
     static mosaic_status launch(const mosaic_kv_cache &c, AttendArgs a, int &blocks, cudaStream_t st) {
         const KvView kv(c);
         alignas(64) CUtensorMap mk = {}, mv = {};
-        if (pool_map<T>(&mk, c, c.k, &a.token_major) && pool_map<T>(&mv, c, c.v, &a.token_major))
+        // A box is as many slots as divide a page and a unit, 8 at least (a swizzle's rows).
+        for (a.box = 64; a.box >= 8 && (S::kUnit % a.box || c.page_size % a.box); a.box /= 2) {
+        }
+        // Positions are then read 8 at a time.
+        if (a.box >= 8 && (!a.first || aligned16(c.position)) && pool_map<T>(&mk, c, c.k, a.box, &a.token_major) &&
+            pool_map<T>(&mv, c, c.v, a.box, &a.token_major))
             return go<true>(kv, a, mk, mv, blocks, st);
         return go<false>(kv, a, mk, mv, blocks, st);
     }
