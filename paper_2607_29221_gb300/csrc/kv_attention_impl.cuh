@@ -110,7 +110,7 @@ template <class T> constexpr float kShift = 0.0f;
 template <> constexpr float kShift<__half> = 12.0f;
 
 constexpr int kTogether = 4;   // chains of products at a time
-constexpr int kLookup = 4 * 128 + 32;   // bytes of a producer's page ids and live slots
+constexpr int kLookup = 4 * 256 + 32;   // bytes of a producer's page ids and live slots
 
 // DP: head_dim padded to 64, 128 or 256.  NT: tiles of 8 query heads.
 template <class T, int DP, int NT>
@@ -524,14 +524,13 @@ constexpr int kLastUnit = 1 << 30;
 // the positions, one group) before their units are copied; units without a
 // live slot are left out (but for a job's last, which ends it).
 // TMA: tensor copies of a.box slots that share a page, a lane's to issue, the
-// first warp K and the second V; a lane looks up 8 slots.  Else every lane
-// copies 16 bytes at a time, each warp half of a unit's rows, and looks up
-// four single slots.
+// first warp K and the second V; a lane looks up 8 slots at once.  Else every
+// lane copies 16 bytes at a time, each warp half of a unit's rows, and looks up
+// 8 single slots.
 template <class T, int DP, int NT, bool TMA>
 struct Producer {
     using S = Shape<T, DP, NT>;
-    static constexpr int kEach = TMA ? 1 : 4;                  // look-ups of a lane
-    static constexpr int kSpan = TMA ? 256 : 128;              // slots of a group
+    static constexpr int kSpan = 256, kEach = TMA ? 1 : 8;     // slots of a group, look-ups of a lane
     static constexpr int kUnits = kSpan / S::kUnit, kHalves = S::kUnit / 16;
     struct Group {
         int h, hb, s, end, units, low;   // head, first slot, end of the job's slots, units, position bound
@@ -551,7 +550,7 @@ struct Producer {
     int job_units, job_at;   // units of the newest group's job, and how many have a group
     Group now, mid, far;
     int id_mid[kEach], id_far[kEach];
-    int4 pos_mid[TMA ? 2 : 1];
+    int pos_mid[8];
     int count;          // units copied
     bool over;          // no further job
 
@@ -561,7 +560,7 @@ struct Producer {
         : kv(kv_), a(a_), map(pw_ ? mv : mk), pipe(pipe_), smem(smem_), per_seq(per_seq_), pw(pw_),
           lane(threadIdx.x & 31), jobs(j) {
         ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge + pw * kLookup);
-        live = reinterpret_cast<uint8_t *>(ids + 128);
+        live = reinterpret_cast<uint8_t *>(ids + 256);
         job_units = job_at = count = 0;
         over = false;
         now.units = mid.units = far.units = 0;
@@ -581,17 +580,14 @@ struct Producer {
                     if (id_mid[0] >= 0) {
                         on = 0xffu >> max(0, 8 - (mid.end - first_slot(mid, 0)));
                         if (a.first) {
-                            const int4 x = pos_mid[0], y = pos_mid[1];
-                            const int low = mid.low;
-                            on &= (x.x >= low) | (x.y >= low) << 1 | (x.z >= low) << 2 | (x.w >= low) << 3 |
-                                  (y.x >= low) << 4 | (y.y >= low) << 5 | (y.z >= low) << 6 | (y.w >= low) << 7;
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) on &= ~((uint32_t)(pos_mid[x] < mid.low) << x);
                         }
                     }
                     ids[lane] = id_mid[0];
                     live[lane] = (uint8_t)on;
                 } else {
-                    const int p = e == 0 ? pos_mid[0].x : e == 1 ? pos_mid[0].y : e == 2 ? pos_mid[0].z : pos_mid[0].w;
-                    const uint32_t on = __ballot_sync(0xffffffffu, id_mid[e] >= 0 && !(a.first && p < mid.low));
+                    const uint32_t on = __ballot_sync(0xffffffffu, id_mid[e] >= 0 && !(a.first && pos_mid[e] < mid.low));
                     ids[32 * e + lane] = id_mid[e];
                     if (lane == 0) reinterpret_cast<uint32_t *>(live)[e] = on;
                 }
@@ -605,9 +601,11 @@ struct Producer {
             if (!a.first || mid.units == 0 || id_mid[e] < 0) continue;
             const int32_t *p = kv.c.position + kv.mark(id_mid[e], mid.h, offset(first_slot(mid, e)));
             if constexpr (TMA) {   // 8 slots of a page whose size is a multiple of 8
-                pos_mid[0] = reinterpret_cast<const int4 *>(p)[0], pos_mid[1] = reinterpret_cast<const int4 *>(p)[1];
+                const int4 x = reinterpret_cast<const int4 *>(p)[0], y = reinterpret_cast<const int4 *>(p)[1];
+                pos_mid[0] = x.x, pos_mid[1] = x.y, pos_mid[2] = x.z, pos_mid[3] = x.w;
+                pos_mid[4] = y.x, pos_mid[5] = y.y, pos_mid[6] = y.z, pos_mid[7] = y.w;
             } else {
-                (e == 0 ? pos_mid[0].x : e == 1 ? pos_mid[0].y : e == 2 ? pos_mid[0].z : pos_mid[0].w) = *p;
+                pos_mid[e] = *p;
             }
         }
         far.units = 0;
