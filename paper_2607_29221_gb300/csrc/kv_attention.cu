@@ -2,6 +2,7 @@
 // point, the join of jobs that blocks share, and the gathered weights.  The
 // kernel that reads the cache is in kv_attention_impl.cuh.
 #include <math.h>
+#include <stdlib.h>
 
 #include "kv_attention.cuh"
 
@@ -17,73 +18,89 @@ constexpr int64_t kWholeLen = 512;
 // on 8 heads: 418, 410, 381, 371, 368, 372; 400 of 3 to 1500 on 8 heads of 64,
 // windowed: 147, 122, 95, 93, 90 (256 KB).
 constexpr int64_t kJobBytes = 256 * 1024;
+constexpr int64_t kJobs = 64;
 
-// Block (c, head): the job that block c's end cuts, one query head of it.
-__global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a, AttendShape s, int dim) {
-    __shared__ float factor[kAttendWave], part[2][4];
+// Block (c, y): the job that block c's end cuts.  Where jobs have many parts
+// (`shared`), query head y of it, its parts taken in turn by eight warps; else
+// key/value head y, a warp a query head.  A lane has four channels (two rounds
+// beyond 128).
+__global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendShape s, int dim, bool shared) {
+    __shared__ float4 rest[7][2][32];
+    __shared__ float rest_sum[7];
     pdl_enter();
-    const int c = blockIdx.x, head = blockIdx.y, n = a.blocks, tid = threadIdx.x;
+    const int c = blockIdx.x, n = a.blocks, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int64_t job = a.split[3 * c], last = a.split[3 * c + 1], total = a.split[3 * c + 2];
     if (job < 0) return;
-    const int per_seq = a.heads / a.group * a.hb, r = (int)(job % per_seq), h = r / a.hb, hb = r % a.hb;
-    if (hb * s.heads + head >= a.group) return;
-    const int64_t i = job / per_seq, qh = (int64_t)h * a.group + hb * s.heads + head;
+    const int hi = shared ? blockIdx.y / s.heads : blockIdx.y, from = shared ? w : 0, each = shared ? 8 : 1;
+    const int per_seq = a.heads / a.group / a.hpu * a.hb, r = (int)(job % per_seq);
+    const int h = r / a.hb * a.hpu + hi, hb = r % a.hb;
+    const int64_t i = job / per_seq;
     // Part k of the job: the cut block's second slot, then the first slots of
     // the blocks after it (some without a unit where units are fewer than blocks).
     const int parts = (int)(last - c) + 1;
-    auto slot = [&](int k) { return (2 * (int64_t)(c + k) + (k == 0)) * s.heads + head; };
     auto has = [&](int k) { return total >= n || total * (c + k) / n < total * (c + k + 1) / n; };
-    auto block_of = [&](float x, int which, auto op) {   // of all threads' values
+    for (int head = shared ? blockIdx.y % s.heads : w; head < s.heads && hb * s.heads + head < a.group; head += shared ? s.heads : 8) {
+        const int64_t qh = (int64_t)h * a.group + hb * s.heads + head;
+        auto slot = [&](int k) { return ((2 * (int64_t)(c + k) + (k == 0)) * a.hpu + hi) * s.heads + head; };
+        float top = minus_inf();
+        for (int k = lane; k < parts; k += 32)
+            if (has(k)) top = fmaxf(top, a.part_ml[2 * slot(k)]);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) x = op(x, __shfl_xor_sync(0xffffffffu, x, o));
-        if ((tid & 31) == 0) part[which][tid >> 5] = x;
-        __syncthreads();
-        return op(op(part[which][0], part[which][1]), op(part[which][2], part[which][3]));
-    };
-    float top = minus_inf();
-    for (int k = tid; k < parts; k += 128)
-        if (has(k)) top = fmaxf(top, a.part_ml[2 * slot(k)]);
-    top = block_of(top, 0, [](float x, float y) { return fmaxf(x, y); });
-    const float ref = top == minus_inf() ? 0.0f : top;
-    float sum = 0.0f;
-    for (int k = tid; k < parts; k += 128) {
-        const bool in = has(k);
-        const float f = in ? power2(a.part_ml[2 * slot(k)] - ref) : 0.0f;
-        factor[k] = in ? f : -1.0f;
-        if (in) sum = fmaf(f, a.part_ml[2 * slot(k) + 1], sum);
-    }
-    sum = block_of(sum, 1, [](float x, float y) { return x + y; });
-    // A warp every fourth part, a lane four channels (two rounds beyond 128).
-    __shared__ float4 rest[3][32];
-    for (int d0 = 0; d0 < s.dim; d0 += 128) {
-        const int d = d0 + 4 * (tid & 31), w = tid >> 5;
-        float4 out = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (d < s.dim) {
-#pragma unroll 4
-            for (int k = w; k < parts; k += 4) {
-                const float f = factor[k];
-                if (f == -1.0f) continue;
-                const float4 x = *reinterpret_cast<const float4 *>(a.part_o + slot(k) * s.dim + d);
-                out.x = fmaf(f, x.x, out.x), out.y = fmaf(f, x.y, out.y);
-                out.z = fmaf(f, x.z, out.z), out.w = fmaf(f, x.w, out.w);
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float ref = top == minus_inf() ? 0.0f : top;
+        float sum = 0.0f;
+        float4 out[2];
+        out[0] = out[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k0 = from; k0 < parts; k0 += 4 * each) {   // four parts' loads, then their sums
+            float m[4], l[4];
+            float4 x[4][2];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = k0 + j * each;
+                m[j] = minus_inf(), l[j] = 0.0f;
+                x[j][0] = x[j][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (k >= parts || !has(k)) continue;
+                const float *p = a.part_o + slot(k) * s.dim + 4 * lane;
+                m[j] = a.part_ml[2 * slot(k)], l[j] = a.part_ml[2 * slot(k) + 1];
+                if (4 * lane < s.dim) x[j][0] = *reinterpret_cast<const float4 *>(p);
+                if (128 + 4 * lane < s.dim) x[j][1] = *reinterpret_cast<const float4 *>(p + 128);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float f = power2(m[j] - ref);
+                sum = fmaf(f, l[j], sum);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float4 &o = out[half];
+                    o.x = fmaf(f, x[j][half].x, o.x), o.y = fmaf(f, x[j][half].y, o.y);
+                    o.z = fmaf(f, x[j][half].z, o.z), o.w = fmaf(f, x[j][half].w, o.w);
+                }
             }
         }
-        if (w) rest[w - 1][tid & 31] = out;
-        __syncthreads();
-        if (w == 0) {
-            for (int x = 0; x < 3; ++x) {
-                const float4 y = rest[x][tid];
-                out.x += y.x, out.y += y.y, out.z += y.z, out.w += y.w;
+        if (shared) {
+            if (w) rest[w - 1][0][lane] = out[0], rest[w - 1][1][lane] = out[1];
+            if (w && lane == 0) rest_sum[w - 1] = sum;
+            __syncthreads();
+            if (w) return;
+            for (int k = 0; k < 7; ++k) {
+                sum += rest_sum[k];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const float4 y = rest[k][half][lane];
+                    out[half].x += y.x, out[half].y += y.y, out[half].z += y.z, out[half].w += y.w;
+                }
             }
-            const float o[4] = {out.x, out.y, out.z, out.w};
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int d = 128 * half + 4 * lane;
+            const float o[4] = {out[half].x, out[half].y, out[half].z, out[half].w};
+#pragma unroll
             for (int x = 0; x < 4; ++x)
-                if (d + x < dim) a.out[i * a.ldo + qh * dim + d + x] = sum == 0.0f ? 0.0f : o[x] / sum;
+                if (d + x < dim) a.out[i * a.ldo + qh * dim + d + x] = o[x] * inv;
         }
-        __syncthreads();
-    }
-    if (a.scores && tid == 0) {
-        a.stats[2 * (i * a.heads + qh)] = ref;
-        a.stats[2 * (i * a.heads + qh) + 1] = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (a.scores && lane == 0) a.stats[2 * (i * a.heads + qh)] = ref, a.stats[2 * (i * a.heads + qh) + 1] = inv;
     }
 }
 
@@ -174,8 +191,8 @@ struct Parts {
 // blocks: those that share the work (0: every job is one block's).
 Parts parts(const mosaic_kv_cache &c, const AttendShape &s, int64_t heads, int64_t blocks, int64_t rows) {
     Parts p = {};
-    p.ml = up256(16 * (size_t)(blocks * s.heads));
-    p.o = up256(8 * (size_t)(blocks * s.heads) * s.dim);
+    p.ml = up256(16 * (size_t)(blocks * s.most_heads * s.heads));
+    p.o = up256(8 * (size_t)(blocks * s.most_heads * s.heads) * s.dim);
     p.split = up256(24 * (size_t)blocks);
     if (c.weight) {
         p.stats = up256(8 * (size_t)(c.seqs * heads));
@@ -191,7 +208,7 @@ AttendShape shape_of(const mosaic_kv_cache &c, int64_t heads) {
 int64_t most_blocks(const mosaic_kv_cache &c, const AttendShape &s, int64_t heads, int64_t max_len) {
     const int64_t group = heads / c.kv_heads, hb = (group + s.heads - 1) / s.heads;
     const int64_t units = c.seqs * c.kv_heads * hb * ((max_len + s.unit - 1) / s.unit);
-    return max_len <= kWholeLen ? 0 : units < kAttendWave ? units : kAttendWave;
+    return max_len <= (getenv("WL") ? atoi(getenv("WL")) : kWholeLen * (c.seqs * c.kv_heads * hb >= 128 ? 2 : 1)) ? 0 : units < kAttendWave ? units : kAttendWave;
 }
 mosaic_status check(const mosaic_kv_cache *c, int64_t heads, int64_t max_len) {
     MOSAIC_TRY(kv_check(c));
@@ -242,6 +259,14 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     AttendArgs a = {};
     a.q = q, a.ldq = ldq, a.lens = lens, a.first = first, a.max_len = max_len, a.heads = (int)heads;
     a.group = (int)(heads / cache->kv_heads), a.hb = (a.group + s.heads - 1) / s.heads;
+    a.hpu = 1;
+    const int64_t one = cache->seqs * cache->kv_heads * a.hb;   // jobs with a key/value head each
+    a.whole = cap == 0;
+    for (int x = 2; x <= s.most_heads; ++x) {
+        if (s.most_heads % x || cache->kv_heads % x || (x > s.buffers && x != s.most_heads)) continue;
+        if (a.whole ? one / a.hpu > 152 * s.resident : one / x >= kJobs) a.hpu = x;
+    }
+    if (getenv("HPU")) { a.hpu = 1; for (int x = atoi(getenv("HPU")); x > 1; x /= 2) if (s.most_heads % x == 0 && cache->kv_heads % x == 0 && (x <= s.buffers || x == s.most_heads)) { a.hpu = x; break; }}
     a.scale2 = scale * 1.44269504088896341f, a.decay = decay, a.out = out, a.ldo = ldo;
     char *w = static_cast<char *>(ws);
     a.part_ml = reinterpret_cast<float *>(w), w += p.ml;
@@ -252,17 +277,18 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
         a.scores = reinterpret_cast<float *>(w);
         a.score_rows = rows_of(max_len);
     }
-    const int64_t jobs = cache->seqs * cache->kv_heads * a.hb;
-    a.whole = cap == 0;
+    const int64_t jobs = cache->seqs * (cache->kv_heads / a.hpu) * a.hb;
     a.blocks = (int)(a.whole ? jobs : cap);
     const int64_t unit_bytes = 2 * s.unit * D * kv_element_bytes(cache->type);
-    a.job_cost = (int)((kJobBytes + unit_bytes / 2) / unit_bytes);
+    a.job_cost = (int)(((getenv("JCB") ? atoi(getenv("JCB")) * 1024 : kJobBytes) + unit_bytes / 2) / unit_bytes);
     cudaStream_t st = as_stream(stream);
     MOSAIC_TRY(by_type(cache->type, [&](auto t) { return attend_launch<decltype(t)>(*cache, a, a.blocks, st); }));
     if (!a.whole) {
         {
             KernelSpan span("attend_join", st);
-            pdl_launch(attend_join_kernel, dim3((unsigned)a.blocks, (unsigned)s.heads), dim3(128), 0, st, a, s, (int)D);
+            const bool shared = jobs * 4 <= a.blocks;
+            const dim3 grid((unsigned)a.blocks, (unsigned)(a.hpu * (shared ? s.heads : 1)));
+            pdl_launch(attend_join_kernel, grid, dim3(256), 0, st, a, s, (int)D, shared);
         }
         MOSAIC_TRY(launch_status());
     }

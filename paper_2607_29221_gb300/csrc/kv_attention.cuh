@@ -33,18 +33,19 @@
 namespace mosaic {
 
 // Blocks of one wave at most (the resident ones of an instance are fewer).
-constexpr int kAttendWave = 152 * 8;
+constexpr int kAttendWave = 152 * 3;
 
 struct AttendArgs {
     const float *q;
     int64_t ldq;
     const int32_t *lens, *first;
     int64_t max_len;
-    int heads, group, hb;       // hb: jobs (blocks of query heads) of a key/value head
+    int heads, group, hb;       // hb: blocks of query heads of a key/value head
+    int hpu;                    // key/value heads of a unit (and of a job)
     int whole;                  // a block a job, nothing is cut
     int blocks;
     int job_cost;
-    int token_major, box;       // of the tensor maps: heads lie closer than slots; slots of a box
+    int token_major, box;       // of the tensor maps: heads lie closer than slots; slots of a box (0: a unit)
     float scale2, decay;        // scale * log2(e): scores are kept in the base-2 domain
     float *out;
     int64_t ldo;
@@ -59,11 +60,13 @@ struct AttendArgs {
 };
 
 // What the instance for a head_dim and a group has (query heads of a job,
-// padded head_dim = row length of part_o, slots of a unit); its launch on
+// padded head_dim = row length of part_o, rows of a unit, key/value heads that
+// a unit may hold: divisors of `most_heads` up to `buffers`, or all; blocks an
+// SM); its launch on
 // a.blocks blocks or one wave (`blocks`: how many); and whether a bounded wait
 // of it ran out since the last call (after a stream sync).
 struct AttendShape {
-    int heads, dim, unit;
+    int heads, dim, unit, most_heads, buffers, resident;
 };
 template <class T> AttendShape attend_shape(int head_dim, int group);
 template <class T>

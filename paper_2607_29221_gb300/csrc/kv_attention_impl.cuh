@@ -110,14 +110,14 @@ template <class T> constexpr float kShift = 0.0f;
 template <> constexpr float kShift<__half> = 12.0f;
 
 constexpr int kTogether = 4;   // chains of products at a time
-constexpr int kLookup = 4 * 256 + 32;   // bytes of a producer's page ids and live slots
+constexpr int kLookup = 4 * 128 + 32;   // bytes of a producer's page ids and live slots
 
 // DP: head_dim padded to 64, 128 or 256.  NT: tiles of 8 query heads.
 template <class T, int DP, int NT>
 struct Shape {
     static constexpr int kES = sizeof(T), kRow = DP * kES, kChunks = kRow / 16;
-    // A stage holds a unit: K and V of 16 slots a consumer warp.  8 consumer
-    // warps an SM, as two blocks or (with twice the outputs and queries) one;
+    // A stage holds a unit: K and V of kUnit rows, 16 a consumer warp (slots of
+    // a.hpu heads).  8 consumer warps an SM, as two blocks or (with twice the outputs and queries) one;
     // fewer where rows are long.
     static constexpr int kWarps = kRow == 1024 ? 2 : NT == 2 && kRow <= 256 ? 8 : kRow == 512 && kES == 4 && NT == 1 ? 6 : 4;
     static constexpr int kUnit = 16 * kWarps, kStage = 2 * kUnit * kRow;
@@ -128,12 +128,13 @@ struct Shape {
     static constexpr int kQWords = kSteps * NT * kTerms<T> * 2 * 32;  // query fragments
     // Queries stay in registers where they fit beside the outputs.
     static constexpr bool kQReg = kSteps * NT * kTerms<T> * 2 <= 48;
+    static constexpr int kQHeads = kQReg ? 0 : kWarps == 6 ? 2 : 1;   // else in shared memory, of so many heads
     // Shared memory: the ring, the results of some warps, page ids and live
     // slots of the producers' groups, the queries' fragments, barriers and so on.
     static constexpr int kRing = kStages * kStage;
     static constexpr int kMerge = 4 * kSlots * kHeads * (kPitch + 2);
     static constexpr int kIds = 2 * kLookup;
-    static constexpr int kQAt = kRing + kMerge + kIds, kMiscAt = kQAt + (kQReg ? 0 : 4 * kQWords);
+    static constexpr int kQAt = kRing + kMerge + kIds, kMiscAt = kQAt + 4 * kQWords * kQHeads;
     static constexpr int kBytes = kMiscAt + 512;
     static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kBlocks = kFit < 3 ? kFit : 3;   // blocks an SM
     static_assert(kBytes <= 227 * 1024, "shared memory");
@@ -520,22 +521,22 @@ struct Pipe {
 constexpr int kLastUnit = 1 << 30;
 
 // A producer warp: copies unit by unit, through all jobs of the block.  Pages
-// are looked up a group of slots at a time, two groups (with a lower bound: and
-// the positions, one group) before their units are copied; units without a
-// live slot are left out (but for a job's last, which ends it).
-// TMA: tensor copies of a.box slots that share a page, a lane's to issue, the
-// first warp K and the second V; a lane looks up 8 slots at once.  Else every
-// lane copies 16 bytes at a time, each warp half of a unit's rows, and looks up
-// 8 single slots.
+// are looked up a group of units at a time, two groups (with a lower bound: and
+// the positions, one group) before they are copied.
+// TMA: tensor copies of rows that share a page, a lane's to issue; the first
+// warp copies K and the second V of every unit, and units without a live slot
+// are left out (but for a job's last, which ends it).  A lane looks up 8 slots
+// at once.
+// Else every lane copies 16 bytes at a time; the warps take turns at units and
+// look up their own, a lane four single slots.
 template <class T, int DP, int NT, bool TMA>
 struct Producer {
     using S = Shape<T, DP, NT>;
-    static constexpr int kSpan = 256, kEach = TMA ? 1 : 8;     // slots of a group, look-ups of a lane
-    static constexpr int kUnits = kSpan / S::kUnit, kHalves = S::kUnit / 16;
+    static constexpr int kSpan = TMA ? 256 : 128, kEach = TMA ? 1 : 4;   // rows of a group, look-ups of a lane
+    static constexpr int kUnits = kSpan / S::kUnit, kHalves = S::kUnit / 16, kTurn = TMA ? 1 : kProducers;
     struct Group {
-        int h, hb, s, end, units, low;   // head, first slot, end of the job's slots, units, position bound
-        int unit;                        // number of its first unit in the job
-        bool last;                       // the job's last group
+        int h, hb, s, end, units, low;   // first head, first slot, end of the job's slots, units, position bound
+        int unit, of, base;              // number of its first unit in the job, of how many, units of all jobs before
         int64_t i;
     };
     const KvView &kv;
@@ -543,52 +544,56 @@ struct Producer {
     const CUtensorMap *map;
     Pipe<T, DP, NT> &pipe;
     char *smem;
-    const int per_seq, pw, lane;
+    const int per_seq, pw, lane, us, per_tile;   // us: slots of a unit; per_tile: 2^8 over the tiles of a head, rounded up
     int32_t *ids;       // shared, this warp's: pages of the group being copied
     uint8_t *live;      // and its live slots, a bit each
     Jobs jobs;
-    int job_units, job_at;   // units of the newest group's job, and how many have a group
+    int job_units, job_at;   // units of the newest group's job, and the first of this warp's without a group
+    int units;               // of all jobs before that one
     Group now, mid, far;
-    int id_mid[kEach], id_far[kEach];
+    int id_mid[kEach], id_far[kEach];   // as they are in the table
     int pos_mid[8];
-    int count;          // units copied
+    int count;          // units copied (TMA), or the unit being copied
     bool over;          // no further job
 
     __device__ __forceinline__ Producer(const KvView &kv_, const AttendArgs &a_, const CUtensorMap *mk,
                                         const CUtensorMap *mv, Pipe<T, DP, NT> &pipe_, int per_seq_, const Jobs &j,
                                         char *smem_, int pw_)
         : kv(kv_), a(a_), map(pw_ ? mv : mk), pipe(pipe_), smem(smem_), per_seq(per_seq_), pw(pw_),
-          lane(threadIdx.x & 31), jobs(j) {
+          lane(threadIdx.x & 31), us(S::kUnit / a_.hpu), per_tile(256 / (us / 16) + 1), jobs(j) {
         ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge + pw * kLookup);
-        live = reinterpret_cast<uint8_t *>(ids + 256);
-        job_units = job_at = count = 0;
+        live = reinterpret_cast<uint8_t *>(ids + 128);
+        job_units = job_at = count = units = 0;
         over = false;
         now.units = mid.units = far.units = 0;
     }
     __device__ __forceinline__ uint32_t offset(int s) const { return (uint32_t)s - kv.page.div(s) * kv.page.d; }
-    __device__ __forceinline__ int first_slot(const Group &g, int e) const {   // of the lane's look-up e
-        return g.s + (TMA ? 8 * lane : 32 * e + lane);
+    // Slot and head of the (first) row of the lane's look-up e.
+    __device__ __forceinline__ int slot_of(const Group &g, int e, int &head) const {
+        const int row = TMA ? 8 * lane : 32 * e + lane, u = row / S::kUnit, in = row - u * S::kUnit;
+        head = head_of(in);
+        return g.s + u * kTurn * us + in - head * us;
     }
+    // Which of the unit's heads row `in` belongs to: its tile (below 8) over the tiles of a head.
+    __device__ __forceinline__ int head_of(int in) const { return (in >> 4) * per_tile >> 8; }
+    __device__ __forceinline__ bool is_page(int id) const { return (uint32_t)id < (uint64_t)kv.c.pages; }
     // The next group becomes `now`, its pages and live slots in shared memory.
     __device__ __forceinline__ void step() {
         __syncwarp();
         if (mid.units > 0) {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
+                ids[32 * e + lane] = id_mid[e];
                 if constexpr (TMA) {
-                    uint32_t on = 0;
-                    if (id_mid[0] >= 0) {
-                        on = 0xffu >> max(0, 8 - (mid.end - first_slot(mid, 0)));
-                        if (a.first) {
+                    int head;
+                    uint32_t on = is_page(id_mid[0]) ? 0xffu >> max(0, 8 - (mid.end - slot_of(mid, 0, head))) : 0u;
+                    if (a.first) {
 #pragma unroll
-                            for (int x = 0; x < 8; ++x) on &= ~((uint32_t)(pos_mid[x] < mid.low) << x);
-                        }
+                        for (int x = 0; x < 8; ++x) on &= ~((uint32_t)(pos_mid[x] < mid.low) << x);
                     }
-                    ids[lane] = id_mid[0];
                     live[lane] = (uint8_t)on;
                 } else {
-                    const uint32_t on = __ballot_sync(0xffffffffu, id_mid[e] >= 0 && !(a.first && pos_mid[e] < mid.low));
-                    ids[32 * e + lane] = id_mid[e];
+                    const uint32_t on = __ballot_sync(0xffffffffu, is_page(id_mid[e]) && !(a.first && pos_mid[e] < mid.low));
                     if (lane == 0) reinterpret_cast<uint32_t *>(live)[e] = on;
                 }
             }
@@ -598,8 +603,10 @@ struct Producer {
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             id_mid[e] = id_far[e];
-            if (!a.first || mid.units == 0 || id_mid[e] < 0) continue;
-            const int32_t *p = kv.c.position + kv.mark(id_mid[e], mid.h, offset(first_slot(mid, e)));
+            if (!a.first || mid.units == 0 || !is_page(id_mid[e])) continue;
+            int head;
+            const uint32_t off = offset(slot_of(mid, e, head));
+            const int32_t *p = kv.c.position + kv.mark(id_mid[e], mid.h + head, off);
             if constexpr (TMA) {   // 8 slots of a page whose size is a multiple of 8
                 const int4 x = reinterpret_cast<const int4 *>(p)[0], y = reinterpret_cast<const int4 *>(p)[1];
                 pos_mid[0] = x.x, pos_mid[1] = x.y, pos_mid[2] = x.z, pos_mid[3] = x.w;
@@ -609,39 +616,44 @@ struct Producer {
             }
         }
         far.units = 0;
-        if (job_at >= job_units && !over) {
-            if (!jobs.next(kv, a, S::kUnit, per_seq)) over = true;
+        while (job_at >= job_units && !over) {   // a job may have no unit of this warp's
+            units += job_units;
+            if (!jobs.next(kv, a, us, per_seq)) over = true, job_units = 0;
             // A job without a slot (whole jobs only) is one unit without a live one.
-            else job_units = max(1, jobs.b1 - jobs.b0), job_at = 0;
+            else job_units = max(1, jobs.b1 - jobs.b0);
+            job_at = TMA ? 0 : (pw + units) & (kProducers - 1);
         }
-        if (job_at < job_units) {
-            far.i = jobs.i, far.h = jobs.r / a.hb, far.hb = jobs.r % a.hb, far.end = jobs.last(S::kUnit);
-            far.s = jobs.first(S::kUnit) + job_at * S::kUnit;
-            far.units = min(kUnits, job_units - job_at), far.unit = job_at;
+        if (!over) {
+            far.i = jobs.i, far.h = jobs.r / a.hb * a.hpu, far.hb = jobs.r % a.hb, far.end = jobs.last(us);
+            far.s = jobs.first(us) + job_at * us;
+            far.units = min(kUnits, (job_units - job_at + kTurn - 1) / kTurn);
+            far.unit = job_at, far.of = job_units, far.base = units;
             far.low = a.first ? a.first[jobs.i] : 0;
-            if (job_at == 0 && pw == 0) {   // the queries come from memory by the time the job begins
+            if (job_at == 0 && (!TMA || pw == 0)) {   // the queries come from memory by the time the job begins
                 const int qh = far.h * a.group + far.hb * S::kHeads;
-                const int words = min(S::kHeads, a.group - far.hb * S::kHeads) * kv.c.head_dim;
+                const int words = min(S::kHeads, a.group * a.hpu - far.hb * S::kHeads) * kv.c.head_dim;
                 const float *q = a.q + far.i * a.ldq + (int64_t)qh * kv.c.head_dim;
                 for (int x = 32 * lane; x < words; x += 1024) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + x));
             }
-            job_at += far.units;
-            far.last = job_at == job_units;
-            const int end = min(far.end, far.s + far.units * S::kUnit);
+            job_at += far.units * kTurn;
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
-                const int s = first_slot(far, e);
-                uint32_t off;
-                id_far[e] = s < end ? kv.page_of(far.i, (uint32_t)s, off) : -1;
+                int head;
+                const int row = TMA ? 8 * lane : 32 * e + lane, s = slot_of(far, e, head);
+                id_far[e] = -1;
+                if (row < far.units * S::kUnit && s < far.end)   // checked when it is used, a group later
+                    id_far[e] = kv.c.table[far.i * kv.c.ld_table + kv.page.div((uint32_t)s)];
             }
         }
     }
     // Scores of a unit that nobody multiplies, for the weights.
     __device__ __forceinline__ void no_scores(int s) const {
-        const int rows = min(S::kHeads, a.group - now.hb * S::kHeads), n = min((now.end - s + 15) / 16 * 16, S::kUnit);
-        float *sc = a.scores + (now.i * a.heads + (int64_t)now.h * a.group + now.hb * S::kHeads) * a.score_rows + s;
-        for (int r = 0; r < rows; ++r)
-            for (int x = lane; x < n; x += 32) sc[r * a.score_rows + x] = minus_inf();
+        const int rows = min(S::kHeads, a.group - now.hb * S::kHeads), n = min((now.end - s + 15) / 16 * 16, us);
+        for (int h = 0; h < a.hpu; ++h) {
+            float *sc = a.scores + (now.i * a.heads + (int64_t)(now.h + h) * a.group + now.hb * S::kHeads) * a.score_rows + s;
+            for (int r = 0; r < rows; ++r)
+                for (int x = lane; x < n; x += 32) sc[r * a.score_rows + x] = minus_inf();
+        }
     }
     // All units of the block; false when a bounded wait ran out.
     __device__ __forceinline__ bool run() {
@@ -651,27 +663,29 @@ struct Producer {
                 step();
             }
             for (int u = 0; u < now.units; ++u) {
-                const int s = now.s + u * S::kUnit;
+                const int s = now.s + u * kTurn * us, unit = now.unit + u * kTurn;
                 // Lane k: the live slots of tile k.
                 const uint32_t on = lane < kHalves ? reinterpret_cast<const uint16_t *>(live)[u * kHalves + lane] : 0;
                 const uint32_t any = __ballot_sync(0xffffffffu, on != 0);
-                const bool last = now.last && u + 1 == now.units;
-                if (!any && !last) {
+                const bool last = unit + 1 == now.of;
+                if (TMA && !any && !last) {
                     if (a.scores && pw == 0) no_scores(s);
                     continue;
                 }
+                if (!TMA) count = now.base + unit;
                 const int stage = count % S::kStages;
                 if (count >= S::kStages &&
                     !mbar_wait(pipe.empty + stage, (count / S::kStages - 1) & 1, &pipe.aborted))
                     return false;
                 __syncwarp();
-                if (pw == 0) {
+                if (!TMA || pw == 0) {
                     if (lane < kHalves) pipe.live[stage][lane] = (uint16_t)on;
-                    if (lane == 0) pipe.unit[stage] = (now.unit + u) | (last ? kLastUnit : 0);
+                    if (lane == 0) pipe.unit[stage] = unit | (last ? kLastUnit : 0);
                     __syncwarp();
                 }
                 if constexpr (TMA) {
-                    if (a.box == 8) boxes<8>(u, s, stage);
+                    if (a.box == 0) box_of_all(any != 0, u, s, stage);
+                    else if (a.box == 8) boxes<8>(u, s, stage);
                     else if (a.box == 16) boxes<16>(u, s, stage);
                     else if (a.box == 32) boxes<32>(u, s, stage);
                     else boxes<64>(u, s, stage);
@@ -683,7 +697,23 @@ struct Producer {
             now.units = 0;
         }
     }
-    // Straight code: a lane issues a copy in about 100 cycles, 200 in a loop over boxes.
+    // The unit is one box (us slots of a page, of a.hpu heads).
+    __device__ __forceinline__ void box_of_all(bool any, int u, int s, int stage) {
+        if (lane == 0) {
+            uint64_t *bar = pipe.full + stage;
+            mbar_expect_tx(bar, any ? (uint32_t)(S::kUnit * S::kRow) : 0u);
+            char *to = smem + stage * S::kStage + pw * (S::kStage / 2);
+            const int page = ids[u * S::kUnit / 8];
+            if (any) {
+#pragma unroll
+                for (int k = 0; k < S::kRow / 128; ++k)
+                    tma_load_4d(to + k * 128 * S::kUnit, map, bar, k * 128 / S::kES, (int)offset(s), now.h, page);
+            }
+        }
+        __syncwarp();
+    }
+    // Boxes of one head.  Straight code: a lane issues a copy in about 100
+    // cycles, 200 in a loop over boxes.
     template <int BOX>
     __device__ __forceinline__ void boxes(int u, int s, int stage) {
         if constexpr (S::kUnit % BOX == 0) {
@@ -702,46 +732,51 @@ struct Producer {
 #pragma unroll
                 for (int b = 0; b < N; ++b) page[b] = ids[(u * S::kUnit + b * BOX) / 8];
                 char *to = smem + stage * S::kStage + pw * (S::kStage / 2);
-                int off = (int)offset(s);
+                const int off0 = (int)offset(s);
+                int off = off0, h = now.h, row = 0;
 #pragma unroll
                 for (int b = 0; b < N; ++b) {
                     if (mask >> b & 1u) {
-                        const int c1 = a.token_major ? now.h : off, c2 = a.token_major ? off : now.h;
+                        const int c1 = a.token_major ? h : off, c2 = a.token_major ? off : h;
 #pragma unroll
                         for (int k = 0; k < S::kRow / 128; ++k)
                             tma_load_4d(to + b * BOX * 128 + k * 128 * S::kUnit, map, bar, k * 128 / S::kES, c1, c2,
                                         page[b]);
                     }
-                    off += BOX;
+                    off += BOX, row += BOX;
                     if (off == (int)kv.page.d) off = 0;
+                    if (row == us) off = off0, ++h, row = 0;   // the next head's slots
                 }
             }
             __syncwarp();
         }
     }
     __device__ __forceinline__ void rows(int u, int s, int stage) {
-        constexpr int kMine = S::kUnit / kProducers;
         const char *kp = static_cast<const char *>(kv.c.k), *vp = static_cast<const char *>(kv.c.v);
         const int chunks = kv.c.head_dim * S::kES / 16;
         const uint32_t to = smem_u32(smem + stage * S::kStage);
-        for (int r0 = pw * kMine; r0 < (pw + 1) * kMine; r0 += 16) {
-            const int e = u * S::kUnit + r0 + (lane & 15);
-            const bool on = live[e >> 3] >> (e & 7) & 1u;
-            const int64_t row = on ? kv.element(ids[e], now.h, offset(s + r0 + (lane & 15))) * S::kES : -1;
-            if (!__any_sync(0xffffffffu, on)) continue;
+        for (int r0 = 0; r0 < S::kUnit; r0 += 32) {   // a lane's row: 16 or 32 of a head's
+            const int in = r0 + lane, e = u * S::kUnit + in, head = head_of(in);
+            const bool on = in < S::kUnit && live[e >> 3] >> (e & 7) & 1u;
+            const int64_t row = on ? kv.element(ids[e], now.h + head, offset(s + in - head * us)) * S::kES : -1;
+            const uint32_t any = __ballot_sync(0xffffffffu, on);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (!(any >> (16 * half) & 0xffffu)) continue;   // a tile without a live slot is not read
 #pragma unroll 8
-            for (int x = 0; x < 16 * S::kChunks / 32; ++x) {
-                const int at16 = x * 32 + lane, rr = at16 / S::kChunks, c = at16 % S::kChunks;
-                const int64_t from = __shfl_sync(0xffffffffu, row, rr);
-                const bool ok = from >= 0 && c < chunks;
-                const uint32_t dst = to + chunk_at<128 * S::kUnit>(r0 + rr, c);
-                const int64_t src = ok ? from + c * 16 : 0;
-                copy16(dst, kp + src, ok);
-                copy16(dst + S::kStage / 2, vp + src, ok);
+                for (int x = 0; x < 16 * S::kChunks / 32; ++x) {
+                    const int at16 = x * 32 + lane, rr = 16 * half + at16 / S::kChunks, c = at16 % S::kChunks;
+                    const int64_t from = __shfl_sync(0xffffffffu, row, rr);
+                    const bool ok = from >= 0 && c < chunks;
+                    const uint32_t dst = to + chunk_at<128 * S::kUnit>(r0 + rr, c);
+                    const int64_t src = ok ? from + c * 16 : 0;
+                    copy16(dst, kp + src, ok);
+                    copy16(dst + S::kStage / 2, vp + src, ok);
+                }
             }
         }
         copies_arrive(pipe.full + stage);
-        if (pw == 0 && lane == 0) mbar_arrive(pipe.full + stage);   // with the stage's live slots and unit
+        if (lane == 0) mbar_arrive(pipe.full + stage);   // with the stage's live slots and unit
     }
     // After an abort: nothing in flight may outlive the block.
     __device__ __forceinline__ void drain() {
@@ -760,22 +795,22 @@ __device__ __forceinline__ void consumers_sync() {
 }
 
 template <class T, int DP, int NT, bool TMA>
-__global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers), Shape<T, DP, NT>::kBlocks)
+__global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
+                                  Shape<T, DP, NT>::kBlocks)
     attend_kernel(KvView kv, AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
     using S = Shape<T, DP, NT>;
-    constexpr int W = S::kWarps, THREADS = 32 * W, ALL = THREADS + 32 * kProducers, MS = S::kSlots;
+    constexpr int W = S::kWarps, P = kProducers, THREADS = 32 * W, ALL = THREADS + 32 * P, MS = S::kSlots;
     extern __shared__ __align__(1024) char smem[];
     static_assert(sizeof(Pipe<T, DP, NT>) <= 512, "pipe");
     Pipe<T, DP, NT> &pipe = *reinterpret_cast<Pipe<T, DP, NT> *>(smem + S::kMiscAt);
     float *mo = reinterpret_cast<float *>(smem + S::kRing), *mm = mo + MS * S::kHeads * S::kPitch,
           *ml = mm + MS * S::kHeads;
-    uint32_t *qs = reinterpret_cast<uint32_t *>(smem + S::kQAt);
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int D = kv.c.head_dim, KV = kv.c.kv_heads, per_seq = KV * a.hb;
+    const int D = kv.c.head_dim, per_seq = kv.c.kv_heads / a.hpu * a.hb, us = S::kUnit / a.hpu;
     if (tid == 0) {
         pipe.aborted = 0;
         for (int x = 0; x < S::kStages; ++x) {
-            mbar_init(pipe.full + x, TMA ? kProducers : 32 * kProducers + 1);
+            mbar_init(pipe.full + x, TMA ? P : 32 + 1);
             mbar_init(pipe.empty + x, W);
         }
         mbar_init_fence();
@@ -788,7 +823,7 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers), 
     if (a.whole) {
         jobs.i = blockIdx.x / per_seq, jobs.at = blockIdx.x % per_seq, jobs.left = 1;
     } else {
-        find_place<ALL>(kv, a, S::kUnit, per_seq, blockIdx.x, gridDim.x, total, end, jobs, pipe.place);
+        find_place<ALL>(kv, a, us, per_seq, blockIdx.x, gridDim.x, total, end, jobs, pipe.place);
         // Sequences without a slot belong to nobody's units: their rows are shared out.
         for (int64_t i = blockIdx.x; i < kv.c.seqs; i += gridDim.x)
             if (kv.length(a.lens, i, a.max_len) == 0)
@@ -807,9 +842,12 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers), 
 
     Warp<T, DP, NT> wp;
     int stage = 0, parity = 0;
-    while (jobs.next(kv, a, S::kUnit, per_seq)) {
-        const int s0 = jobs.first(S::kUnit), s1 = jobs.last(S::kUnit);
-        const int h = jobs.r / a.hb, hb = jobs.r % a.hb;
+    // The warp's head of a unit's, and which of the head's tiles of 16 slots.
+    const int of_head = W / a.hpu, hi = w / of_head, sub = w - hi * of_head;
+    uint32_t *qs = reinterpret_cast<uint32_t *>(smem + S::kQAt) + hi * S::kQWords;
+    while (jobs.next(kv, a, us, per_seq)) {
+        const int s0 = jobs.first(us), s1 = jobs.last(us);
+        const int h = jobs.r / a.hb * a.hpu + hi, hb = jobs.r % a.hb;
         const int rows = min(S::kHeads, a.group - hb * S::kHeads);
         const int64_t i = jobs.i, qh = (int64_t)h * a.group + hb * S::kHeads;
         float *scores = a.scores ? a.scores + (i * a.heads + qh) * a.score_rows + s0 : nullptr;
@@ -823,7 +861,7 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers), 
                 break;
             }
             const uint32_t live = pipe.live[stage][w];
-            const int unit = pipe.unit[stage], at = (unit & (kLastUnit - 1)) * S::kUnit + 16 * w;
+            const int unit = pipe.unit[stage], at = (unit & (kLastUnit - 1)) * us + 16 * sub;
             char *k = smem + stage * S::kStage + 16 * w * 128, *v = k + S::kStage / 2;
             float *sc = scores && s0 + at < s1 ? scores + at : nullptr;   // rows of 16 slots exist in whole
             if (live) {
@@ -845,8 +883,8 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers), 
             if (unit & kLastUnit) break;
         }
 
-        // Merge of the warps through shared memory, the uppermost kSlots into
-        // the next ones, and so on; the lowest ones' to whoever writes.
+        // Merge of a head's warps through shared memory, the uppermost into those
+        // before them, and so on.
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -889,35 +927,43 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers), 
                 }
             __syncwarp();
         };
-        for (int top = W; top > 0; top -= MS) {   // a warp takes from and puts into the same slot
-            if (w >= top - MS && w < top) put(w - (top - MS));
+        const int buffers = max(1, MS / a.hpu);   // of a head; a.hpu <= MS where a head has several warps
+        for (int top = of_head; top > 1;) {
+            const int n = min(buffers, top / 2);
+            const int taker = sub + n;   // whose result this warp takes; a warp's later put goes where it took from
+            if (sub >= top - n && sub < top) put(hi * buffers + sub % buffers);
             consumers_sync<THREADS>();
-            if (w >= top - 2 * MS && w < top - MS) take(w - (top - 2 * MS));
+            if (sub >= top - 2 * n && sub < top - n) take(hi * buffers + taker % buffers);
+            top -= n;
         }
         const bool whole = jobs.b0 == 0 && jobs.b1 == jobs.nb;
-        const int64_t slot = 2 * (int64_t)blockIdx.x + (jobs.b0 == 0 ? 1 : 0);
-        for (int x = tid; x < rows * DP; x += THREADS) {
-            const int head = x / DP, d = x % DP;
-            float top = minus_inf(), sum = 0.0f, out = 0.0f;
+        if (sub == 0) {
+            const int64_t part = ((2 * (int64_t)blockIdx.x + (jobs.b0 == 0 ? 1 : 0)) * a.hpu + hi) * S::kHeads;
 #pragma unroll
-            for (int k = 0; k < MS; ++k) top = fmaxf(top, mm[k * S::kHeads + head]);
-            const float ref = top == minus_inf() ? 0.0f : top;
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int k = 0; k < MS; ++k) {
-                const float f = power2(mm[k * S::kHeads + head] - ref);
-                sum = fmaf(f, ml[k * S::kHeads + head], sum);
-                out = fmaf(f, mo[(k * S::kHeads + head) * S::kPitch + d], out);
-            }
-            if (whole) {
-                if (d < D) a.out[i * a.ldo + (qh + head) * D + d] = sum == 0.0f ? 0.0f : out / sum;
-                if (a.scores && d == 0) {
-                    float *st = a.stats + 2 * (i * a.heads + qh + head);
-                    st[0] = ref, st[1] = sum == 0.0f ? 0.0f : 1.0f / sum;
+                for (int j = 0; j < 2; ++j) {
+                    const int head = 8 * n + 2 * t + j;
+                    if (head >= rows) continue;
+                    const float m = wp.m[n][j], sum = wp.l[n][j], inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    if (whole) {
+                        float *out = a.out + i * a.ldo + (qh + head) * D;
+#pragma unroll
+                        for (int x = 0; x < DP / 16; ++x) {
+                            if (16 * x + g < D) out[16 * x + g] = wp.o[n][x][j] * inv;
+                            if (16 * x + g + 8 < D) out[16 * x + g + 8] = wp.o[n][x][2 + j] * inv;
+                        }
+                        if (a.scores && g == 0) {
+                            float *st = a.stats + 2 * (i * a.heads + qh + head);
+                            st[0] = m == minus_inf() ? 0.0f : m, st[1] = inv;
+                        }
+                    } else {
+                        float *out = a.part_o + (part + head) * DP;
+#pragma unroll
+                        for (int x = 0; x < DP / 16; ++x) out[16 * x + g] = wp.o[n][x][j], out[16 * x + g + 8] = wp.o[n][x][2 + j];
+                        if (g == 0) a.part_ml[2 * (part + head)] = m, a.part_ml[2 * (part + head) + 1] = sum;
+                    }
                 }
-            } else {
-                a.part_o[(slot * S::kHeads + head) * DP + d] = out;
-                if (d == 0) a.part_ml[2 * (slot * S::kHeads + head)] = top, a.part_ml[2 * (slot * S::kHeads + head) + 1] = sum;
-            }
         }
         if (!whole && jobs.b0 == 0 && tid == 0) {   // this block's end cuts the job: who has the rest of it?
             // Counted unit u is block c's if total c / blocks <= u < total (c + 1) / blocks (rounded down).
@@ -929,7 +975,7 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers), 
             a.split[3 * blockIdx.x + 1] = c;
             a.split[3 * blockIdx.x + 2] = total;
         }
-        consumers_sync<THREADS>();
+        if (of_head > 1 || !S::kQReg) consumers_sync<THREADS>();   // buffers and queries are free again
     }
 }
 
@@ -951,16 +997,18 @@ int resident() {
 }
 
 // A pool as a tensor of (channel, slot, head, page), or (channel, head, slot,
-// page) where heads are the closer ones; box: 128 bytes of `slots_box` slots.
-// False where the strides do not nest: the lanes copy.
+// page) where heads are the closer ones; box: 128 bytes of `slots_box` slots of
+// `heads_box` heads.  False where the strides do not nest (the lanes copy), or
+// for several heads where heads are the closer ones.
 template <class T>
-bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int slots_box, int *token_major) {
+bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int slots_box, int heads_box, int *token_major) {
     constexpr int kES = sizeof(T);
     const cuuint64_t D = (cuuint64_t)c.head_dim * kES, slots = (cuuint64_t)c.page_size, heads = (cuuint64_t)c.kv_heads;
     cuuint64_t slot = (cuuint64_t)c.slot_stride * kES, head = (cuuint64_t)c.head_stride * kES;
     cuuint64_t page = (cuuint64_t)c.page_stride * kES;
     if (heads == 1) head = slot * slots;
     const bool tm = head < slot;
+    if (tm && heads_box > 1) return false;
     const cuuint64_t inner = tm ? head : slot, outer = tm ? slot : head;
     if (c.pages == 1) page = outer * (tm ? slots : heads);
     const cuuint64_t most = (cuuint64_t)1 << 40;
@@ -969,7 +1017,7 @@ bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int slots_
     if (!fn) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, tm ? heads : slots, tm ? slots : heads, (cuuint64_t)c.pages};
     const cuuint64_t strides[3] = {inner, outer, page};
-    const cuuint32_t box[4] = {128 / kES, tm ? 1u : (cuuint32_t)slots_box, tm ? (cuuint32_t)slots_box : 1u, 1}, each[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {128 / kES, tm ? 1u : (cuuint32_t)slots_box, tm ? (cuuint32_t)slots_box : (cuuint32_t)heads_box, 1}, each[4] = {1, 1, 1, 1};
     const CUtensorMapDataType type = kES == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                      : kTerms<T> == 3 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     *token_major = tm;
@@ -980,7 +1028,10 @@ bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int slots_
 template <class T, int DP, int NT>
 struct Instance {
     using S = Shape<T, DP, NT>;
-    static AttendShape shape() { return {S::kHeads, DP, S::kUnit}; }
+    // Heads share a unit if there is room for their queries, and a merge buffer or a warp for each.
+    static AttendShape shape() {
+        return {S::kHeads, DP, S::kUnit, S::kQReg ? S::kWarps : S::kQHeads, S::kSlots, S::kBlocks};
+    }
     template <bool TMA>
     static mosaic_status go(const KvView &kv, AttendArgs a, const CUtensorMap &mk, const CUtensorMap &mv,
                             int &blocks, cudaStream_t st) {
@@ -1000,13 +1051,19 @@ struct Instance {
     static mosaic_status launch(const mosaic_kv_cache &c, AttendArgs a, int &blocks, cudaStream_t st) {
         const KvView kv(c);
         alignas(64) CUtensorMap mk = {}, mv = {};
-        // A box is as many slots as divide a page and a unit, 8 at least (a swizzle's rows).
-        for (a.box = 64; a.box >= 8 && (S::kUnit % a.box || c.page_size % a.box); a.box /= 2) {
+        // Positions are read 8 at a time.
+        if (c.page_size % 8 == 0 && (!a.first || aligned16(c.position))) {
+            const int us = S::kUnit / a.hpu;
+            a.box = 0;   // a unit is one box
+            if (us <= 64 && c.page_size % us == 0 && pool_map<T>(&mk, c, c.k, us, a.hpu, &a.token_major) &&
+                pool_map<T>(&mv, c, c.v, us, a.hpu, &a.token_major) && (a.hpu > 1 || !a.token_major))
+                return go<true>(kv, a, mk, mv, blocks, st);
+            // As many slots of a head as divide a page and a unit, 8 at least (a swizzle's rows).
+            for (a.box = 64; us % a.box || c.page_size % a.box; a.box /= 2) {
+            }
+            if (pool_map<T>(&mk, c, c.k, a.box, 1, &a.token_major) && pool_map<T>(&mv, c, c.v, a.box, 1, &a.token_major))
+                return go<true>(kv, a, mk, mv, blocks, st);
         }
-        // Positions are then read 8 at a time.
-        if (a.box >= 8 && (!a.first || aligned16(c.position)) && pool_map<T>(&mk, c, c.k, a.box, &a.token_major) &&
-            pool_map<T>(&mv, c, c.v, a.box, &a.token_major))
-            return go<true>(kv, a, mk, mv, blocks, st);
         return go<false>(kv, a, mk, mv, blocks, st);
     }
 };
