@@ -2,7 +2,6 @@
 // point, the join of jobs that blocks share, and the gathered weights.  The
 // kernel that reads the cache is in kv_attention_impl.cuh.
 #include <math.h>
-#include <stdlib.h>
 
 #include "kv_attention.cuh"
 
@@ -10,15 +9,25 @@ namespace mosaic {
 namespace {
 
 constexpr int kMaxGroup = 64;
-// Up to here every job is one block's: nothing to join, one launch fewer.
-constexpr int64_t kWholeLen = 512;
+// Up to these lengths every job is one block's: nothing to join, and blocks
+// beyond a wave follow as others end.  Microseconds, whole jobs / shared, 8
+// key/value heads of 128, bf16 (one sequence, then 16, 32, 64 of equal and 64
+// of spread lengths): 256 slots 8 / 12, 9 / 15, 11 / 19, 17 / 25, 14 / 21; 512:
+// 12 / 13, 13 / 18, 17 / 24, 27 / 36, 23 / 26; 1024: 20 / 15, 22 / 24, 27 / 35,
+// 47 / 56, 40 / 36; 2048: 35 / 19, 38 / 34, 47 / 55, 85 / 95, 67 / 57.
+constexpr int64_t kWholeFew = 512, kWholeMany = 1024, kManyJobs = 128;
+// Heads share a unit (the blocks' warps then have a head each and nothing to
+// merge) while so many jobs remain to be shared out; whole jobs while there is
+// more than a wave of them.  Shared jobs with 1 / 2 / 4 heads a unit, up to 1024
+// slots: one sequence 14 / 19 / 27, 16: 20 / 20 / 22, 32: 29 / 26 / 25, 64: 42 /
+// 38 / 36, 256: 117 / 106 / 102.
+constexpr int64_t kFewestJobs = 64;
 // What a job costs beside its slots, as bytes of cache read in that time.  48
 // sequences of 41 to 2000 slots on 32 heads of 128: 266 us at 0, 231 at 32 KB,
-// 140 at 128 KB, 135 at 192 KB, 139 at 256 KB, 153 at 512 KB; 64 of 256 to 16384
-// on 8 heads: 418, 410, 381, 371, 368, 372; 400 of 3 to 1500 on 8 heads of 64,
-// windowed: 147, 122, 95, 93, 90 (256 KB).
+// 140 at 128 KB, 135 at 192 KB, 139 at 256 KB, 153 at 512 KB; 400 of 3 to 1500
+// on 8 heads of 64, windowed: 147, 122, 95, 93, 90 (256 KB).  With four heads a
+// unit 64 KB to 384 KB are within 4 and 12 per cent.
 constexpr int64_t kJobBytes = 256 * 1024;
-constexpr int64_t kJobs = 64;
 
 // Block (c, y): the job that block c's end cuts.  Where jobs have many parts
 // (`shared`), query head y of it, its parts taken in turn by eight warps; else
@@ -32,9 +41,9 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendSh
     const int64_t job = a.split[3 * c], last = a.split[3 * c + 1], total = a.split[3 * c + 2];
     if (job < 0) return;
     const int hi = shared ? blockIdx.y / s.heads : blockIdx.y, from = shared ? w : 0, each = shared ? 8 : 1;
-    const int per_seq = a.heads / a.group / a.hpu * a.hb, r = (int)(job % per_seq);
-    const int h = r / a.hb * a.hpu + hi, hb = r % a.hb;
-    const int64_t i = job / per_seq;
+    const uint32_t per_seq = a.heads / a.group / a.hpu * a.hb, at = (uint32_t)job / per_seq;   // jobs: below 2^31
+    const int r = (int)((uint32_t)job - at * per_seq), h = r / a.hb * a.hpu + hi, hb = r % a.hb;
+    const int64_t i = at;
     // Part k of the job: the cut block's second slot, then the first slots of
     // the blocks after it (some without a unit where units are fewer than blocks).
     const int parts = (int)(last - c) + 1;
@@ -208,7 +217,7 @@ AttendShape shape_of(const mosaic_kv_cache &c, int64_t heads) {
 int64_t most_blocks(const mosaic_kv_cache &c, const AttendShape &s, int64_t heads, int64_t max_len) {
     const int64_t group = heads / c.kv_heads, hb = (group + s.heads - 1) / s.heads;
     const int64_t units = c.seqs * c.kv_heads * hb * ((max_len + s.unit - 1) / s.unit);
-    return max_len <= (getenv("WL") ? atoi(getenv("WL")) : kWholeLen * (c.seqs * c.kv_heads * hb >= 128 ? 2 : 1)) ? 0 : units < kAttendWave ? units : kAttendWave;
+    return max_len <= (c.seqs * c.kv_heads * hb >= kManyJobs ? kWholeMany : kWholeFew) ? 0 : units < kAttendWave ? units : kAttendWave;
 }
 mosaic_status check(const mosaic_kv_cache *c, int64_t heads, int64_t max_len) {
     MOSAIC_TRY(kv_check(c));
@@ -264,9 +273,8 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     a.whole = cap == 0;
     for (int x = 2; x <= s.most_heads; ++x) {
         if (s.most_heads % x || cache->kv_heads % x || (x > s.buffers && x != s.most_heads)) continue;
-        if (a.whole ? one / a.hpu > 152 * s.resident : one / x >= kJobs) a.hpu = x;
+        if (a.whole ? one / a.hpu > 152 * s.resident : one / x >= kFewestJobs) a.hpu = x;
     }
-    if (getenv("HPU")) { a.hpu = 1; for (int x = atoi(getenv("HPU")); x > 1; x /= 2) if (s.most_heads % x == 0 && cache->kv_heads % x == 0 && (x <= s.buffers || x == s.most_heads)) { a.hpu = x; break; }}
     a.scale2 = scale * 1.44269504088896341f, a.decay = decay, a.out = out, a.ldo = ldo;
     char *w = static_cast<char *>(ws);
     a.part_ml = reinterpret_cast<float *>(w), w += p.ml;
@@ -280,7 +288,7 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     const int64_t jobs = cache->seqs * (cache->kv_heads / a.hpu) * a.hb;
     a.blocks = (int)(a.whole ? jobs : cap);
     const int64_t unit_bytes = 2 * s.unit * D * kv_element_bytes(cache->type);
-    a.job_cost = (int)(((getenv("JCB") ? atoi(getenv("JCB")) * 1024 : kJobBytes) + unit_bytes / 2) / unit_bytes);
+    a.job_cost = (int)((kJobBytes + unit_bytes / 2) / unit_bytes);
     cudaStream_t st = as_stream(stream);
     MOSAIC_TRY(by_type(cache->type, [&](auto t) { return attend_launch<decltype(t)>(*cache, a, a.blocks, st); }));
     if (!a.whole) {

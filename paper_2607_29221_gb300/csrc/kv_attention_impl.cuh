@@ -119,16 +119,17 @@ struct Shape {
     // A stage holds a unit: K and V of kUnit rows, 16 a consumer warp (slots of
     // a.hpu heads).  8 consumer warps an SM, as two blocks or (with twice the outputs and queries) one;
     // fewer where rows are long.
-    static constexpr int kWarps = kRow == 1024 ? 2 : NT == 2 && kRow <= 256 ? 8 : kRow == 512 && kES == 4 && NT == 1 ? 6 : 4;
+    static constexpr int kWarps = kRow == 1024 ? 2 : NT == 2 && kRow <= 256 ? 8 : 4;
     static constexpr int kUnit = 16 * kWarps, kStage = 2 * kUnit * kRow;
-    static constexpr int kStages = kRow == 128 ? 4 : (NT == 2 && DP == 256) || kWarps == 6 ? 2 : 3;
+    static constexpr int kStages = kRow == 128 ? 4 : (NT == 2 && DP == 256) ? 2 : 3;
     static constexpr int kSlots = kWarps == 2 || (NT == 2 && kRow >= 512) ? 1 : 2;   // warps' results at a time
     static constexpr int kK = kES == 4 ? 8 : 16, kSteps = DP / kK;    // channels of a product step
     static constexpr int kHeads = 8 * NT, kPitch = DP + 4;
     static constexpr int kQWords = kSteps * NT * kTerms<T> * 2 * 32;  // query fragments
     // Queries stay in registers where they fit beside the outputs.
-    static constexpr bool kQReg = kSteps * NT * kTerms<T> * 2 <= 48;
-    static constexpr int kQHeads = kQReg ? 0 : kWarps == 6 ? 2 : 1;   // else in shared memory, of so many heads
+    static constexpr int kQRegs = kSteps * NT * kTerms<T> * 2;
+    static constexpr bool kQReg = kQRegs <= 48 || (kQRegs <= 64 && NT == 1 && kRow == 512);
+    static constexpr int kQHeads = kQReg ? 0 : 1;   // else in shared memory, of one head
     // Shared memory: the ring, the results of some warps, page ids and live
     // slots of the producers' groups, the queries' fragments, barriers and so on.
     static constexpr int kRing = kStages * kStage;
