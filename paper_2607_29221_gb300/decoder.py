@@ -8,7 +8,7 @@ the paper keeps them on the client (attention is local, Sec. 3.2 "Local
 attention computation"): RMSNorm and SiLU(gate) * up (one-pass kernels of this
 library), causal grouped-query attention with a softmax (torch's fused
 scaled-dot-product attention in fp32, causal), and the residual adds.  Rotary position embeddings are not described by
-the paper and are left out.
+the paper; the layer's own pass leaves them out, and ``session.DecodeSession`` (cached decoding) has them.
 
 Weights are seeded random N(0, 0.02) (the paper's checkpoints are not
 available); RMSNorm weights are 1.
@@ -155,8 +155,10 @@ class SecureDecoderLayer:
         mark("glue")
         return Y
 
-    def forward(self, x: torch.Tensor, masks=None, mark=None, compose=None) -> torch.Tensor:
-        """One pass over l tokens (x: l x hidden fp32).  `mark(part)`, if given,
+    def forward(self, x: torch.Tensor, masks=None, mark=None, compose=None, attend=None) -> torch.Tensor:
+        """One pass over l tokens (x: l x hidden fp32).  `attend(qkv)`, if
+        given, takes the place of the causal attention over the pass's own
+        tokens (e.g. attention over a cache).  `mark(part)`, if given,
         is called where each part of the pass begins (init_x, encode, server,
         unmask, glue), e.g. to record CUDA events.  With `compose`, call i's
         Init X composition runs (compose(i)) right before its encode."""
@@ -167,7 +169,8 @@ class SecureDecoderLayer:
             masks = self.init_x(x.shape[0])
         mark("glue")
         h = rmsnorm(x, s.eps)
-        a = attention(self._linear(0, h, masks[0], mark, compose), s)
+        qkv = self._linear(0, h, masks[0], mark, compose)
+        a = attention(qkv, s) if attend is None else attend(qkv)
         x = x + self._linear(1, a, masks[1], mark, compose)
         gu = self._linear(2, rmsnorm(x, s.eps), masks[2], mark, compose)
         act = swiglu(gu, s.ffn)

@@ -117,6 +117,12 @@ class PagedCache:
             n = self._ws[key] = size(self._ref, *args)
         return n
 
+    def read(self, seq: int, n: int):
+        """Keys and values of the first n slots of a sequence, kv_heads x n x head_dim in the cache's type (a copy)."""
+        page = self.k.shape[2]
+        ids = self.table[seq, : -(-n // page)].long()
+        return tuple(x[ids].transpose(0, 1).reshape(self.kv_heads, -1, self.head_dim)[:, :n] for x in (self.k, self.v))
+
     def append(self, qkv, heads: int, seq, slot, index=None, rope: Rope | None = None, pos=None, out=None):
         """Rotates row t of qkv (l x (heads + 2 kv_heads) head_dim fp32) and
         stores its keys and values in slot[t] of sequence seq[t] (a negative
