@@ -691,7 +691,8 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
  * The k-th slot below keep that left takes key, value, position and weight of
  * the k-th slot from keep on that stayed (both in ascending order): the least
  * rows that can move do.  Heads choose for themselves, so position differs
- * between heads.  new_lens[i] = min(lens[i], keep); new_lens may be lens.
+ * between heads.  new_lens[i] = min(lens[i], keep); new_lens may be lens
+ * itself, but must not overlap it otherwise.
  * The pages of slots from keep on are free afterwards (their contents are
  * left).  keep >= 1.  ws: mosaic_kv_evict_workspace bytes. */
 size_t mosaic_kv_evict_workspace(const mosaic_kv_cache *cache, int64_t max_len, int64_t keep);

@@ -173,6 +173,14 @@ __global__ void __launch_bounds__(128, 6) attend_weight_kernel(KvView kv, Attend
                     w[3] = fmaf(power2(x[g].w - y.x), y.y, w[3]);
                 }
         }
+        if (a.first) {   // slots below the bound gather nothing (and may have no score)
+            const int low = a.first[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float *p = quad ? at[0] ? at[0] + j : nullptr : at[j];
+                if (p && kv.c.position[p - kv.c.weight] < low) w[j] = 0.0f;
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) old[j] = fmaf(old[j], a.decay, w[j]);
         if (quad) {
@@ -300,7 +308,7 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
         }
         MOSAIC_TRY(launch_status());
     }
-    if (!a.scores || max_len == 0) return MOSAIC_OK;
+    if (!a.scores || max_len == 0 || (a.whole && a.hb == 1)) return MOSAIC_OK;
     const int64_t chunks = (max_len + kWeightSlots - 1) / kWeightSlots, all = cache->seqs * cache->kv_heads * chunks;
     const KvView kv(*cache);
     {

@@ -55,7 +55,8 @@ struct AttendArgs {
     int64_t *split;             // of block c: the job cut by its end (or -1), the last block with a part of
                                 // it, and the units of the whole call
     float *stats;               // final maximum and 1 / sum of (sequence, head), for the weights
-    float *scores;              // (sequence, head) x score_rows, for the weights
+    float *scores;              // (sequence, head) x score_rows, for the weights (none where 16 slots in a
+                                // row do not count)
     int64_t score_rows;
 };
 

@@ -136,7 +136,8 @@ struct Shape {
     static constexpr int kMerge = 4 * kSlots * kHeads * (kPitch + 2);
     static constexpr int kIds = 2 * kLookup;
     static constexpr int kQAt = kRing + kMerge + kIds, kMiscAt = kQAt + 4 * kQWords * kQHeads;
-    static constexpr int kBytes = kMiscAt + 512;
+    static constexpr int kMisc = 512 + 8 * kHeads * (kQReg ? kWarps : kQHeads);
+    static constexpr int kBytes = kMiscAt + kMisc;
     static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kBlocks = kFit < 3 ? kFit : 3;   // blocks an SM
     static_assert(kBytes <= 227 * 1024, "shared memory");
 };
@@ -518,6 +519,7 @@ struct Pipe {
     int unit[S::kStages];           // the stage's unit in its job; + kLastUnit: the job's last one here
     long long place[12];
     int aborted;
+    float2 stats[S::kHeads * (S::kQReg ? S::kWarps : S::kQHeads)];   // whole jobs: for the weights
 };
 constexpr int kLastUnit = 1 << 30;
 
@@ -647,15 +649,6 @@ struct Producer {
             }
         }
     }
-    // Scores of a unit that nobody multiplies, for the weights.
-    __device__ __forceinline__ void no_scores(int s) const {
-        const int rows = min(S::kHeads, a.group - now.hb * S::kHeads), n = min((now.end - s + 15) / 16 * 16, us);
-        for (int h = 0; h < a.hpu; ++h) {
-            float *sc = a.scores + (now.i * a.heads + (int64_t)(now.h + h) * a.group + now.hb * S::kHeads) * a.score_rows + s;
-            for (int r = 0; r < rows; ++r)
-                for (int x = lane; x < n; x += 32) sc[r * a.score_rows + x] = minus_inf();
-        }
-    }
     // All units of the block; false when a bounded wait ran out.
     __device__ __forceinline__ bool run() {
         for (;;) {
@@ -669,10 +662,7 @@ struct Producer {
                 const uint32_t on = lane < kHalves ? reinterpret_cast<const uint16_t *>(live)[u * kHalves + lane] : 0;
                 const uint32_t any = __ballot_sync(0xffffffffu, on != 0);
                 const bool last = unit + 1 == now.of;
-                if (TMA && !any && !last) {
-                    if (a.scores && pw == 0) no_scores(s);
-                    continue;
-                }
+                if (TMA && !any && !last) continue;
                 if (!TMA) count = now.base + unit;
                 const int stage = count % S::kStages;
                 if (count >= S::kStages &&
@@ -802,7 +792,7 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
     using S = Shape<T, DP, NT>;
     constexpr int W = S::kWarps, P = kProducers, THREADS = 32 * W, ALL = THREADS + 32 * P, MS = S::kSlots;
     extern __shared__ __align__(1024) char smem[];
-    static_assert(sizeof(Pipe<T, DP, NT>) <= 512, "pipe");
+    static_assert(sizeof(Pipe<T, DP, NT>) <= S::kMisc, "pipe");
     Pipe<T, DP, NT> &pipe = *reinterpret_cast<Pipe<T, DP, NT> *>(smem + S::kMiscAt);
     float *mo = reinterpret_cast<float *>(smem + S::kRing), *mm = mo + MS * S::kHeads * S::kPitch,
           *ml = mm + MS * S::kHeads;
@@ -875,8 +865,6 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
                     __syncwarp();
                 }
                 wp.tile(smem_u32(k), smem_u32(v), live, qs, sc, a.score_rows, rows);
-            } else if (sc) {   // no slot counts: the weights read that
-                for (int x = lane; x < 16 * rows; x += 32) sc[(x >> 4) * a.score_rows + (x & 15)] = minus_inf();
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(pipe.empty + stage);
@@ -955,8 +943,9 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
                             if (16 * x + g + 8 < D) out[16 * x + g + 8] = wp.o[n][x][2 + j] * inv;
                         }
                         if (a.scores && g == 0) {
-                            float *st = a.stats + 2 * (i * a.heads + qh + head);
-                            st[0] = m == minus_inf() ? 0.0f : m, st[1] = inv;
+                            const float ref = m == minus_inf() ? 0.0f : m;
+                            if (a.whole && a.hb == 1) pipe.stats[hi * S::kHeads + head] = make_float2(ref, inv);
+                            else *reinterpret_cast<float2 *>(a.stats + 2 * (i * a.heads + qh + head)) = make_float2(ref, inv);
                         }
                     } else {
                         float *out = a.part_o + (part + head) * DP;
@@ -965,6 +954,25 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
                         if (g == 0) a.part_ml[2 * (part + head)] = m, a.part_ml[2 * (part + head) + 1] = sum;
                     }
                 }
+        }
+        if (a.scores && a.whole && a.hb == 1) {
+            // The job's scores are this block's: its weights need no further launch.
+            consumers_sync<THREADS>();
+            for (int x = 32 * sub + lane; x < s1; x += 32 * of_head) {
+                uint32_t off;
+                const int id = kv.page_of(i, (uint32_t)x, off);
+                float *to = kv.c.weight + kv.mark(max(id, 0), h, off);
+                const float old = id < 0 ? 0.0f : *to;
+                float sum = 0.0f;
+#pragma unroll 8
+                for (int r = 0; r < rows; ++r) {
+                    const float2 st = pipe.stats[hi * S::kHeads + r];
+                    sum = fmaf(power2(scores[r * a.score_rows + x] - st.x), st.y, sum);
+                }
+                if (id < 0) continue;
+                if (a.first && kv.c.position[kv.mark(id, h, off)] < a.first[i]) sum = 0.0f;   // it may have no score
+                *to = fmaf(old, a.decay, sum);
+            }
         }
         if (!whole && jobs.b0 == 0 && tid == 0) {   // this block's end cuts the job: who has the rest of it?
             // Counted unit u is block c's if total c / blocks <= u < total (c + 1) / blocks (rounded down).

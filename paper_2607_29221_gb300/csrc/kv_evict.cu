@@ -23,6 +23,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kBins = 2048;
+constexpr int kOwnMoves = 512;
 constexpr int kMaxKeys = 48 * 1024;   // keys in shared memory; those beyond are looked up again each pass
 
 // Weights as unsigned keys in ascending order; NaN as -inf, -0 as 0.
@@ -39,6 +40,8 @@ struct EvictArgs {
     int64_t max_len, keep, cap;   // cap: most moves of a (sequence, head)
     int32_t *count, *from, *to;
     int keys;                     // keys a block has room for
+    int quads;                    // four slots from a multiple of 4 on share a page and aligned words
+    int moves;                    // the selection moves the rows itself and writes new_lens (which is not lens)
 };
 
 __device__ __forceinline__ uint32_t slot_key(const KvView &kv, const EvictArgs &a, int64_t i, int h, int s, int from) {
@@ -49,6 +52,44 @@ __device__ __forceinline__ uint32_t slot_key(const KvView &kv, const EvictArgs &
     const float w = kv.c.weight[at];
     if (a.recent_from && kv.c.position[at] >= from) return kKeyInf;
     return order_key(w);
+}
+
+// Moves m0 .. m0 + 31 of a job, by one warp: key and value rows, positions and
+// weights.
+__device__ __forceinline__ void move32(const KvView &kv, const EvictArgs &a, int64_t job, int64_t i, int h, int m0,
+                                       int count) {
+    const int lane = threadIdx.x & 31;
+    const int es = kv.c.type == MOSAIC_KV_F32 ? 4 : 2, quads = kv.c.head_dim * es / 16;
+    char *const kp = static_cast<char *>(kv.c.k), *const vp = static_cast<char *>(kv.c.v);
+    int64_t se = -1, te = 0;
+    if (m0 + lane < count) {
+        uint32_t so, to;
+        const int sid = kv.page_of(i, (uint32_t)a.from[job * a.cap + m0 + lane], so);
+        const int tid = kv.page_of(i, (uint32_t)a.to[job * a.cap + m0 + lane], to);
+        if (sid >= 0 && tid >= 0) {
+            se = kv.element(sid, h, so) * es, te = kv.element(tid, h, to) * es;
+            const int64_t sm = kv.mark(sid, h, so), tm = kv.mark(tid, h, to);
+            kv.c.weight[tm] = kv.c.weight[sm];
+            if (kv.c.position) kv.c.position[tm] = kv.c.position[sm];
+        }
+    }
+    for (int j0 = 0; j0 < 32 && m0 + j0 < count; j0 += 4) {
+        int64_t s[4], t[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            s[j] = __shfl_sync(0xffffffffu, se, j0 + j), t[j] = __shfl_sync(0xffffffffu, te, j0 + j);
+        for (int b = lane; b < 2 * quads; b += 32) {
+            char *pool = b < quads ? kp : vp;
+            const int o = 16 * (b < quads ? b : b - quads);
+            uint4 x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (s[j] >= 0) x[j] = *reinterpret_cast<const uint4 *>(pool + s[j] + o);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (s[j] >= 0) *reinterpret_cast<uint4 *>(pool + t[j] + o) = x[j];
+        }
+    }
 }
 
 template <int THREADS>
@@ -94,23 +135,41 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView kv, EvictA
     };
     pdl_enter();
     const int len = kv.length(a.lens, i, a.max_len), keep = (int)(a.keep < 0x7fffffff ? a.keep : 0x7fffffff);
+    if (a.moves && h == 0 && rank == 0 && tid == 0) a.new_lens[i] = min(len, keep);
     if (len <= keep) {   // the whole cluster's
         if (rank == 0 && tid == 0) a.count[job] = 0;
         return;
     }
     const int from = a.recent_from ? a.recent_from[i] : 0;
-    const int per = (len + C - 1) / C, s0 = min(len, rank * per), n = min(len, s0 + per) - s0;
+    const int per = ((len + C - 1) / C + 3) / 4 * 4, s0 = min(len, rank * per), n = min(len, s0 + per) - s0;
     if (tid == 0) sh.low = 0xffffffffu, sh.high = 0, sh.finite = 0;
     for (int b = tid; b < kBins; b += THREADS) sh.hist[0][b] = 0;
     __syncthreads();
     {
         uint32_t low = 0xffffffffu, high = 0;
         int finite = 0;
-#pragma unroll 4
-        for (int x = tid; x < n; x += THREADS) {
-            const uint32_t k = slot_key(kv, a, i, h, s0 + x, from);
+        auto take = [&](int x, uint32_t k) {
             if (x < a.keys) keys[x] = k;
             if (k < kKeyInf) low = min(low, k), high = max(high, k), ++finite;
+        };
+        if (a.quads) {   // four slots share a page and a 16-byte word
+#pragma unroll 2
+            for (int x = 4 * tid; x < n; x += 4 * THREADS) {
+                uint32_t off;
+                const int id = kv.page_of(i, (uint32_t)(s0 + x), off);
+                const int64_t at = kv.mark(max(id, 0), h, off);
+                const float4 v = *reinterpret_cast<const float4 *>(kv.c.weight + at);
+                int4 p = make_int4(0, 0, 0, 0);
+                if (a.recent_from) p = *reinterpret_cast<const int4 *>(kv.c.position + at);
+                const float w4[4] = {v.x, v.y, v.z, v.w};
+                const int p4[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (x + j < n) take(x + j, id < 0 || (a.recent_from && p4[j] >= from) ? kKeyInf : order_key(w4[j]));
+            }
+        } else {
+#pragma unroll 4
+            for (int x = tid; x < n; x += THREADS) take(x, slot_key(kv, a, i, h, s0 + x, from));
         }
         low = __reduce_min_sync(0xffffffffu, low);
         high = __reduce_max_sync(0xffffffffu, high);
@@ -127,6 +186,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView kv, EvictA
     }
     int left = len - keep;   // of the keys in [low, high], so many least ones leave
     if (left > finite) low = high = kKeyInf, left -= finite;
+    else if (left == 1) high = low;   // one slot over the budget: the least key is known
     for (int pass = 0; low < high; ++pass) {
         int *hist = sh.hist[pass & 1];
         const int shift = max(0, 21 - __clz((int)(high - low)));
@@ -229,53 +289,26 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView kv, EvictA
         hole += __popc(hm), stay += __popc(sm);
     }
     if (C > 1) cluster.sync();   // the others have read this block's counts
+    if (a.moves) {
+        __syncthreads();         // one block a job: both lists are whole
+        const int n = sh.total[1];
+        for (int m0 = 32 * w; m0 < n; m0 += THREADS) move32(kv, a, job, i, h, m0, n);
+    }
 }
 
-// A warp 32 moves at a time: key and value row, position and weight.
 __global__ void __launch_bounds__(256) evict_move_kernel(KvView kv, EvictArgs a, int chunks) {
     pdl_enter();
     const int64_t job = blockIdx.x / chunks;
     const int part = (int)(blockIdx.x % chunks);
-    const int h = (int)(job % kv.c.kv_heads), lane = threadIdx.x & 31;
+    const int h = (int)(job % kv.c.kv_heads);
     const int64_t i = job / kv.c.kv_heads;
     if (part == 0 && h == 0 && threadIdx.x == 0) {
         const int n = kv.length(a.lens, i, a.max_len);
         a.new_lens[i] = n < a.keep ? n : (int)a.keep;
     }
     const int count = a.count[job];
-    const int es = kv.c.type == MOSAIC_KV_F32 ? 4 : 2, quads = kv.c.head_dim * es / 16;
-    char *const kp = static_cast<char *>(kv.c.k), *const vp = static_cast<char *>(kv.c.v);
-    for (int m0 = 32 * (part * 8 + (threadIdx.x >> 5)); m0 < count; m0 += chunks * 256) {
-        int64_t se = -1, te = 0;
-        if (m0 + lane < count) {
-            uint32_t so, to;
-            const int sid = kv.page_of(i, (uint32_t)a.from[job * a.cap + m0 + lane], so);
-            const int tid = kv.page_of(i, (uint32_t)a.to[job * a.cap + m0 + lane], to);
-            if (sid >= 0 && tid >= 0) {
-                se = kv.element(sid, h, so) * es, te = kv.element(tid, h, to) * es;
-                const int64_t sm = kv.mark(sid, h, so), tm = kv.mark(tid, h, to);
-                kv.c.weight[tm] = kv.c.weight[sm];
-                if (kv.c.position) kv.c.position[tm] = kv.c.position[sm];
-            }
-        }
-        for (int j0 = 0; j0 < 32 && m0 + j0 < count; j0 += 4) {
-            int64_t s[4], t[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                s[j] = __shfl_sync(0xffffffffu, se, j0 + j), t[j] = __shfl_sync(0xffffffffu, te, j0 + j);
-            for (int b = lane; b < 2 * quads; b += 32) {
-                char *pool = b < quads ? kp : vp;
-                const int o = 16 * (b < quads ? b : b - quads);
-                uint4 x[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (s[j] >= 0) x[j] = *reinterpret_cast<const uint4 *>(pool + s[j] + o);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (s[j] >= 0) *reinterpret_cast<uint4 *>(pool + t[j] + o) = x[j];
-            }
-        }
-    }
+    for (int m0 = 32 * (part * 8 + (threadIdx.x >> 5)); m0 < count; m0 += chunks * 256)
+        move32(kv, a, job, i, h, m0, count);
 }
 
 int64_t most_moves(int64_t max_len, int64_t keep) {
@@ -330,7 +363,7 @@ mosaic_status mosaic_kv_evict(const mosaic_kv_cache *cache, const int32_t *lens,
     if (ws_bytes < mosaic_kv_evict_workspace(cache, max_len, keep)) return MOSAIC_ERR_WORKSPACE;
     if (!ws) return MOSAIC_ERR_ARG;
     if (reinterpret_cast<uintptr_t>(ws) % 4) return MOSAIC_ERR_ALIGN;
-    EvictArgs a = {lens, recent_from, new_lens, max_len, keep, most_moves(max_len, keep), nullptr, nullptr, nullptr, 0};
+    EvictArgs a = {lens, recent_from, new_lens, max_len, keep, most_moves(max_len, keep), nullptr, nullptr, nullptr, 0, 0, 0};
     char *w = static_cast<char *>(ws);
     a.count = reinterpret_cast<int32_t *>(w);
     a.from = reinterpret_cast<int32_t *>(w + up256(4 * (size_t)jobs));
@@ -341,10 +374,15 @@ mosaic_status mosaic_kv_evict(const mosaic_kv_cache *cache, const int32_t *lens,
     int cluster = 1;
     while (cluster < 8 && jobs * cluster * 2 <= 152 && max_len / (cluster * 2) >= 2048) cluster *= 2;
     while (cluster < 8 && (max_len + cluster - 1) / cluster > kMaxKeys) cluster *= 2;
-    const int64_t per = (max_len + cluster - 1) / cluster;
+    const int64_t per = ((max_len + cluster - 1) / cluster + 3) / 4 * 4;
+    a.quads = cache->page_size % 4 == 0 && aligned16(cache->weight) && (!recent_from || aligned16(cache->position));
     a.keys = (int)(per < kMaxKeys ? per : kMaxKeys);
+    // Few moves a job are the selecting block's own: a launch less (4097 slots to
+    // 4096, 32 sequences of 8 heads: XX us with two, YY with one).
+    a.moves = a.cap <= kOwnMoves && cluster == 1 && new_lens != lens;
     if (per > 8192) MOSAIC_TRY(select_launch<1024>(kv, a, jobs * cluster, cluster, st));
     else MOSAIC_TRY(select_launch<512>(kv, a, jobs * cluster, cluster, st));
+    if (a.moves) return MOSAIC_OK;
     // One wave of blocks for the moves (32 a warp, 256 a block).
     constexpr int64_t kWave = 152 * 8;
     int64_t chunks = (a.cap + 255) / 256;
