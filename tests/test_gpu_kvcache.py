@@ -383,6 +383,10 @@ def evict_reference(weight, position, n, keep, start):
     ([4096, 4097, 4098], 2, 8, 128, 4096, 0, "head", "equal"),
     ([40000, 9000], 1, 16, 64, 8200, 64, "head", "random"),
     ([70001], 2, 8, 16, 35000, 1000, "head", "ties"),
+    ([420001], 1, 8, 64, 200000, 1000, "head", "ties"),             # more slots than a cluster holds keys of
+    ([420001], 1, 8, 64, 419990, 0, "head", "random"),
+    ([130, 129, 128, 1], 2, 64, 6, 128, 10, "head", "random"),      # a few over the budget, odd pages
+    ([130, 129, 128, 1], 2, 64, 8, 128, 0, "token", "equal"),
 ])
 def test_evict(lens, kv, dim, page, keep, recent, layout, kind, typ):
     c = make(lens, kv, dim, page, typ, layout, seed=keep, poison=False)
