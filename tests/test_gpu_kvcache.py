@@ -159,6 +159,45 @@ def test_attention(case, window, typ):
 
 
 @pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("seqs,most,heads,kv,dim,page,layout,window", [
+    (20, 1100, 64, 8, 128, 16, "head", False),      # shared jobs, two heads a unit
+    (40, 1200, 24, 8, 64, 8, "token", True),        # four
+    (44, 1030, 16, 8, 128, 5, "head", True),        # four, copied by lanes
+    (36, 1500, 32, 8, 128, 32, "padded", False),    # four, boxes of several heads
+    (48, 300, 24, 8, 128, 64, "head", True),        # whole jobs, two heads a unit
+    (100, 130, 16, 8, 128, 16, "token", False),     # four
+    (24, 90, 64, 32, 64, 128, "head", True),
+    (70, 1100, 24, 2, 64, 16, "head", False),       # 12 query heads a key/value head
+    (6, 1200, 40, 1, 64, 16, "head", True),         # 40
+    (9, 200, 4, 2, 8, 16, "head", False),           # rows shorter than a copy's 128 bytes
+    (30, 1050, 12, 4, 24, 8, "token", True),
+    (5, 1300, 20, 2, 256, 8, "head", False),
+])
+def test_attention_of_many_sequences(seqs, most, heads, kv, dim, page, layout, window, typ):
+    """The ways in which jobs are shared out: heads a unit, whole jobs, boxes."""
+    lens = [(most * (i + 1) // seqs) if i % 7 != 3 else 0 for i in range(seqs)]
+    c = make(lens, kv, dim, page, typ, layout, seed=seqs)
+    g = gen(seqs + 1)
+    q = torch.randn(seqs, heads, dim, generator=g, device="cuda") * 1.5
+    first = None
+    if window:     # most of the units, some heads and some sequences have no live slot
+        c.position.copy_(torch.randint(0, 1000, c.position.shape, generator=g, device="cuda"))
+        c.position[:, 0] //= 4
+        first = torch.full((seqs,), 250, dtype=torch.int32, device="cuda")
+        first[2::5] = 998
+        first[4::5] = 1000
+    want, tol, weights = reference(c, q, dim ** -0.5, first, 0.5)
+    out = c.attend(q, torch.tensor(lens, dtype=torch.int32, device="cuda"), most, first=first, decay=0.5)
+    assert ((out.double() - want).abs() <= tol).all(), float(((out.double() - want).abs() / (tol + 1e-300)).max())
+    for i, n in enumerate(lens):
+        if n:
+            w, wt = weights[i]
+            assert ((rows(c, c.weight, i, n) - w).abs() <= wt).all(), i
+    from paper_2607_29221_gb300 import mosaic as M
+    M.mosaic_device_status()
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
 def test_attention_of_strided_rows_on_another_stream_in_a_graph(typ):
     """q and out rows of wider buffers, a stream of its own, no weights, a
     max_len beyond every length; then a replay with other lengths."""
