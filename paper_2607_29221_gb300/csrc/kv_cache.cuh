@@ -10,7 +10,8 @@
 namespace mosaic {
 namespace {
 
-// n / d for 0 <= n < 2^31 by a multiply and a shift (round-up reciprocal).
+// n / d for 0 <= n < 2^31 by a multiply and a shift (Granlund and Montgomery,
+// "Division by invariant integers using multiplication", 1994).
 struct FastDiv {
     uint32_t d, mul, shift;
     explicit FastDiv(uint32_t d_) : d(d_), mul(0), shift(0) {

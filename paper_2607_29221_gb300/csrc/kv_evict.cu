@@ -9,8 +9,8 @@
 // row is both read and written.
 //
 // Selection: bound by its trips to memory (length, page, weight) and barriers,
-// not by bytes: of 32000 cycles for 16384 slots on one block about 12000 load the
-// keys, 17000 are three histograms and 3000 the rest (20000 while every warp
+// not by bytes: of 37000 cycles for 16384 slots on one block about 12000 load the
+// keys, 16000 are three histograms and 9000 the rest (23000 while every warp
 // walked its slots 32 at a time, instead of every thread its neighbouring ones
 // as bits of a word).  A cluster of blocks takes a (sequence, head), each block
 // a stretch of slots whose keys it keeps in shared memory, with histograms and
