@@ -72,6 +72,27 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(KvView kv, Appen
     const int64_t t = blockIdx.y + (int64_t)blockIdx.z * 65535;
     if (t >= a.l) return;
     const int D = kv.c.head_dim, units = D / 8, rot = a.rope.rot_dim;
+    // The thread's channels c0 .. c0 + 3 and c1 .. c1 + 3 of every head, in the
+    // halves of the channels that turn or of those that do not.
+    const int u = threadIdx.x % units, lane = threadIdx.x / units, lanes = blockDim.x / units;
+    const bool spins = 8 * u < rot;
+    const int c0 = spins ? 4 * u : rot + 4 * (u - rot / 8), c1 = c0 + (spins ? rot : D - rot) / 2;
+    const int H = a.heads, KV = kv.c.kv_heads;
+    const int last = min((int)(blockIdx.x + 1) * a.share, H + 2 * KV);
+    const float *row = a.qkv + t * a.ldx;
+    float *qrow = a.q + t * a.ldq;
+    constexpr int N = 4;
+    Load4 xs[N], ys[N];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (h0 + k * lanes < last) {
+                xs[k] = load4(row + (int64_t)(h0 + k * lanes) * D + c0, a.vec);
+                ys[k] = load4(row + (int64_t)(h0 + k * lanes) * D + c1, a.vec);
+            }
+    };
+    int h0 = blockIdx.x * a.share + lane;
+    load(h0);   // under way while the phases are looked up
     if ((int)threadIdx.x < rot / 2) {
         const int j = threadIdx.x;
         int ax = a.rope.axis ? a.rope.axis[j] : 0;
@@ -85,24 +106,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(KvView kv, Appen
     uint32_t off = 0;
     if (sq >= 0 && sq < kv.c.seqs && sl >= 0 && sl < kv.slots()) id = kv.page_of(sq, (uint32_t)sl, off);
     __syncthreads();
-    // The thread's channels c0 .. c0 + 3 and c1 .. c1 + 3 of every head, in the
-    // halves of the channels that turn or of those that do not.
-    const int u = threadIdx.x % units, lane = threadIdx.x / units, lanes = blockDim.x / units;
-    const bool spins = 8 * u < rot;
-    const int c0 = spins ? 4 * u : rot + 4 * (u - rot / 8), c1 = c0 + (spins ? rot : D - rot) / 2;
-    const int H = a.heads, KV = kv.c.kv_heads;
-    const int last = min((int)(blockIdx.x + 1) * a.share, H + 2 * KV);
-    const float *row = a.qkv + t * a.ldx;
-    float *qrow = a.q + t * a.ldq;
-    constexpr int N = 4;
-    for (int h0 = blockIdx.x * a.share + lane; h0 < last; h0 += N * lanes) {
-        Load4 xs[N], ys[N];
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (h0 + k * lanes < last) {
-                xs[k] = load4(row + (int64_t)(h0 + k * lanes) * D + c0, a.vec);
-                ys[k] = load4(row + (int64_t)(h0 + k * lanes) * D + c1, a.vec);
-            }
+    while (h0 < last) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const int h = h0 + k * lanes;
@@ -142,6 +146,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(KvView kv, Appen
                 }
             }
         }
+        h0 += N * lanes;
+        load(h0);
     }
 }
 

@@ -98,6 +98,8 @@ class PagedCache:
                                     max(table.stride(0), table.shape[1]), k.stride(0), k.stride(1), k.stride(2),
                                     *ptr)
         self._ref = ctypes.byref(self._c)
+        lib = M.lib()
+        self._calls = lib.mosaic_kv_append, lib.mosaic_kv_attention, lib.mosaic_kv_evict
         self._ws = {}
 
     @classmethod
@@ -141,8 +143,13 @@ class PagedCache:
             _need(pos is not None and pos.shape[-1] == l, "pos: a position for every token goes with rope")
             r = rope.at(pos)
         q = torch.empty((l, heads, d), dtype=torch.float32, device=self.device) if out is None else out
-        M.mosaic_kv_append(self._ref, qkv, max(qkv.stride(0), width), l, heads, seq, slot, index,
-                           None if r is None else ctypes.byref(r), q, _rows(q, "out", l, heads, d, self._index))
+        status = self._calls[0](self._ref, qkv.data_ptr(), max(qkv.stride(0), width), l, heads, seq.data_ptr(),
+                                slot.data_ptr(), None if index is None else index.data_ptr(),
+                                None if r is None else ctypes.byref(r), q.data_ptr(),
+                                heads * d if out is None else _rows(q, "out", l, heads, d, self._index),
+                                M._stream(None))
+        if status:
+            raise M.MosaicError("mosaic_kv_append", status)
         return q
 
     def attend(self, q, lens, max_len: int, first=None, scale: float | None = None, decay: float = 1.0, out=None):
@@ -159,8 +166,12 @@ class PagedCache:
         o = torch.empty((n, heads, d), dtype=torch.float32, device=self.device) if out is None else out
         need = self._bytes((heads, max_len), M.mosaic_kv_attention_workspace, heads, max_len)
         ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        M.mosaic_kv_attention(self._ref, q, ldq, heads, lens, max_len, first, d ** -0.5 if scale is None else scale,
-                              decay, o, _rows(o, "out", n, heads, d, at), ws)
+        status = self._calls[1](self._ref, q.data_ptr(), ldq, heads, lens.data_ptr(), max_len,
+                                None if first is None else first.data_ptr(), d ** -0.5 if scale is None else scale,
+                                decay, o.data_ptr(), heads * d if out is None else _rows(o, "out", n, heads, d, at),
+                                None if ws is None else ws.data_ptr(), need, M._stream(None))
+        if status:
+            raise M.MosaicError("mosaic_kv_attention", status)
         return o
 
     def evict(self, lens, max_len: int, keep: int, recent_from=None, new_lens=None):
@@ -171,10 +182,15 @@ class PagedCache:
         if recent_from is not None:
             _int32(recent_from, "recent_from", self.seqs, self._index)
         new = torch.empty_like(lens) if new_lens is None else new_lens
-        _int32(new, "new_lens", self.seqs, self._index)
+        if new_lens is not None:
+            _int32(new, "new_lens", self.seqs, self._index)
         need = self._bytes(("evict", max_len, keep), M.mosaic_kv_evict_workspace, max_len, keep)
         ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        M.mosaic_kv_evict(self._ref, lens, max_len, keep, recent_from, new, ws)
+        status = self._calls[2](self._ref, lens.data_ptr(), max_len, keep,
+                                None if recent_from is None else recent_from.data_ptr(), new.data_ptr(),
+                                None if ws is None else ws.data_ptr(), need, M._stream(None))
+        if status:
+            raise M.MosaicError("mosaic_kv_evict", status)
         return new
 
 
