@@ -11,13 +11,15 @@ call on the current stream:
   out   = cache.attend(q, lens, max_len)
   lens  = cache.evict(lens, max_len, keep, recent_from=recent_from)
 
-Arguments are tensors on the cache's device; scratch comes from torch's
-allocator for the current stream.  ``PageTable`` is the host's account of which
-page belongs to whom.
+Arguments are tensors on the cache's device.  Scratch is kept for each stream
+and host thread (5 us a call to allocate it anew); calls that are captured into
+a graph get scratch of their own, since the graph may run beside anything.
+``PageTable`` is the host's account of which page belongs to whom.
 """
 from __future__ import annotations
 
 import ctypes
+import threading
 
 import torch
 
@@ -100,7 +102,7 @@ class PagedCache:
         self._ref = ctypes.byref(self._c)
         lib = M.lib()
         self._calls = lib.mosaic_kv_append, lib.mosaic_kv_attention, lib.mosaic_kv_evict
-        self._ws = {}
+        self._ws, self._scratch = {}, {}
 
     @classmethod
     def empty(cls, pages: int, kv_heads: int, page_size: int, head_dim: int, table, dtype=torch.bfloat16,
@@ -118,6 +120,17 @@ class PagedCache:
                 self._ws.clear()
             n = self._ws[key] = size(self._ref, *args)
         return n
+
+    def _workspace(self, need: int, stream: int):
+        if not need:
+            return None
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(need, dtype=torch.uint8, device=self.device)
+        key = stream, threading.get_ident()
+        ws = self._scratch.get(key)
+        if ws is None or ws.numel() < need:
+            ws = self._scratch[key] = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return ws
 
     def read(self, seq: int, n: int):
         """Keys and values of the first n slots of a sequence, kv_heads x n x head_dim in the cache's type (a copy)."""
@@ -165,11 +178,12 @@ class PagedCache:
             _int32(first, "first", n, at)
         o = torch.empty((n, heads, d), dtype=torch.float32, device=self.device) if out is None else out
         need = self._bytes((heads, max_len), M.mosaic_kv_attention_workspace, heads, max_len)
-        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        stream = M._stream(None)
+        ws = self._workspace(need, stream)
         status = self._calls[1](self._ref, q.data_ptr(), ldq, heads, lens.data_ptr(), max_len,
                                 None if first is None else first.data_ptr(), d ** -0.5 if scale is None else scale,
                                 decay, o.data_ptr(), heads * d if out is None else _rows(o, "out", n, heads, d, at),
-                                None if ws is None else ws.data_ptr(), need, M._stream(None))
+                                None if ws is None else ws.data_ptr(), need, stream)
         if status:
             raise M.MosaicError("mosaic_kv_attention", status)
         return o
@@ -185,10 +199,11 @@ class PagedCache:
         if new_lens is not None:
             _int32(new, "new_lens", self.seqs, self._index)
         need = self._bytes(("evict", max_len, keep), M.mosaic_kv_evict_workspace, max_len, keep)
-        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        stream = M._stream(None)
+        ws = self._workspace(need, stream)
         status = self._calls[2](self._ref, lens.data_ptr(), max_len, keep,
                                 None if recent_from is None else recent_from.data_ptr(), new.data_ptr(),
-                                None if ws is None else ws.data_ptr(), need, M._stream(None))
+                                None if ws is None else ws.data_ptr(), need, stream)
         if status:
             raise M.MosaicError("mosaic_kv_evict", status)
         return new

@@ -286,6 +286,47 @@ def test_attention_repeats_bit_for_bit():
         assert all(torch.equal(a, b) for a, b in zip(first, got))
 
 
+def test_scratch_of_streams_threads_and_graphs_is_apart():
+    """Calls on several streams and host threads and replays of a graph, all at
+    once, with scratch that grows: each gives what it gives alone."""
+    import threading
+    lens = [3000, 1700, 40, 2100]
+    c = make(lens, 8, 64, 16, "bf16", seed=13)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    qs = [torch.randn(4, h, 64, generator=gen(h), device="cuda") for h in (8, 64, 16, 32)]
+    bare = type(c)(c.k, c.v, c.table, position=c.position)
+    want = [bare.attend(q, n, 3000) for q in qs]
+    first = torch.randn(4, 8, 64, generator=gen(99), device="cuda")
+    alone = bare.attend(first, n, 3000)
+    graph, out = torch.cuda.CUDAGraph(), torch.empty_like(first)
+    with torch.cuda.graph(graph):
+        bare.attend(first, n, 3000, out=out)
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(k):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(30):
+                if not torch.equal(bare.attend(qs[k], n, 3000), want[k]):
+                    bad.append(k)
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    side = torch.cuda.Stream()
+    for _ in range(30):
+        out.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graph.replay()
+        got = [bare.attend(q, n, 3000) for q in qs]
+        torch.cuda.synchronize()
+        assert torch.equal(out, alone) and all(torch.equal(a, b) for a, b in zip(got, want))
+    for t in threads:
+        t.join()
+    assert not bad
+
+
 def test_offsets_past_32_bits():
     """Pages more than 2^31 elements apart: append, attention and eviction reach them."""
     from paper_2607_29221_gb300 import kvcache as KV
