@@ -14,8 +14,10 @@ constexpr int kMaxGroup = 64;
 // key/value heads of 128, bf16 (one sequence, then 16, 32, 64 of equal and 64
 // of spread lengths): 256 slots 8 / 12, 9 / 15, 11 / 19, 17 / 25, 14 / 21; 512:
 // 12 / 13, 13 / 18, 17 / 24, 27 / 36, 23 / 26; 1024: 20 / 15, 22 / 24, 27 / 35,
-// 47 / 56, 40 / 36; 2048: 35 / 19, 38 / 34, 47 / 55, 85 / 95, 67 / 57.
-constexpr int64_t kWholeFew = 512, kWholeMany = 1024, kManyJobs = 128;
+// 47 / 56, 40 / 36; 2048: 35 / 19, 38 / 34, 47 / 55, 85 / 95, 67 / 57.  Long rows
+// earlier: fp32, one sequence 256 slots 11 / 14, 512: 17 / 15; 64 of spread
+// lengths 512: 47 / 47, 1024: 75 / 68.
+constexpr int64_t kWholeFew = 512, kWholeMany = 1024, kManyJobs = 128, kWholeBytes = 128 * 1024;
 // Heads share a unit (the blocks' warps then have a head each and nothing to
 // merge) while so many jobs remain to be shared out; whole jobs while there is
 // more than a wave of them.  Shared jobs with 1 / 2 / 4 heads a unit, up to 1024
@@ -115,12 +117,10 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendSh
 
 // A thread four slots of a (sequence, key/value head): the weight that they
 // gather.  Bound by reading the scores (4 bytes a slot and query head); every
-// load of a thread is issued before its use.  vec: four slots share a page and
-// a 16-byte word of the weights.
+// load of a thread is issued before its use.
 constexpr int kWeightSlots = 4 * 128;
 struct WeightWalk {
     int64_t chunks, jobs_step, chunk_step;   // the grid's stride over (job, chunk of slots)
-    int vec;
 };
 __global__ void __launch_bounds__(128, 6) attend_weight_kernel(KvView kv, AttendArgs a, WeightWalk walk) {
     pdl_enter();
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(128, 6) attend_weight_kernel(KvView kv, Attend
         uint32_t off;
         const int id = kv.page_of(i, (uint32_t)s, off);
         at[0] = id < 0 ? nullptr : kv.c.weight + kv.mark(id, h, off);
-        const bool quad = walk.vec && s + 4 <= len;
+        const bool quad = a.quads && s + 4 <= len;
         if (!quad) {
 #pragma unroll
             for (int j = 1; j < 4; ++j) {
@@ -225,7 +225,10 @@ AttendShape shape_of(const mosaic_kv_cache &c, int64_t heads) {
 int64_t most_blocks(const mosaic_kv_cache &c, const AttendShape &s, int64_t heads, int64_t max_len) {
     const int64_t group = heads / c.kv_heads, hb = (group + s.heads - 1) / s.heads;
     const int64_t units = c.seqs * c.kv_heads * hb * ((max_len + s.unit - 1) / s.unit);
-    return max_len <= (c.seqs * c.kv_heads * hb >= kManyJobs ? kWholeMany : kWholeFew) ? 0 : units < kAttendWave ? units : kAttendWave;
+    const bool many = c.seqs * c.kv_heads * hb >= kManyJobs;
+    const int64_t row = c.head_dim * kv_element_bytes(c.type);
+    const bool whole = max_len <= (many ? kWholeMany : kWholeFew) && max_len * row <= (many ? 2 : 1) * kWholeBytes;
+    return whole ? 0 : units < kAttendWave ? units : kAttendWave;
 }
 mosaic_status check(const mosaic_kv_cache *c, int64_t heads, int64_t max_len) {
     MOSAIC_TRY(kv_check(c));
@@ -292,6 +295,7 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
         a.stats = reinterpret_cast<float *>(w), w += p.stats;
         a.scores = reinterpret_cast<float *>(w);
         a.score_rows = rows_of(max_len);
+        a.quads = cache->page_size % 4 == 0 && aligned16(cache->weight);
     }
     const int64_t jobs = cache->seqs * (cache->kv_heads / a.hpu) * a.hb;
     a.blocks = (int)(a.whole ? jobs : cap);
@@ -314,8 +318,7 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     {
         KernelSpan span("attend_weight", st);
         const int64_t grid = all < 152 * 6 ? all : 152 * 6;
-        const WeightWalk walk = {chunks, grid / chunks, grid % chunks,
-                                 cache->page_size % 4 == 0 && aligned16(cache->weight)};
+        const WeightWalk walk = {chunks, grid / chunks, grid % chunks};
         pdl_launch(attend_weight_kernel, dim3((unsigned)grid), dim3(128), 0, st, kv, a, walk);
     }
     return launch_status();

@@ -71,6 +71,7 @@ struct AttendArgs {
     float *scores;              // (sequence, head) x score_rows, for the weights (none where 16 slots in a
                                 // row do not count)
     int64_t score_rows;
+    int quads;                  // four slots from a multiple of 4 on share a page and an aligned word of weights
 };
 
 // What the instance for a head_dim and a group has (query heads of a job,

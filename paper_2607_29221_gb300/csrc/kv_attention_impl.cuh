@@ -958,20 +958,44 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
         if (a.scores && a.whole && a.hb == 1) {
             // The job's scores are this block's: its weights need no further launch.
             consumers_sync<THREADS>();
-            for (int x = 32 * sub + lane; x < s1; x += 32 * of_head) {
-                uint32_t off;
-                const int id = kv.page_of(i, (uint32_t)x, off);
-                float *to = kv.c.weight + kv.mark(max(id, 0), h, off);
-                const float old = id < 0 ? 0.0f : *to;
-                float sum = 0.0f;
-#pragma unroll 8
-                for (int r = 0; r < rows; ++r) {
-                    const float2 st = pipe.stats[hi * S::kHeads + r];
-                    sum = fmaf(power2(scores[r * a.score_rows + x] - st.x), st.y, sum);
+            for (int x = 4 * (32 * sub + lane); x < s1; x += 128 * of_head) {   // a lane four slots
+                const bool quad = a.quads && x + 4 <= s1;
+                int64_t at[4];
+                __align__(16) float old[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (quad && j) {
+                        at[j] = at[0] < 0 ? -1 : at[0] + j;
+                        continue;
+                    }
+                    uint32_t off;
+                    const int id = x + j < s1 ? kv.page_of(i, (uint32_t)(x + j), off) : -1;
+                    at[j] = id < 0 ? -1 : kv.mark(id, h, off);
                 }
-                if (id < 0) continue;
-                if (a.first && kv.c.position[kv.mark(id, h, off)] < a.first[i]) sum = 0.0f;   // it may have no score
-                *to = fmaf(old, a.decay, sum);
+                if (quad && at[0] >= 0) *reinterpret_cast<float4 *>(old) = *reinterpret_cast<const float4 *>(kv.c.weight + at[0]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (!quad && at[j] >= 0) old[j] = kv.c.weight[at[j]];
+#pragma unroll 8
+                for (int r = 0; r < rows; ++r) {   // rows of 16 slots exist in whole
+                    const float2 st = pipe.stats[hi * S::kHeads + r];
+                    const float4 v = *reinterpret_cast<const float4 *>(scores + r * a.score_rows + x);
+                    sum[0] = fmaf(power2(v.x - st.x), st.y, sum[0]);
+                    sum[1] = fmaf(power2(v.y - st.x), st.y, sum[1]);
+                    sum[2] = fmaf(power2(v.z - st.x), st.y, sum[2]);
+                    sum[3] = fmaf(power2(v.w - st.x), st.y, sum[3]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    // Slots below the bound gather nothing (and may have no score).
+                    if (a.first && at[j] >= 0 && kv.c.position[at[j]] < a.first[i]) sum[j] = 0.0f;
+                    old[j] = fmaf(old[j], a.decay, sum[j]);
+                }
+                if (quad && at[0] >= 0) *reinterpret_cast<float4 *>(kv.c.weight + at[0]) = *reinterpret_cast<const float4 *>(old);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (!quad && at[j] >= 0) kv.c.weight[at[j]] = old[j];
             }
         }
         if (!whole && jobs.b0 == 0 && tid == 0) {   // this block's end cuts the job: who has the rest of it?
