@@ -674,8 +674,8 @@ mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, i
  *     weight_j = decay weight_j + sum of p_j over the head's query heads.
  * Products of queries, weights and 16-bit values are carried to 22 bits or
  * more and summed in fp32.  heads: a multiple of kv_heads, at most 64 query
- * heads a key/value head.  max_len: an upper bound of the lengths, which
- * sizes the workspace (mosaic_kv_attention_workspace bytes for the same
+ * heads a key/value head.  max_len (max_len heads < 2^34): an upper bound of
+ * the lengths, which sizes the workspace (mosaic_kv_attention_workspace bytes for the same
  * cache, heads and max_len; 0 if none is needed or they are not valid).  out: seqs x heads
  * head_dim fp32 (ldo), no overlap with q.  Results do not depend on the run. */
 size_t mosaic_kv_attention_workspace(const mosaic_kv_cache *cache, int64_t heads, int64_t max_len);

@@ -236,6 +236,8 @@ mosaic_status check(const mosaic_kv_cache *c, int64_t heads, int64_t max_len) {
         return MOSAIC_ERR_SHAPE;
     if (heads / c->kv_heads > kMaxGroup) return MOSAIC_ERR_UNSUPPORTED;
     if (c->seqs * heads > 0x7fffffff || c->seqs * heads * (max_len + 1) > (int64_t)1 << 46) return MOSAIC_ERR_SHAPE;
+    // Units of a sequence (16 slots or more of a head, and a job's cost) are counted in 31 bits.
+    if ((max_len / 16 + 4096) * heads > 0x7fffffff) return MOSAIC_ERR_SHAPE;
     return MOSAIC_OK;
 }
 int64_t rows_of(int64_t max_len) { return (max_len + 15) / 16 * 16; }

@@ -75,7 +75,7 @@ def test_no_cache_is_an_argument_error(lib):
 
 @pytest.mark.parametrize("over,status", [
     (dict(heads=0), SHAPE), (dict(heads=60), SHAPE), (dict(ldq=8191), SHAPE), (dict(ldo=8191), SHAPE),
-    (dict(max_len=-1), SHAPE), (dict(heads=8 * 65, ldq=1 << 20, ldo=1 << 20), UNSUPPORTED),
+    (dict(max_len=-1), SHAPE), (dict(max_len=1 << 30), SHAPE), (dict(heads=8 * 65, ldq=1 << 20, ldo=1 << 20), UNSUPPORTED),
     (dict(scale=math.inf), ARG), (dict(scale=math.nan), ARG), (dict(decay=math.nan), ARG), (dict(q=None), ARG),
     (dict(out=None), ARG), (dict(lens=None), ARG), (dict(ws=None), ARG), (dict(ws=FAKE + 8), ALIGN),
     (dict(ws_bytes=100), WORKSPACE)])
