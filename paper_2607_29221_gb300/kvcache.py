@@ -39,13 +39,24 @@ def _int32(t, name: str, n: int, index: int) -> None:
         raise ValueError(f"{name}: a contiguous int32 tensor of {n} elements on the cache's device is needed")
 
 
+def _row_stride(t, width: int, name: str) -> int:
+    """The distance of t's rows, at least ``width``: rows that share memory
+    (expanded or overlapping views) have no leading dimension."""
+    stride = t.stride(0)
+    if stride >= width:
+        return stride
+    if t.shape[0] > 1:
+        raise ValueError(f"{name}: rows must not share memory (an expanded view needs .contiguous())")
+    return width
+
+
 def _rows(t, name: str, n: int, heads: int, dim: int, index: int) -> int:
     """The row stride of a float32 n x heads x dim tensor whose rows are contiguous."""
     st = t.stride() if t.dim() == 3 else (0, 0, 0)
     if (t.dtype is not torch.float32 or t.get_device() != index or t.shape != (n, heads, dim) or st[2] != 1
             or (heads > 1 and st[1] != dim)):
         raise ValueError(f"{name}: float32, {n} x {heads} x {dim}, rows contiguous, on the cache's device")
-    return max(st[0], heads * dim)
+    return _row_stride(t, heads * dim, name)
 
 
 class Rope:
@@ -72,7 +83,7 @@ class Rope:
                 or (pos.shape[1] > 1 and pos.stride(1) != 1) or pos.get_device() != self.turns.get_device()):
             raise ValueError(f"pos: int32, {self.axes} x tokens, rows contiguous, on the rope's device")
         return M.mosaic_rope(self.rot_dim, self.interleaved, self.axes, self._turns, self._axis, pos.data_ptr(),
-                             max(pos.stride(0), pos.shape[1]))
+                             _row_stride(pos, pos.shape[1], "pos"))
 
 
 class PagedCache:
@@ -97,7 +108,7 @@ class PagedCache:
         self._index = k.get_device()
         ptr = [None if t is None else t.data_ptr() for t in (k, v, table, position, weight)]
         self._c = M.mosaic_kv_cache(_TYPES[k.dtype], kv_heads, dim, page, pages, table.shape[0], table.shape[1],
-                                    max(table.stride(0), table.shape[1]), k.stride(0), k.stride(1), k.stride(2),
+                                    _row_stride(table, table.shape[1], "table"), k.stride(0), k.stride(1), k.stride(2),
                                     *ptr)
         self._ref = ctypes.byref(self._c)
         lib = M.lib()
@@ -146,7 +157,7 @@ class PagedCache:
         if (qkv.dtype is not torch.float32 or qkv.dim() != 2 or qkv.get_device() != self._index
                 or qkv.shape[1] != width or qkv.stride(1) != 1):
             raise ValueError("qkv: float32, l x (heads + 2 kv_heads) head_dim, rows contiguous, on the cache's device")
-        l = qkv.shape[0]
+        l, ldx = qkv.shape[0], _row_stride(qkv, width, "qkv")
         _int32(seq, "seq", l, self._index)
         _int32(slot, "slot", l, self._index)
         if index is not None:
@@ -156,7 +167,7 @@ class PagedCache:
             _need(pos is not None and pos.shape[-1] == l, "pos: a position for every token goes with rope")
             r = rope.at(pos)
         q = torch.empty((l, heads, d), dtype=torch.float32, device=self.device) if out is None else out
-        status = self._calls[0](self._ref, qkv.data_ptr(), max(qkv.stride(0), width), l, heads, seq.data_ptr(),
+        status = self._calls[0](self._ref, qkv.data_ptr(), ldx, l, heads, seq.data_ptr(),
                                 slot.data_ptr(), None if index is None else index.data_ptr(),
                                 None if r is None else ctypes.byref(r), q.data_ptr(),
                                 heads * d if out is None else _rows(q, "out", l, heads, d, self._index),

@@ -558,3 +558,26 @@ def test_python_refusals():
         KV.PagedCache(c.k, c.v, c.table, weight=c.weight.double())
     with pytest.raises(ValueError):
         c.append(torch.zeros(1, 7 * 64, device="cuda"), 4, n, n, n)
+
+
+def test_expanded_rows_are_refused():
+    """Rows that share memory, wherever a call takes rows: nothing is launched."""
+    from paper_2607_29221_gb300 import kvcache as KV
+    from paper_2607_29221_gb300 import mosaic as M
+    c = make([20, 20, 20], 2, 64, 16, "bf16")
+    n = torch.tensor([20, 20, 20], dtype=torch.int32, device="cuda")
+    q, one = torch.zeros(3, 4, 64, device="cuda"), torch.zeros(1, 4, 64, device="cuda")
+    row = torch.zeros(1, 8 * 64, device="cuda")
+    rope = KV.Rope(64, sections=[8, 12, 12])
+    pos = torch.zeros(1, 3, dtype=torch.int32, device="cuda")
+    before = M.mosaic_kernel_launches()
+    for call in (lambda: c.attend(one.expand(3, 4, 64), n, 20), lambda: c.attend(q, n, 20, out=one.expand(3, 4, 64)),
+                 lambda: c.append(row.expand(3, 512), 4, n, n, n),
+                 lambda: c.append(row.repeat(3, 1), 4, n, n, n, out=one.expand(3, 4, 64)),
+                 lambda: c.append(row.repeat(3, 1), 4, n, n, n, rope=rope, pos=pos.expand(3, 3)),
+                 lambda: KV.PagedCache(c.k, c.v, c.table[:1].expand(3, 2))):
+        with pytest.raises(ValueError, match="share memory"):
+            call()
+    assert M.mosaic_kernel_launches() == before
+    same = c.append(row.repeat(3, 1), 4, n - n - 1, n - n - 1, n, rope=rope, pos=pos.expand(3, 3).contiguous())
+    assert (same == 0).all()

@@ -187,3 +187,24 @@ def test_page_table_accounts_for_its_pages(lib):
         t.resize(0, 65)
     t.resize(0, 0)
     assert t.owned[0] == []
+
+
+def test_rows_that_share_memory_have_no_leading_dimension(lib):
+    """An expanded or overlapping view must not be given a stride that walks past its storage."""
+    torch = pytest.importorskip("torch")
+    from paper_2607_29221_gb300 import kvcache as KV
+    rope = KV.Rope(64, sections=[8, 12, 12], device="cpu")
+    pos = torch.arange(5, dtype=torch.int32)
+    for bad in (pos[None].expand(3, 5), torch.arange(9, dtype=torch.int32).as_strided((3, 5), (2, 1))):
+        with pytest.raises(ValueError, match="share memory"):
+            rope.at(bad)
+    assert rope.at(pos[None].expand(3, 5).contiguous()).ldp == 5
+    assert rope.at(torch.arange(24, dtype=torch.int32).reshape(3, 8)[:, :5]).ldp == 8
+    one = KV.Rope(64, device="cpu")
+    assert one.at(pos).ldp == 5 and one.at(pos[:1]).ldp == 1
+    for bad in (torch.zeros(1, 4, 8).expand(3, 4, 8), torch.zeros(64).as_strided((3, 4, 8), (16, 8, 1))):
+        with pytest.raises(ValueError, match="share memory"):
+            KV._rows(bad, "out", 3, 4, 8, -1)
+    assert KV._rows(torch.zeros(1, 4, 8), "q", 1, 4, 8, -1) == 32
+    assert KV._rows(torch.zeros(0, 4, 8), "q", 0, 4, 8, -1) == 32
+    assert KV._rows(torch.zeros(3, 40)[:, 8:].unflatten(1, (4, 8)), "q", 3, 4, 8, -1) == 40
