@@ -164,6 +164,8 @@ class PagedCache:
             _int32(index, "index", l, self._index)
         r = None
         if rope is not None:
+            if rope.turns.get_device() != self._index:
+                raise ValueError("rope: on another device than the cache")
             _need(pos is not None and pos.shape[-1] == l, "pos: a position for every token goes with rope")
             r = rope.at(pos)
         q = torch.empty((l, heads, d), dtype=torch.float32, device=self.device) if out is None else out

@@ -208,3 +208,24 @@ def test_rows_that_share_memory_have_no_leading_dimension(lib):
     assert KV._rows(torch.zeros(1, 4, 8), "q", 1, 4, 8, -1) == 32
     assert KV._rows(torch.zeros(0, 4, 8), "q", 0, 4, 8, -1) == 32
     assert KV._rows(torch.zeros(3, 40)[:, 8:].unflatten(1, (4, 8)), "q", 3, 4, 8, -1) == 40
+
+
+def test_append_refuses_a_rope_on_another_device(lib, monkeypatch):
+    """Host pointers must not reach a kernel.  The handle is a stand-in on host tensors whose library calls only
+    count."""
+    torch = pytest.importorskip("torch")
+    from paper_2607_29221_gb300 import kvcache as KV
+    monkeypatch.setattr(M, "_stream", lambda s: 0)
+    c, calls = object.__new__(KV.PagedCache), []
+    c.head_dim, c.kv_heads, c.device, c._ref = 8, 1, torch.device("cpu"), None
+    c._calls = [lambda *a: calls.append(a) or 0] * 3
+    c._index = 0                                     # the cache's device is cuda:0; host tensors report -1
+    rope, at = KV.Rope(8, device="cpu"), torch.zeros(2, dtype=torch.int32)
+
+    class OnDevice(torch.Tensor):                    # host tensors that say that they lie on cuda:0
+        def get_device(self):
+            return 0
+    ints, qkv = at.as_subclass(OnDevice), torch.zeros(2, 24).as_subclass(OnDevice)
+    with pytest.raises(ValueError, match="another device"):
+        c.append(qkv, 1, ints, ints, ints, rope=rope, pos=at)
+    assert not calls
