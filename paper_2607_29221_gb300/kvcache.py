@@ -132,6 +132,12 @@ class PagedCache:
             n = self._ws[key] = size(self._ref, *args)
         return n
 
+    def _stream(self) -> int:
+        """The current stream, which has to be one of the cache's device."""
+        if torch.cuda.current_device() != self._index:
+            raise ValueError("the cache's device is not the current one")
+        return M._stream(None)
+
     def _workspace(self, need: int, stream: int):
         if not need:
             return None
@@ -173,7 +179,7 @@ class PagedCache:
                                 slot.data_ptr(), None if index is None else index.data_ptr(),
                                 None if r is None else ctypes.byref(r), q.data_ptr(),
                                 heads * d if out is None else _rows(q, "out", l, heads, d, self._index),
-                                M._stream(None))
+                                self._stream())
         if status:
             raise M.MosaicError("mosaic_kv_append", status)
         return q
@@ -190,8 +196,8 @@ class PagedCache:
         if first is not None:
             _int32(first, "first", n, at)
         o = torch.empty((n, heads, d), dtype=torch.float32, device=self.device) if out is None else out
+        stream = self._stream()
         need = self._bytes((heads, max_len), M.mosaic_kv_attention_workspace, heads, max_len)
-        stream = M._stream(None)
         ws = self._workspace(need, stream)
         status = self._calls[1](self._ref, q.data_ptr(), ldq, heads, lens.data_ptr(), max_len,
                                 None if first is None else first.data_ptr(), d ** -0.5 if scale is None else scale,
@@ -211,8 +217,8 @@ class PagedCache:
         new = torch.empty_like(lens) if new_lens is None else new_lens
         if new_lens is not None:
             _int32(new, "new_lens", self.seqs, self._index)
+        stream = self._stream()
         need = self._bytes(("evict", max_len, keep), M.mosaic_kv_evict_workspace, max_len, keep)
-        stream = M._stream(None)
         ws = self._workspace(need, stream)
         status = self._calls[2](self._ref, lens.data_ptr(), max_len, keep,
                                 None if recent_from is None else recent_from.data_ptr(), new.data_ptr(),

@@ -229,3 +229,26 @@ def test_append_refuses_a_rope_on_another_device(lib, monkeypatch):
     with pytest.raises(ValueError, match="another device"):
         c.append(qkv, 1, ints, ints, ints, rope=rope, pos=at)
     assert not calls
+
+
+@pytest.mark.parametrize("call", ["append", "attend", "evict"])
+def test_calls_refuse_while_another_device_is_current(lib, monkeypatch, call):
+    """The stream is the current device's: a launch there would run on the wrong GPU.  Host tensors and library
+    calls that only count stand in."""
+    torch = pytest.importorskip("torch")
+    from paper_2607_29221_gb300 import kvcache as KV
+    monkeypatch.setattr(M, "_stream", lambda s: 0)
+    c, calls = object.__new__(KV.PagedCache), []
+    c.head_dim, c.kv_heads, c.seqs, c.device, c._ref, c._index = 8, 1, 2, torch.device("cpu"), None, -1
+    c._calls = [lambda *a: calls.append(a) or 0] * 3
+    c._bytes = lambda *a: 0
+    ints = torch.zeros(2, dtype=torch.int32)
+    run = {"append": lambda: c.append(torch.zeros(2, 24), 1, ints, ints, ints),
+           "attend": lambda: c.attend(torch.zeros(2, 1, 8), ints, 5), "evict": lambda: c.evict(ints, 5, 2)}[call]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    run()
+    assert len(calls) == 1
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="not the current one"):
+        run()
+    assert len(calls) == 1
