@@ -669,8 +669,8 @@ mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, i
  * Live: j < lens[i] (clamped to [0, max_len] and the table) and, with `first`
  * (seqs entries; needs cache->position), position_j >= first[i].  A slot that
  * is not live is never used, whatever its page holds; a row without a live
- * slot gives zeros.  A live key or value that is infinite counts as NaN.  With
- * cache->weight, every slot j < lens[i] gets
+ * slot gives zeros.  A live key or value that is infinite counts as NaN, and so does
+ * a score or an output beyond fp32.  With cache->weight, every slot j < lens[i] gets
  *     weight_j = decay weight_j + sum of p_j over the head's query heads.
  * Products of queries, weights and 16-bit values are carried to 22 bits or
  * more and summed in fp32.  heads: a multiple of kv_heads, at most 64 query

@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a, AttendSh
             const float o[4] = {out[half].x, out[half].y, out[half].z, out[half].w};
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-                if (d + x < dim) a.out[i * a.ldo + qh * dim + d + x] = o[x] * inv;
+                if (d + x < dim) a.out[i * a.ldo + qh * dim + d + x] = finite_or_nan(o[x] * inv);
         }
         if (a.scores && lane == 0) a.stats[2 * (i * a.heads + qh)] = ref, a.stats[2 * (i * a.heads + qh) + 1] = inv;
     }

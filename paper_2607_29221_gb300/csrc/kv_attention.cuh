@@ -91,6 +91,10 @@ template <class T> mosaic_status attend_status();
 namespace {
 
 __device__ __forceinline__ float minus_inf() { return __int_as_float(0xff800000); }
+// x, and NaN where x is infinite.
+__device__ __forceinline__ float finite_or_nan(float x) {
+    return fabsf(x) < __int_as_float(0x7f800000) ? x : __int_as_float(0x7fffffff);
+}
 // 2^x to 2^-22 relative; results below 2^-126 are zeros.
 __device__ __forceinline__ float power2(float x) {
     float y;

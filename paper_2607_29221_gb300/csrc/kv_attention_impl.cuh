@@ -302,7 +302,8 @@ struct Warp {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if constexpr (sizeof(T) == 2 && kTermsN == 2) s[n][j] *= unscale[n][j & 1];
-                s[n][j] = (j < 2 ? up : dn) ? s[n][j] : minus_inf();
+                // An infinite key: the terms of a query sum to either infinity or NaN, by their signs.
+                s[n][j] = (j < 2 ? up : dn) ? finite_or_nan(s[n][j]) : minus_inf();
             }
             if (sc) {
 #pragma unroll
@@ -939,8 +940,9 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
                         float *out = a.out + i * a.ldo + (qh + head) * D;
 #pragma unroll
                         for (int x = 0; x < DP / 16; ++x) {
-                            if (16 * x + g < D) out[16 * x + g] = wp.o[n][x][j] * inv;
-                            if (16 * x + g + 8 < D) out[16 * x + g + 8] = wp.o[n][x][2 + j] * inv;
+                            // (an infinite value: as with keys)
+                            if (16 * x + g < D) out[16 * x + g] = finite_or_nan(wp.o[n][x][j] * inv);
+                            if (16 * x + g + 8 < D) out[16 * x + g + 8] = finite_or_nan(wp.o[n][x][2 + j] * inv);
                         }
                         if (a.scores && g == 0) {
                             const float ref = m == minus_inf() ? 0.0f : m;

@@ -581,3 +581,45 @@ def test_expanded_rows_are_refused():
     assert M.mosaic_kernel_launches() == before
     same = c.append(row.repeat(3, 1), 4, n - n - 1, n - n - 1, n, rope=rope, pos=pos.expand(3, 3).contiguous())
     assert (same == 0).all()
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("lens,heads,kv,dim,page,layout", [
+    ([200, 90], 8, 2, 64, 16, "head"),
+    ([200, 90], 32, 2, 128, 7, "token"),
+    ([3000, 700], 16, 4, 128, 16, "head"),
+    ([3000, 700], 12, 1, 256, 5, "head"),
+    ([1100] * 20, 16, 8, 64, 8, "head"),
+])
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+def test_attention_counts_live_infinities_as_nan(lens, heads, kv, dim, page, layout, value, typ):
+    """A live infinite key makes its head's rows NaN and a live infinite value
+    its channel, whatever the signs of the queries, in the first slots and later
+    ones; other heads, sequences and channels keep their results, and so does a
+    row whose bound leaves the slot out."""
+    bad = []
+    group = heads // kv
+    q = torch.randn(len(lens), heads, dim, generator=gen(21), device="cuda")
+    q[:, 0] = q[:, 0].abs()
+    q[:, 1 % group] = -q[:, 1 % group].abs()
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    for slot in (0, 5, lens[0] // 2, lens[0] - 1):
+        c = make(lens, kv, dim, page, typ, layout, seed=slot, poison=False)
+        c.position.zero_()
+        at = int(c.table[0, slot // page]), slot % page
+        c.position[at[0], :, at[1]] = -1
+        want, tol, _ = reference(c, q, 0.125)
+        c.k[at[0], 0, at[1], 3] = value
+        c.v[at[0], kv - 1, at[1], 6] = value
+        out = c.attend(q, n, max(lens), scale=0.125)
+        nan = torch.zeros_like(out, dtype=torch.bool)
+        nan[0, :group] = True
+        nan[0, heads - group:, 6] = True
+        if not torch.isnan(out[nan]).all():
+            bad.append((slot, "nan", float(torch.isnan(out[nan]).float().mean())))
+        if not ((out.double() - want).abs() <= tol)[~nan].all():
+            bad.append((slot, "rest"))
+        keep = c.attend(q, n, max(lens), first=torch.zeros_like(n), scale=0.125)
+        if not torch.isfinite(keep).all():
+            bad.append((slot, "left out"))
+    assert not bad, bad
