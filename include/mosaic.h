@@ -673,7 +673,9 @@ mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, i
  * a score or an output beyond fp32.  With cache->weight, every slot j < lens[i] gets
  *     weight_j = decay weight_j + sum of p_j over the head's query heads.
  * Products of queries, weights and 16-bit values are carried to 22 bits or
- * more and summed in fp32.  heads: a multiple of kv_heads, at most 64 query
+ * more and summed in fp32 (fp16 caches: of query channels down to 2^-29 of the
+ * head's largest and weights p down to 2^-87 of the row's largest; smaller ones
+ * are off by up to 2^-51 and 2^-110 of those).  heads: a multiple of kv_heads, at most 64 query
  * heads a key/value head.  max_len (max_len heads < 2^34): an upper bound of
  * the lengths, which sizes the workspace (mosaic_kv_attention_workspace bytes for the same
  * cache, heads and max_len; 0 if none is needed or they are not valid).  out: seqs x heads

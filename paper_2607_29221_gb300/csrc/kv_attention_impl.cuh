@@ -83,6 +83,10 @@ __device__ __forceinline__ float2 unpack2(uint32_t v, __nv_bfloat16) {
 __device__ __forceinline__ float2 unpack2(uint32_t v, __half) {
     return __half22float2(*reinterpret_cast<const __half2 *>(&v));
 }
+// fp16: a term is kept times 2^12 of the next greater one's scale, which keeps
+// it clear of subnormals: of an x of up to 2^15 a term's rest is 8 at most.
+template <class T> constexpr float kStep = 1.0f;
+template <> constexpr float kStep<__half> = 4096.0f;
 // x, y -> terms t[0] (the least) .. t[N-1] (the greatest), packed.
 template <class T, int N>
 __device__ __forceinline__ void split2(float x, float y, uint32_t (&t)[N]) {
@@ -91,7 +95,7 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&t)[N]) {
         t[i] = pack2(x, y, T());
         if (i) {
             const float2 v = unpack2(t[i], T());
-            x -= v.x, y -= v.y;
+            x = (x - v.x) * kStep<T>, y = (y - v.y) * kStep<T>;
         }
     }
 }
@@ -105,9 +109,13 @@ __device__ __forceinline__ uint32_t tf32_low(float x, uint32_t high) {
 
 template <class T> constexpr int kTerms = sizeof(T) == 4 ? 2 : 3;
 template <> constexpr int kTerms<__half> = 2;
-// Probabilities are kept times 2^shift, so that fp16's lower term stays clear of subnormals.
-template <class T> constexpr float kShift = 0.0f;
-template <> constexpr float kShift<__half> = 12.0f;
+// Probabilities, and with them sums and outputs of a job, are kept times this:
+// two fp16 terms then hold 22 bits of one down to 2^-29.
+template <class T> constexpr float kScaleP = 1.0f;
+template <> constexpr float kScaleP<__half> = 0x1p15f;
+// Those below (scaled: the least normal fp16) take a pass of their own, 2^29
+// times as large, and those below 2^-58 a third.
+constexpr float kLeastP = 0x1p-14f, kPassP = 0x1p29f;
 
 constexpr int kTogether = 4;   // chains of products at a time
 constexpr int kLookup = 4 * 128 + 32;   // bytes of a producer's page ids and live slots
@@ -195,11 +203,11 @@ struct Warp {
                     for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(v[k][j]));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                // Largest |q| to [2^10, 2^11); nothing to scale in zeros, NaN and infinities.
+                // Largest |q| to [2^14, 2^15); nothing to scale in zeros, NaN and infinities.
                 int e = (int)(__float_as_uint(top) >> 23) - 127;
-                e = e == 128 || top == 0.0f ? 10 : e < -100 ? -100 : e;
-                const float up = __uint_as_float((uint32_t)(10 - e + 127) << 23);
-                const float down = __uint_as_float((uint32_t)(e - 10 + 127) << 23);
+                e = e == 128 || top == 0.0f ? 14 : e < -100 ? -100 : e;
+                const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
+                const float down = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
                 unscale[n][0] = __shfl_sync(0xffffffffu, down, 8 * t);
                 unscale[n][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
 #pragma unroll
@@ -237,6 +245,19 @@ struct Warp {
         const int at = ((k * NT + n) * kTermsN + i) * 2 + b;
         if constexpr (S::kQReg) return qr[at];
         else return qs[at * 32 + (threadIdx.x & 31)];
+    }
+
+    // Sums of products of one term, on the scale of the next greater one.
+    template <int N>
+    static __device__ __forceinline__ void next_term(float (&c)[N][NT][4]) {
+        if constexpr (kStep<T> != 1.0f) {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) c[k][n][j] *= 1.0f / kStep<T>;
+        }
     }
 
     // One tile of 16 slots, K rows at `tile` and V rows at `vbase`; bit r of
@@ -283,9 +304,11 @@ struct Warp {
                     for (int k = 0; k < KB; ++k) product(false, k, a[k], i);
             } else {
 #pragma unroll
-                for (int i = 0; i < kTermsN; ++i)
+                for (int i = 0; i < kTermsN; ++i) {
 #pragma unroll
                     for (int k = 0; k < KB; ++k) product(i == 0 && k < KT, k, a[k], i);
+                    if (i + 1 < kTermsN) next_term(c);
+                }
             }
 #pragma unroll
             for (int k = 0; k < KT; ++k)
@@ -295,7 +318,6 @@ struct Warp {
                     for (int j = 0; j < 4; ++j) s[n][j] = k0 + k == 0 ? c[k][n][j] : s[n][j] + c[k][n][j];
         }
         const bool up = live >> g & 1, dn = live >> (g + 8) & 1;
-        uint32_t p16[NT][kTermsN][2];   // 16-bit types: terms of P^T, as the product wants them
         float alpha[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -320,47 +342,83 @@ struct Warp {
                 top = fmaxf(top, m[n][j]);
                 alpha[n][j] = power2(m[n][j] - top);
                 m[n][j] = top;
-                const float ref = top - kShift<T>;
-                s[n][j] = power2(s[n][j] - ref);
-                s[n][2 + j] = power2(s[n][2 + j] - ref);
+                s[n][j] = power2(s[n][j] - top) * kScaleP<T>;
+                s[n][2 + j] = power2(s[n][2 + j] - top) * kScaleP<T>;
                 l[n][j] = fmaf(l[n][j], alpha[n][j], s[n][j] + s[n][2 + j]);
-            }
-            if constexpr (sizeof(T) == 2) {
-                uint32_t x[kTermsN], y[kTermsN];
-                split2<T, kTermsN>(s[n][0], s[n][1], x);
-                split2<T, kTermsN>(s[n][2], s[n][3], y);
-#pragma unroll
-                for (int i = 0; i < kTermsN; ++i) p16[n][i][0] = transpose8(x[i]), p16[n][i][1] = transpose8(y[i]);
             }
         }
         if constexpr (sizeof(T) == 2) {
             // Slots (lane / 16) * 8 + lane % 8, channels 16 i + 8 (lane / 8 % 2).
             const uint32_t at = vbase + chunk_at<kBlock>((lane >> 4) * 8 + (lane & 7), lane >> 3 & 1);
-#pragma unroll
-            for (int i0 = 0; i0 < DP / 16; i0 += KT) {
-                uint32_t a[KT][4];
-                float c[KT][NT][4];
-#pragma unroll
-                for (int i = 0; i < KT; ++i) {
-                    ldm4t(a[i], (at ^ (2 * (i0 + i) % 8 << 4)) + (2 * (i0 + i) / 8) * kBlock);
-                }
-#pragma unroll
-                for (int x = 0; x < kTermsN; ++x)
-#pragma unroll
-                    for (int i = 0; i < KT; ++i)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            if (x == 0) mma0(c[i][n], a[i], p16[n][x][0], p16[n][x][1], T());
-                            else mma(c[i][n], a[i], p16[n][x][0], p16[n][x][1], T());
-                        }
-#pragma unroll
-                for (int i = 0; i < KT; ++i)
+            int pass = 0;
+            float up = 1.0f;   // fp16: of the pass
+            if constexpr (kScaleP<T> != 1.0f) {
+                auto below = [&](float least) {   // any of (0, least)?
+                    bool any = false;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            o[n][i0 + i][j] = fmaf(o[n][i0 + i][j], alpha[n][j & 1], c[i][n][j]);
+                        for (int j = 0; j < 4; ++j) any |= __float_as_uint(s[n][j]) - 1 < __float_as_uint(least) - 1;
+                    return __any_sync(0xffffffffu, any);
+                };
+                if (below(kLeastP)) {   // the smallest first: outputs are scaled for them and back
+                    pass = below(kLeastP / kPassP) ? 2 : 1;
+                    up = pass == 2 ? kPassP * kPassP : kPassP;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) alpha[n][0] *= up, alpha[n][1] *= up;
+                }
             }
+            const int first = pass;
+            do {
+                uint32_t p16[NT][kTermsN][2];   // terms of P^T, as the product wants them
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float v[4] = {s[n][0], s[n][1], s[n][2], s[n][3]};
+                    if (kScaleP<T> != 1.0f && first > 0) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            v[j] *= up;
+                            if ((pass > 0 && v[j] >= kLeastP * kPassP) || (pass < first && v[j] < kLeastP)) v[j] = 0.0f;
+                        }
+                    }
+                    uint32_t x[kTermsN], y[kTermsN];
+                    split2<T, kTermsN>(v[0], v[1], x);
+                    split2<T, kTermsN>(v[2], v[3], y);
+#pragma unroll
+                    for (int i = 0; i < kTermsN; ++i) p16[n][i][0] = transpose8(x[i]), p16[n][i][1] = transpose8(y[i]);
+                }
+#pragma unroll
+                for (int i0 = 0; i0 < DP / 16; i0 += KT) {
+                    uint32_t a[KT][4];
+                    float c[KT][NT][4];
+#pragma unroll
+                    for (int i = 0; i < KT; ++i) {
+                        ldm4t(a[i], (at ^ (2 * (i0 + i) % 8 << 4)) + (2 * (i0 + i) / 8) * kBlock);
+                    }
+#pragma unroll
+                    for (int x = 0; x < kTermsN; ++x) {
+#pragma unroll
+                        for (int i = 0; i < KT; ++i)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                if (x == 0) mma0(c[i][n], a[i], p16[n][x][0], p16[n][x][1], T());
+                                else mma(c[i][n], a[i], p16[n][x][0], p16[n][x][1], T());
+                            }
+                        if (x + 1 < kTermsN) next_term(c);
+                    }
+#pragma unroll
+                    for (int i = 0; i < KT; ++i)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                o[n][i0 + i][j] = fmaf(o[n][i0 + i][j], alpha[n][j & 1], c[i][n][j]);
+                }
+                if constexpr (kScaleP<T> == 1.0f) break;
+                up *= 1.0f / kPassP;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) alpha[n][0] = alpha[n][1] = 1.0f / kPassP;
+            } while (--pass >= 0);
         } else {
             // By step of 8 slots; the step's row t is slot 2t, row t + 4 slot 2t + 1.
             uint32_t ph[NT][2][2], pl[NT][2][2];
@@ -881,7 +939,11 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) wp.l[n][j] += __shfl_xor_sync(0xffffffffu, wp.l[n][j], x);
-                wp.m[n][j] -= kShift<T>;
+                if constexpr (kScaleP<T> != 1.0f) {
+                    wp.l[n][j] *= 1.0f / kScaleP<T>;
+#pragma unroll
+                    for (int x = 0; x < DP / 16; ++x) wp.o[n][x][j] *= 1.0f / kScaleP<T>, wp.o[n][x][2 + j] *= 1.0f / kScaleP<T>;
+                }
             }
         auto put = [&](int slot) {
 #pragma unroll

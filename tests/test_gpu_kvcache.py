@@ -623,3 +623,46 @@ def test_attention_counts_live_infinities_as_nan(lens, heads, kv, dim, page, lay
         if not torch.isfinite(keep).all():
             bad.append((slot, "left out"))
     assert not bad, bad
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("lens,heads,kv,dim,page", [([300, 40], 8, 1, 64, 16), ([300, 40], 24, 2, 128, 5),
+                                                    ([5000, 700], 16, 8, 128, 16), ([900, 40], 12, 1, 256, 8)])
+@pytest.mark.parametrize("depth", [12.0, 20.0, 28.0, 45.0])
+def test_attention_of_small_probabilities(lens, heads, kv, dim, page, depth, typ):
+    """One slot with a value of zero takes nearly all of the weight: the output is
+    what the others' probabilities of about e^-depth make of theirs."""
+    g = gen(31)
+    c = make(lens, kv, dim, page, typ, seed=3, poison=False)
+    q = torch.randn(len(lens), heads, dim, generator=g, device="cuda")
+    q[..., 0] = 4.0
+    c.k[..., 0] = 0.0
+    for i, n in enumerate(lens):
+        page_of = int(c.table[i, (n // 3) // page]), slice(None), (n // 3) % page
+        c.k[page_of] = 0.0
+        c.k[(*page_of, 0)] = depth * dim ** 0.5 / 4.0
+        c.v[page_of] = 0.0
+    c.weight.zero_()
+    want, tol, weights = reference(c, q, dim ** -0.5)
+    out = c.attend(q, torch.tensor(lens, dtype=torch.int32, device="cuda"), max(lens))
+    assert ((out.double() - want).abs() <= tol).all(), float(((out.double() - want).abs() / tol).max())
+    for i, n in enumerate(lens):
+        w, wt = weights[i]
+        assert ((rows(c, c.weight, i, n) - w).abs() <= wt).all()
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("lens,heads,kv,dim,page", [([300, 40], 8, 1, 64, 16), ([300, 40], 24, 2, 128, 5),
+                                                    ([900, 40], 12, 1, 256, 8)])
+@pytest.mark.parametrize("spread", [14, 20, 26])
+def test_attention_of_queries_with_a_wide_spread(lens, heads, kv, dim, page, spread, typ):
+    """A channel 2^spread above the others meets keys of zero: the score is the others'."""
+    g = gen(33)
+    c = make(lens, kv, dim, page, typ, seed=4, poison=False)
+    q = torch.randn(len(lens), heads, dim, generator=g, device="cuda") * 2.0 ** -12
+    q[..., 5] = 2.0 ** (spread - 12)
+    c.k[:] = (c.k.float() * 2.0 ** 13).to(c.k.dtype)
+    c.k[..., 5] = 0.0
+    want, tol, _ = reference(c, q, dim ** -0.5)
+    out = c.attend(q, torch.tensor(lens, dtype=torch.int32, device="cuda"), max(lens))
+    assert ((out.double() - want).abs() <= tol).all(), float(((out.double() - want).abs() / tol).max())
