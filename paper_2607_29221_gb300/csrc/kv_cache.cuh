@@ -62,7 +62,9 @@ inline mosaic_status kv_check(const mosaic_kv_cache *c) {
         c->page_size < 1 || c->page_size > 65536 || c->pages < 1 || c->pages > 0x7fffffff || c->seqs < 0 ||
         c->seqs > (1 << 24) || c->table_cols < 1 || c->table_cols > 0x7fffffff || c->ld_table < c->table_cols)
         return MOSAIC_ERR_SHAPE;
-    if (c->table_cols * c->page_size > 0x7fffffff) return MOSAIC_ERR_SHAPE;
+    // Slots are counted in 31 bits, also at the end of a unit or group of look-ups (512 slots at
+    // most) that begins inside a sequence.
+    if (c->table_cols * c->page_size > ((int64_t)1 << 31) - 1024) return MOSAIC_ERR_SHAPE;
     if (c->page_stride < 0 || c->head_stride < 0 || c->slot_stride < 0) return MOSAIC_ERR_SHAPE;
     if (!c->k || !c->v || !c->table) return MOSAIC_ERR_ARG;
     const int64_t unit = 16 / kv_element_bytes(c->type);

@@ -252,3 +252,16 @@ def test_calls_refuse_while_another_device_is_current(lib, monkeypatch, call):
     with pytest.raises(ValueError, match="not the current one"):
         run()
     assert len(calls) == 1
+
+
+@pytest.mark.parametrize("slots,status", [((1 << 31) - 1, SHAPE), ((1 << 31) - 1023, SHAPE), ((1 << 31) - 1024, OK)])
+def test_slots_are_counted_in_31_bits(lib, slots, status):
+    """A unit of slots that begins inside a sequence must end below 2^31 too.  No compute call is made: the refused
+    calls fail validation, and an accepted cache is only asked for its workspace."""
+    c = cache(kv_heads=1, head_dim=8, page_size=1, table_cols=slots, ld_table=slots, page_stride=8, head_stride=8,
+              slot_stride=8)
+    r = ctypes.byref(c)
+    assert (lib.mosaic_kv_evict_workspace(r, slots, 5) > 0) == (status == OK)
+    assert (lib.mosaic_kv_attention_workspace(r, 1, slots) > 0) == (status == OK)
+    if status != OK:
+        assert attention(lib, c, heads=1, ldq=8, ldo=8) == append(lib, c, heads=1) == evict(lib, c) == status
