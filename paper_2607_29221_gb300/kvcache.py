@@ -11,9 +11,10 @@ call on the current stream:
   out   = cache.attend(q, lens, max_len)
   lens  = cache.evict(lens, max_len, keep, recent_from=recent_from)
 
-Arguments are tensors on the cache's device.  Scratch is kept for each stream
-and host thread (5 us a call to allocate it anew); calls that are captured into
-a graph get scratch of their own, since the graph may run beside anything.
+Arguments are tensors on the cache's device.  Scratch is kept for the last few
+streams of each host thread until the thread ends (5 us a call to allocate it
+anew); calls that are captured into a graph get scratch of their own, since the
+graph may run beside anything.
 ``PageTable`` is the host's account of which page belongs to whom.
 """
 from __future__ import annotations
@@ -25,6 +26,7 @@ import torch
 
 from . import mosaic as M
 
+_STREAMS = 4   # streams of a host thread whose scratch is kept
 _TYPES = {torch.float32: M.KV_F32, torch.bfloat16: M.KV_BF16, torch.float16: M.KV_F16}
 
 
@@ -113,7 +115,7 @@ class PagedCache:
         self._ref = ctypes.byref(self._c)
         lib = M.lib()
         self._calls = lib.mosaic_kv_append, lib.mosaic_kv_attention, lib.mosaic_kv_evict
-        self._ws, self._scratch = {}, {}
+        self._ws, self._scratch = {}, threading.local()
 
     @classmethod
     def empty(cls, pages: int, kv_heads: int, page_size: int, head_dim: int, table, dtype=torch.bfloat16,
@@ -143,10 +145,13 @@ class PagedCache:
             return None
         if torch.cuda.is_current_stream_capturing():
             return torch.empty(need, dtype=torch.uint8, device=self.device)
-        key = stream, threading.get_ident()
-        ws = self._scratch.get(key)
+        held = self._scratch.__dict__   # the host thread's, by stream; it ends with the thread
+        ws = held.get(stream)
         if ws is None or ws.numel() < need:
-            ws = self._scratch[key] = torch.empty(need, dtype=torch.uint8, device=self.device)
+            held.pop(stream, None)
+            if len(held) >= _STREAMS:   # the allocator reuses it in its own stream's order
+                held.pop(next(iter(held)))
+            ws = held[stream] = torch.empty(need, dtype=torch.uint8, device=self.device)
         return ws
 
     def read(self, seq: int, n: int):

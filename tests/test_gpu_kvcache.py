@@ -666,3 +666,27 @@ def test_attention_of_queries_with_a_wide_spread(lens, heads, kv, dim, page, spr
     want, tol, _ = reference(c, q, dim ** -0.5)
     out = c.attend(q, torch.tensor(lens, dtype=torch.int32, device="cuda"), max(lens))
     assert ((out.double() - want).abs() <= tol).all(), float(((out.double() - want).abs() / tol).max())
+
+
+def test_scratch_ends_with_its_thread_and_streams():
+    """Host threads that have ended leave nothing behind, and a thread keeps the scratch of a few streams only."""
+    import threading
+    c = make([3000, 1700], 8, 64, 16, "bf16", seed=13)
+    n = torch.tensor([3000, 1700], dtype=torch.int32, device="cuda")
+    q = torch.randn(2, 64, 64, generator=gen(1), device="cuda")
+    out = torch.empty_like(q)
+    c.attend(q, n, 3000, out=out)
+    before = torch.cuda.memory_allocated()
+    for _ in range(4):
+        t = threading.Thread(target=lambda: c.attend(q, n, 3000, out=out))
+        t.start()
+        t.join()
+    assert torch.cuda.memory_allocated() == before
+    used = []
+    for stream in [torch.cuda.Stream() for _ in range(12)]:
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            c.attend(q, n, 3000, out=out)
+        stream.synchronize()
+        used.append(torch.cuda.memory_allocated())
+    assert used[-1] == used[5] and used[-1] - before <= 4 * (used[0] - before)
