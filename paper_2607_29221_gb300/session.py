@@ -22,8 +22,8 @@ from .decoder import SecureDecoderLayer
 
 class DecodeSession:
     """``keep``: slots a sequence may hold (None: no eviction); it may run over
-    by ``slack`` slots before it is cut back, without the ``recent`` newest
-    tokens.  ``rope``: its positions are the tokens' ordinals (one axis);
+    by ``slack`` slots (up to max_len) before it is cut back, without the
+    ``recent`` newest tokens.  ``rope``: its positions are the tokens' ordinals (one axis);
     default: the usual rotation of the whole head at base 500000."""
 
     def __init__(self, layer: SecureDecoderLayer, seqs: int, max_len: int, page_size: int = 16,
@@ -83,7 +83,8 @@ class DecodeSession:
         self.lens += 1
         self.seen += 1
         self.host_lens = [n + 1 for n in self.host_lens]
-        if self.keep is not None and after > self.keep + self.slack:
+        # No further step would fit at max_len.
+        if self.keep is not None and after > min(self.keep + self.slack, self.max_len - 1):
             self.cache.evict(self.lens, after, self.keep, recent_from=self.seen - self.recent, new_lens=self.lens)
             self.host_lens = [min(n, self.keep) for n in self.host_lens]
             for i, n in enumerate(self.host_lens):

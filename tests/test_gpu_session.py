@@ -121,3 +121,20 @@ def test_refusals(layer):
         ses.prefill(0, x[:1])
     with pytest.raises(ValueError):
         ses.step(x[:1])
+
+
+def test_a_budget_is_cut_back_at_max_len(layer):
+    """A slack that reaches past max_len does not end the session there."""
+    from paper_2607_29221_gb300.session import DecodeSession
+    ses = DecodeSession(layer, 1, 16, page_size=8, keep=12, recent=3, slack=10)
+    x = torch.from_numpy(wl.activations(40, SHAPE["hidden"], seed=72)).cuda()
+    ses.prefill(0, x[:5])
+    held = []
+    for t in range(30):
+        assert torch.isfinite(ses.step(x[5 + t:6 + t])).all()
+        held.append(ses.host_lens[0])
+    assert max(held) == 15 and held[-1] == int(ses.lens) and int(ses.seen) == 35
+    full = DecodeSession(layer, 1, 8, page_size=4, keep=8)      # a budget of max_len: nothing can leave
+    full.prefill(0, x[:8])
+    with pytest.raises(ValueError):
+        full.step(x[:1])
