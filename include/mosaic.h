@@ -613,6 +613,7 @@ typedef enum { MOSAIC_KV_F32 = 0, MOSAIC_KV_BF16 = 1, MOSAIC_KV_F16 = 2 } mosaic
  * gathered so far.
  * head_dim: a multiple of 8, 8..256.  page_size: 1..65536.  table_cols
  * page_size <= 2^31 - 1024.  k, v and the three strides in bytes: multiples of 16.
+ * table may be NULL without sequences (seqs 0).
  * The struct is a host struct of device pointers, read during the call only.
  * Kernels check every slot against table_cols and every page id against
  * `pages`: a slot without a page is skipped when written and masked when read.

@@ -66,7 +66,7 @@ inline mosaic_status kv_check(const mosaic_kv_cache *c) {
     // most) that begins inside a sequence.
     if (c->table_cols * c->page_size > ((int64_t)1 << 31) - 1024) return MOSAIC_ERR_SHAPE;
     if (c->page_stride < 0 || c->head_stride < 0 || c->slot_stride < 0) return MOSAIC_ERR_SHAPE;
-    if (!c->k || !c->v || !c->table) return MOSAIC_ERR_ARG;
+    if (!c->k || !c->v || (!c->table && c->seqs > 0)) return MOSAIC_ERR_ARG;
     const int64_t unit = 16 / kv_element_bytes(c->type);
     if (!aligned16(c->k) || !aligned16(c->v) || c->page_stride % unit || c->head_stride % unit || c->slot_stride % unit)
         return MOSAIC_ERR_ALIGN;

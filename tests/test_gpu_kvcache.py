@@ -690,3 +690,18 @@ def test_scratch_ends_with_its_thread_and_streams():
         stream.synchronize()
         used.append(torch.cuda.memory_allocated())
     assert used[-1] == used[5] and used[-1] - before <= 4 * (used[0] - before)
+
+
+def test_an_empty_batch():
+    """No sequences: attention and eviction have nothing to do, an append only rotates."""
+    from paper_2607_29221_gb300 import kvcache as KV
+    c = make([20], 2, 64, 16, "bf16")
+    e = KV.PagedCache(c.k, c.v, c.table[:0], c.position, c.weight)
+    n = torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert e.attend(torch.zeros(0, 4, 64, device="cuda"), n, 20).shape == (0, 4, 64)
+    assert e.evict(n, 20, 10).shape == (0,)
+    before = c.weight.clone()
+    x, i = torch.randn(3, 8 * 64, generator=gen(2), device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    assert torch.equal(e.append(x, 4, i, i, i), x[:, :256].unflatten(1, (4, 64)))
+    assert torch.equal(c.weight, before)
+    assert e.append(x[:0], 4, n, n, n).shape == (0, 4, 64)

@@ -265,3 +265,9 @@ def test_slots_are_counted_in_31_bits(lib, slots, status):
     assert (lib.mosaic_kv_attention_workspace(r, 1, slots) > 0) == (status == OK)
     if status != OK:
         assert attention(lib, c, heads=1, ldq=8, ldo=8) == append(lib, c, heads=1) == evict(lib, c) == status
+
+
+def test_a_cache_without_sequences_needs_no_table(lib):
+    c = cache(seqs=0, table=None)
+    assert attention(lib, c) == evict(lib, c) == append(lib, c, l=0) == OK
+    assert lib.mosaic_kv_evict_workspace(ctypes.byref(c), 300, 100) == 0
