@@ -169,8 +169,8 @@ class SecureDecoderLayer:
             masks = self.init_x(x.shape[0])
         mark("glue")
         h = rmsnorm(x, s.eps)
-        qkv = self._linear(0, h, masks[0], mark, compose)
-        a = attention(qkv, s) if attend is None else attend(qkv)
+        attend = attend or (lambda qkv: attention(qkv, s))
+        a = attend(self._linear(0, h, masks[0], mark, compose))   # the QKV rows end here
         x = x + self._linear(1, a, masks[1], mark, compose)
         gu = self._linear(2, rmsnorm(x, s.eps), masks[2], mark, compose)
         act = swiglu(gu, s.ffn)

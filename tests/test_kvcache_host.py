@@ -271,3 +271,27 @@ def test_a_cache_without_sequences_needs_no_table(lib):
     c = cache(seqs=0, table=None)
     assert attention(lib, c) == evict(lib, c) == append(lib, c, l=0) == OK
     assert lib.mosaic_kv_evict_workspace(ctypes.byref(c), 300, 100) == 0
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_a_layer_keeps_no_qkv_rows_past_its_attention(monkeypatch, given):
+    """The largest intermediate of a pass but one: its memory is free for the linears that follow.  The layer's parts
+    are stand-ins on host tensors."""
+    torch = pytest.importorskip("torch")
+    import weakref
+    from paper_2607_29221_gb300 import decoder as D
+    layer, seen = object.__new__(D.SecureDecoderLayer), []
+    layer.s = D.LayerShape(hidden=8, n_heads=2, n_kv=1, head_dim=4, ffn=8)
+    monkeypatch.setattr(D, "rmsnorm", lambda x, eps: x * 1.0)
+    monkeypatch.setattr(D, "swiglu", lambda gu, ffn: gu[:, :ffn] * 1.0)
+
+    def linear(i, x, masks, mark, compose):
+        if i == 1:
+            assert seen[0]() is None
+        y = torch.ones(x.shape[0], (16, 8, 16, 8)[i])
+        seen.append(weakref.ref(y))
+        return y
+    layer._linear = linear
+    attend = (lambda qkv: qkv[:, :8] * 2.0) if given else None
+    y = layer.forward(torch.ones(3, 8), masks=[None] * 4, attend=attend)
+    assert y.shape == (3, 8) and len(seen) == 4
