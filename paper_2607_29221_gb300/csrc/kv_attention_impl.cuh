@@ -828,7 +828,7 @@ struct Producer {
         copies_arrive(pipe.full + stage);
         if (lane == 0) mbar_arrive(pipe.full + stage);   // with the stage's live slots and unit
     }
-    // After an abort: nothing in flight may outlive the block.
+    // Nothing in flight may outlive the block, should the consumers have given up.
     __device__ __forceinline__ void drain() {
         if constexpr (TMA) {
             for (int c = max(0, count - S::kStages); c < count; ++c)
@@ -885,8 +885,8 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
         if (!producer.run()) {
             *(volatile int *)&pipe.aborted = 1;   // results are void; the device status says so
             if (lane == 0) atomicExch(&g_attend_error, 1u);
-            producer.drain();
         }
+        producer.drain();
         return;
     }
 
