@@ -691,6 +691,7 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
  * key/value head the lens[i] - keep slots of the least (weight, slot) leave.
  * With recent_from (seqs entries; needs cache->position) a slot whose position
  * is >= recent_from[i] ranks as +inf; a NaN weight ranks as -inf, and -0 as 0.
+ * A slot without a page ranks as +inf, and a move from or to one is left out.
  * The k-th slot below keep that left takes key, value, position and weight of
  * the k-th slot from keep on that stayed (both in ascending order): the least
  * rows that can move do.  Heads choose for themselves, so position differs

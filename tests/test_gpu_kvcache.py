@@ -705,3 +705,106 @@ def test_an_empty_batch():
     assert torch.equal(e.append(x, 4, i, i, i), x[:, :256].unflatten(1, (4, 64)))
     assert torch.equal(c.weight, before)
     assert e.append(x[:0], 4, n, n, n).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+def test_append_of_more_tokens_than_a_grid_axis_holds(typ):
+    l = 70001
+    c = make([l], 1, 8, 16, typ, poison=False)
+    qkv = torch.randn(l, 24, generator=gen(41), device="cuda")
+    i = torch.arange(l, dtype=torch.int32, device="cuda")
+    slot = i.flip(0).contiguous()
+    q = c.append(qkv, 1, torch.zeros_like(i), slot, i + 5)
+    assert torch.equal(q[:, 0], qkv[:, :8])
+    back = qkv.flip(0)
+    assert torch.equal(rows(c, c.k, 0, l)[0], back[:, 8:16].to(TYPES[typ]).double())
+    assert torch.equal(rows(c, c.v, 0, l)[0], back[:, 16:].to(TYPES[typ]).double())
+    assert torch.equal(rows(c, c.position, 0, l)[0], (i + 5).flip(0).double())
+
+
+def test_a_captured_step_equals_the_eager_one():
+    """append, attend and evict in one graph, replayed with other inputs."""
+    lens = [90, 64, 1]
+
+    def step(c, qkv, seq, n, out, new):
+        q = c.append(qkv, 8, seq, n, n)
+        c.attend(q, n + 1, 101, out=out)
+        c.evict(n + 1, 101, 64, recent_from=n - 8, new_lens=new)
+    results = []
+    for graphed in (False, True):
+        c = make([v + 10 for v in lens], 2, 64, 16, "bf16", seed=6, poison=False)
+        c.position.copy_(torch.arange(c.position.numel(), device="cuda").reshape(c.position.shape) % 97)
+        seq = torch.arange(3, dtype=torch.int32, device="cuda")
+        qkv, n = torch.zeros(3, 12 * 64, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+        out, new = torch.zeros(3, 8, 64, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+        pools = (c.k, c.v, c.position, c.weight)
+        kept = [x.clone() for x in pools]
+        if graphed:
+            n.copy_(torch.tensor(lens, dtype=torch.int32))
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step(c, qkv, seq, n, out, new)
+            assert all(torch.equal(x, y) for x, y in zip(pools, kept))
+        got = []
+        for turn in range(3):
+            qkv.copy_(torch.randn(3, 12 * 64, generator=gen(50 + turn), device="cuda"))
+            n.copy_(torch.tensor(lens, dtype=torch.int32) if turn == 0 else new)
+            graph.replay() if graphed else step(c, qkv, seq, n, out, new)
+            got += [x.clone() for x in (out, new, *pools)]
+        results.append(got)
+    assert results[0][1].tolist() == [64, 64, 2]
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("lens,keep", [([300], 200), ([3000, 2100], 1500), ([70001], 35000)])
+def test_evict_leaves_slots_without_a_page(lens, keep):
+    """They rank as +inf; a move from or to one is left out."""
+    kv, dim, page = 2, 16, 16
+    c = make(lens, kv, dim, page, "bf16", seed=8, poison=False)
+    for i, n in enumerate(lens):
+        c.table[i, : -(-n // page): 5] = -1
+    w = torch.rand(c.weight.shape, generator=gen(9), device="cuda")
+    c.weight.copy_(w)
+    want = [x.clone() for x in (c.k, c.v, c.position, c.weight)]
+    for i, n in enumerate(lens):
+        ids = c.table[i, : -(-n // page)].long().cpu().numpy()
+        at, off = ids[np.arange(n) // page], np.arange(n) % page
+        for h in range(kv):
+            rank = np.where(at < 0, np.inf, c.weight[:, h].cpu().numpy()[at, off])
+            gone = np.zeros(n, dtype=bool)
+            gone[np.argsort(rank, kind="stable")[: n - keep]] = True
+            to, frm = np.flatnonzero(gone[:keep]), keep + np.flatnonzero(~gone[keep:])
+            real = (at[to] >= 0) & (at[frm] >= 0)
+            to, frm = to[real], frm[real]
+            for x, y in zip(want, (c.k, c.v, c.position, c.weight)):
+                x[at[to], h, off[to]] = y[at[frm], h, off[frm]]
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    assert c.evict(n, max(lens), keep).tolist() == [keep] * len(lens)
+    for x, y in zip(want, (c.k, c.v, c.position, c.weight)):
+        assert torch.equal(x, y)
+
+
+def test_library_calls_equal_the_handle():
+    from paper_2607_29221_gb300 import kvcache as KV
+    from paper_2607_29221_gb300 import mosaic as M
+    lens, results = [70, 33], []
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    seq = torch.arange(2, dtype=torch.int32, device="cuda")
+    qkv = torch.randn(2, 8 * 64, generator=gen(14), device="cuda")
+    rope, pos = KV.Rope(64), torch.tensor([70, 33], dtype=torch.int32, device="cuda")
+    for direct in (False, True):
+        c = make([80, 80], 2, 64, 16, "f16", seed=15, poison=False)
+        q, out = torch.empty(2, 4, 64, device="cuda"), torch.empty(2, 4, 64, device="cuda")
+        new = torch.empty_like(n)
+        if direct:
+            scratch = lambda size: torch.empty(max(size, 256), dtype=torch.uint8, device="cuda")
+            M.mosaic_kv_append(c._c, qkv, 512, 2, 4, seq, n, pos, rope.at(pos), q, 256)
+            M.mosaic_kv_attention(c._c, q, 256, 4, n, 70, None, 0.125, 0.5, out, 256,
+                                  scratch(M.mosaic_kv_attention_workspace(c._c, 4, 70)))
+            M.mosaic_kv_evict(c._c, n, 70, 40, None, new, scratch(M.mosaic_kv_evict_workspace(c._c, 70, 40)))
+        else:
+            c.append(qkv, 4, seq, n, pos, rope=rope, pos=pos, out=q)
+            c.attend(q, n, 70, decay=0.5, out=out)
+            c.evict(n, 70, 40, new_lens=new)
+        results.append([x.clone() for x in (q, out, new, c.k, c.v, c.position, c.weight)])
+    assert all(torch.equal(a, b) for a, b in zip(*results))

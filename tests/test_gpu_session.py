@@ -138,3 +138,44 @@ def test_a_budget_is_cut_back_at_max_len(layer):
     full.prefill(0, x[:8])
     with pytest.raises(ValueError):
         full.step(x[:1])
+
+
+def test_attention_after_evictions(layer, monkeypatch):
+    """Every step of a session over its budget: each cached row is the one that was appended at its position, and
+    the outputs are the 64-bit attention over those rows.  Tolerance: scores to 2^-20 of their terms, probabilities
+    to twice that and 2^-19, as for the operator alone."""
+    from paper_2607_29221_gb300.session import DecodeSession
+    keep, page, H, KV, d = 20, 8, SHAPE["n_heads"], SHAPE["n_kv"], SHAPE["head_dim"]
+    ses = DecodeSession(layer, 2, 64, page_size=page, keep=keep, recent=5, slack=2)
+    cache, made, attend, worst = ses.cache, {}, ses.cache.attend, []
+
+    def rows(pool, i, n):
+        ids = cache.table[i, : -(-n // page)].long()
+        return pool[ids].transpose(0, 1).flatten(1, 2)[:, :n]
+
+    def note(i, n):                      # rows appended since the last step
+        k, v, at = (rows(x, i, n).cpu() for x in (cache.k, cache.v, cache.position))
+        for h in range(KV):
+            for s in range(n):
+                row = k[h, s], v[h, s]
+                old = made.setdefault((i, h, int(at[h, s])), row)
+                assert torch.equal(old[0], row[0]) and torch.equal(old[1], row[1])
+
+    def checked(q, lens, most):
+        out = attend(q, lens, most)
+        for i, n in enumerate(lens.tolist()):
+            note(i, n)
+            k, v = rows(cache.k, i, n).double(), rows(cache.v, i, n).double()
+            x = q[i].double().reshape(KV, -1, d)
+            p = torch.softmax(x @ k.transpose(1, 2) * d ** -0.5, 2)
+            rel = 2.0 ** -19 * (1 + (x.abs() @ k.abs().transpose(1, 2) * d ** -0.5).amax(2, keepdim=True))
+            err = (out[i].double().reshape(KV, -1, d) - p @ v).abs()
+            assert (err <= rel * (p @ v.abs())).all()
+        worst.append(max(lens.tolist()))
+        return out
+    monkeypatch.setattr(cache, "attend", checked)
+    x = torch.from_numpy(wl.activations(100, SHAPE["hidden"], seed=75)).cuda()
+    ses.prefill(0, x[:17])
+    for t in range(25):
+        ses.step(x[20 + 2 * t: 22 + 2 * t])
+    assert max(worst) == keep + 3 and ses.host_lens[0] >= keep
