@@ -16,7 +16,12 @@ constexpr int kMaxGroup = 64;
 // 12 / 13, 13 / 18, 17 / 24, 27 / 36, 23 / 26; 1024: 20 / 15, 22 / 24, 27 / 35,
 // 47 / 56, 40 / 36; 2048: 35 / 19, 38 / 34, 47 / 55, 85 / 95, 67 / 57.  Long rows
 // earlier: fp32, one sequence 256 slots 11 / 14, 512: 17 / 15; 64 of spread
-// lengths 512: 47 / 47, 1024: 75 / 68.
+// lengths 512: 47 / 47, 1024: 75 / 68.  The rule is that of instances of two or
+// three blocks an SM.  Those of one (full lengths, one sequence / 16 / 64): bf16
+// heads of 256, 256 slots 10 / 14, 14 / 24, 54 / 61, 512: 15 / 14, 20 / 32, 76 / 80,
+// 1024: 25 / 14, 29 / 44, 117 / 121; 16 query heads of 128, 512: 18 / 21, 19 / 26, 44
+// / 60, 1024: 25 / 22, 28 / 31, 56 / 79; fp32 heads of 128, 512: 16 / 13, 18 / 26, 46 /
+// 60, 1024: 27 / 14, 29 / 36, 83 / 96: it shares some that are faster whole.
 constexpr int64_t kWholeFew = 512, kWholeMany = 1024, kManyJobs = 128, kWholeBytes = 128 * 1024;
 // Heads share a unit (the blocks' warps then have a head each and nothing to
 // merge) while so many jobs remain to be shared out; whole jobs while there is

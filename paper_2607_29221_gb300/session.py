@@ -7,6 +7,10 @@ loop does: the four linears of a layer are outsourced as in
 token of each sequence: append with rotary positions, attention over the
 pages, and, past a budget of slots, eviction by gathered attention weight.
 
+Prompts are for empty sequences, and a step takes all sequences together.
+Weights are gathered by steps only: a prompt longer than the budget is cut by
+the weights of the first step after it.
+
   session = DecodeSession(layer, seqs=4, max_len=4096, keep=1024, recent=128)
   session.prefill(0, x0)              # tokens x hidden of sequence 0
   y = session.step(x)                 # seqs x hidden: one token each
