@@ -600,18 +600,33 @@ mosaic_status mosaic_freivalds_check(int k, const uint32_t *a, const uint32_t *Y
 /* attention stays on the trusted side, so its cache does too).              */
 /* ------------------------------------------------------------------------ */
 /* Element types of cached keys and values. */
-typedef enum { MOSAIC_KV_F32 = 0, MOSAIC_KV_BF16 = 1, MOSAIC_KV_F16 = 2 } mosaic_kv_type;
+typedef enum { MOSAIC_KV_F32 = 0, MOSAIC_KV_BF16 = 1, MOSAIC_KV_F16 = 2, MOSAIC_KV_Q4 = 4 } mosaic_kv_type;
+
+/* Rows of MOSAIC_KV_Q4: head_dim (a multiple of 32) codes of 4 bits, channel c
+ * in bits 4 (c % 2) of byte c / 2; then, for every 32 channels, a step and a
+ * base in fp16; padded to a multiple of 16 bytes (the padding is neither read
+ * nor written, but for the move of whole rows by mosaic_kv_evict).  A channel
+ * stands for base + code step, rounded once to fp16.  A row is written from
+ * fp32 channels y by IEEE operations, each rounded to nearest on its own, so
+ * that its bytes do not depend on the run: y is cut to +-65000; base = the
+ * least of the 32, rounded to fp16; step = (greatest - least) (1/15 in fp32),
+ * rounded to fp16; code = (y - base) (1 / step), rounded to a whole number (ties
+ * to even) and cut to 0..15, or 0 where step is 0.  A group with a channel that is
+ * not finite becomes NaN (base NaN, step and codes 0).
+ * mosaic_kv_row_bytes: bytes of a row of any type (0 if it is not valid). */
+size_t mosaic_kv_row_bytes(int type, int64_t head_dim);
 
 /* A paged cache.  The pool holds `pages` pages of page_size slots for each of
  * kv_heads heads; slot `o` of page `p`, head `h` starts at element
  * p page_stride + h head_stride + o slot_stride of k and of v (both have the
- * same strides), head_dim contiguous elements.  Slot s of sequence i lies in
+ * same strides; MOSAIC_KV_Q4 counts bytes), head_dim contiguous elements (a row of
+ * mosaic_kv_row_bytes).  Slot s of sequence i lies in
  * page table[i ld_table + s / page_size] at offset s % page_size, the same for
  * every head.  position and weight (each pages x kv_heads x page_size,
  * contiguous) may be NULL where an operation does not need them: the ordinal
  * position of the token in a slot, and the attention weight that the slot has
  * gathered so far.
- * head_dim: a multiple of 8, 8..256.  page_size: 1..65536.  table_cols
+ * head_dim: a multiple of 8 (MOSAIC_KV_Q4: 32), at most 256.  page_size: 1..65536.  table_cols
  * page_size <= 2^31 - 1024.  k, v and the three strides in bytes: multiples of 16.
  * table may be NULL without sequences (seqs 0).
  * The struct is a host struct of device pointers, read during the call only.
@@ -662,6 +677,33 @@ mosaic_status mosaic_rope_turns(int64_t rot_dim, double base, uint64_t *turns);
 mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, int64_t ldx, int64_t l, int64_t heads,
                                const int32_t *seq, const int32_t *slot, const int32_t *index,
                                const mosaic_rope *rope, float *q, int64_t ldq, void *stream);
+
+/* Norms of query and key heads: y = (x r) gain with r = 1 / sqrt(mean x^2 + eps)
+ * over the head's channels, before the rotation.  q_gain and k_gain: head_dim
+ * fp32 device values, the same for every head; NULL: ones.  eps >= 0.  The sum of
+ * squares has to stay finite in fp32. */
+typedef struct {
+    float eps;
+    const float *q_gain, *k_gain;
+} mosaic_head_norm;
+
+/* mosaic_kv_append with norms of the queries and keys (norm may be NULL: the
+ * same call).  Keys of MOSAIC_KV_Q4 caches: sines, cosines and r are rounded
+ * once to fp32 (their errors before that are below 2^-34 relative), and every
+ * product and sum after that is rounded on its own; the row is packed from the
+ * result. */
+mosaic_status mosaic_kv_append_norm(const mosaic_kv_cache *cache, const float *qkv, int64_t ldx, int64_t l,
+                                    int64_t heads, const int32_t *seq, const int32_t *slot, const int32_t *index,
+                                    const mosaic_rope *rope, const mosaic_head_norm *norm, float *q, int64_t ldq,
+                                    void *stream);
+
+/* Reads rows back: key and value of every head in slot[t] of sequence seq[t],
+ * t < l, to k and v at element t ld_token + h ld_head (head_dim contiguous
+ * elements of the cache's type; of fp16, the values, for MOSAIC_KV_Q4).  A
+ * token without a slot (as in mosaic_kv_append), or whose slot has no page, reads zeros.  k and
+ * v: 16-byte aligned, the strides multiples of 16 bytes; rows must not overlap. */
+mosaic_status mosaic_kv_rows(const mosaic_kv_cache *cache, const int32_t *seq, const int32_t *slot, int64_t l,
+                             void *k, void *v, int64_t ld_token, int64_t ld_head, void *stream);
 
 /* Attention of one new token per sequence.  Query head h of sequence i (row i
  * of q, seqs x heads head_dim fp32, leading dimension ldq) reads key/value head

@@ -22,7 +22,8 @@ SOURCES = ["abi.cu", "prg.cu", "hadamard.cu", "ring_gemm_imad.cu", "ring_gemm_tc
            "noalloc.cu", "ring_gemm_skinny.cu", "freivalds.cu",
            "ring_gemm_mma_s8.cu", "ring_gemm_tcw.cu", "timing.cu", "glue.cu",
            "unmask_few.cu", "kv_append.cu", "kv_attention.cu", "kv_attention_f32.cu",
-           "kv_attention_bf16.cu", "kv_attention_f16.cu", "kv_evict.cu"]
+           "kv_attention_bf16.cu", "kv_attention_f16.cu", "kv_attention_q4.cu", "kv_evict.cu",
+           "kv_append_norm.cu", "kv_rows.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
          f"-I{ROOT}/include"]

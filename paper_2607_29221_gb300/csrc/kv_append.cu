@@ -16,55 +16,12 @@
 // shared ones, 29 with the early rows (5.5 TB/s, 81% of the copy rate).
 #include <math.h>
 
-#include "kv_cache.cuh"
+#include "kv_append.cuh"
 
 namespace mosaic {
 namespace {
 
 constexpr int kAppendThreads = 256;
-
-struct Load4 {
-    float x[4];
-};
-__device__ __forceinline__ Load4 load4(const float *p, bool vec) {
-    Load4 r;
-    if (vec) {
-        const float4 v = *reinterpret_cast<const float4 *>(p);
-        r.x[0] = v.x; r.x[1] = v.y; r.x[2] = v.z; r.x[3] = v.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.x[i] = p[i];
-    }
-    return r;
-}
-__device__ __forceinline__ void store4(float *p, const Load4 &v, bool vec) {
-    if (vec) *reinterpret_cast<float4 *>(p) = make_float4(v.x[0], v.x[1], v.x[2], v.x[3]);
-    else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = v.x[i];
-    }
-}
-// Four channels into the cache (rounded to nearest once); 8- or 16-byte
-// aligned by the cache's strides and the multiples of 4 channels.
-__device__ __forceinline__ void put4(float *p, const Load4 &v) { store4(p, v, true); }
-template <class T>
-__device__ __forceinline__ void put4(T *p, const Load4 &v) {
-    T e[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) e[i] = Elem<T>::from(v.x[i]);
-    *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(e);
-}
-
-struct AppendArgs {
-    const float *qkv;
-    int64_t ldx, l;
-    int heads, vec;
-    const int32_t *seq, *slot, *index;
-    mosaic_rope rope;
-    float *q;
-    int64_t ldq;
-    int share;   // heads of a block
-};
 
 template <class T>
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(KvView kv, AppendArgs a) {
@@ -173,9 +130,10 @@ mosaic_status mosaic_rope_turns(int64_t rot_dim, double base, uint64_t *turns) {
     return MOSAIC_OK;
 }
 
-mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, int64_t ldx, int64_t l, int64_t heads,
-                               const int32_t *seq, const int32_t *slot, const int32_t *index,
-                               const mosaic_rope *rope, float *q, int64_t ldq, void *stream) {
+mosaic_status mosaic_kv_append_norm(const mosaic_kv_cache *cache, const float *qkv, int64_t ldx, int64_t l,
+                                    int64_t heads, const int32_t *seq, const int32_t *slot, const int32_t *index,
+                                    const mosaic_rope *rope, const mosaic_head_norm *norm, float *q, int64_t ldq,
+                                    void *stream) {
     RoleScope role("kv_append");
     MOSAIC_TRY(kv_check(cache));
     const int64_t D = cache->head_dim, KV = cache->kv_heads;
@@ -190,21 +148,16 @@ mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, i
         if (l && (!rope->turns || !rope->pos)) return MOSAIC_ERR_ARG;
         a.rope = *rope;
     }
+    if (norm && !(norm->eps >= 0.0f)) return MOSAIC_ERR_ARG;
     if (l == 0) return MOSAIC_OK;
     if (!qkv || !q || !seq || !slot || (cache->position && !index)) return MOSAIC_ERR_ARG;
     a.qkv = qkv, a.ldx = ldx, a.l = l, a.heads = (int)heads, a.seq = seq, a.slot = slot, a.index = index, a.q = q, a.ldq = ldq;
     a.vec = aligned16(qkv) && aligned16(q) && ldx % 4 == 0 && ldq % 4 == 0;
-    const int units = (int)D / 8, lanes = kAppendThreads / units;
-    // Heads of a block: all of a token's, unless that leaves SMs without work
-    // (at most four blocks an SM, a head a thread at least).
-    const int64_t all = heads + 2 * KV, most = (all + lanes - 1) / lanes;
-    int64_t cut = 152 * 4 / l;
-    cut = cut < 1 ? 1 : cut > most ? most : cut;
-    a.share = (int)((most + cut - 1) / cut * lanes);
-    const dim3 grid((unsigned)((all + a.share - 1) / a.share), (unsigned)(l < 65535 ? l : 65535),
-                    (unsigned)((l + 65534) / 65535));
     cudaStream_t st = as_stream(stream);
     const KvView kv(*cache);
+    if (norm || cache->type == MOSAIC_KV_Q4) return append_norm_launch(*cache, a, norm, st);
+    const int units = (int)D / 8, lanes = kAppendThreads / units;
+    const dim3 grid = append_grid(*cache, a, lanes);
     {
         KernelSpan span("append", st);
         if (cache->type == MOSAIC_KV_F32) append_launch<float>(kv, a, grid, lanes * units, st);
@@ -212,6 +165,12 @@ mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, i
         else append_launch<__half>(kv, a, grid, lanes * units, st);
     }
     return launch_status();
+}
+
+mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, int64_t ldx, int64_t l, int64_t heads,
+                               const int32_t *seq, const int32_t *slot, const int32_t *index,
+                               const mosaic_rope *rope, float *q, int64_t ldq, void *stream) {
+    return mosaic_kv_append_norm(cache, qkv, ldx, l, heads, seq, slot, index, rope, nullptr, q, ldq, stream);
 }
 
 }  // extern "C"

@@ -202,7 +202,8 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 template <class F>
 auto by_type(int type, F f) {
-    return type == MOSAIC_KV_F32 ? f(float()) : type == MOSAIC_KV_BF16 ? f(__nv_bfloat16()) : f(__half());
+    return type == MOSAIC_KV_F32 ? f(float()) : type == MOSAIC_KV_BF16 ? f(__nv_bfloat16())
+           : type == MOSAIC_KV_F16 ? f(__half()) : f(Q4());
 }
 
 // The parts of the workspace, in order; `base` may be null (sizes only).
@@ -231,7 +232,7 @@ int64_t most_blocks(const mosaic_kv_cache &c, const AttendShape &s, int64_t head
     const int64_t group = heads / c.kv_heads, hb = (group + s.heads - 1) / s.heads;
     const int64_t units = c.seqs * c.kv_heads * hb * ((max_len + s.unit - 1) / s.unit);
     const bool many = c.seqs * c.kv_heads * hb >= kManyJobs;
-    const int64_t row = c.head_dim * kv_element_bytes(c.type);
+    const int64_t row = kv_row_bytes(c.type, c.head_dim);
     const bool whole = max_len <= (many ? kWholeMany : kWholeFew) && max_len * row <= (many ? 2 : 1) * kWholeBytes;
     return whole ? 0 : units < kAttendWave ? units : kAttendWave;
 }
@@ -251,8 +252,9 @@ int64_t rows_of(int64_t max_len) { return (max_len + 15) / 16 * 16; }
 
 // Reads and clears the timeout words of the attention kernels (after a stream sync).
 mosaic_status kv_status() {
-    const mosaic_status a = attend_status<float>(), b = attend_status<__nv_bfloat16>(), c = attend_status<__half>();
-    return a != MOSAIC_OK ? a : b != MOSAIC_OK ? b : c;
+    const mosaic_status a = attend_status<float>(), b = attend_status<__nv_bfloat16>(), c = attend_status<__half>(),
+                        d = attend_status<Q4>();
+    return a != MOSAIC_OK ? a : b != MOSAIC_OK ? b : c != MOSAIC_OK ? c : d;
 }
 
 }  // namespace mosaic
@@ -306,7 +308,7 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     }
     const int64_t jobs = cache->seqs * (cache->kv_heads / a.hpu) * a.hb;
     a.blocks = (int)(a.whole ? jobs : cap);
-    const int64_t unit_bytes = 2 * s.unit * D * kv_element_bytes(cache->type);
+    const int64_t unit_bytes = 2 * s.unit * kv_row_bytes(cache->type, D);
     a.job_cost = (int)((kJobBytes + unit_bytes / 2) / unit_bytes);
     cudaStream_t st = as_stream(stream);
     MOSAIC_TRY(by_type(cache->type, [&](auto t) { return attend_launch<decltype(t)>(*cache, a, a.blocks, st); }));

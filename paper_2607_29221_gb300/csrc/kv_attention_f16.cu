@@ -1,5 +1,5 @@
 #include "kv_attention_impl.cuh"
 
 namespace mosaic {
-MOSAIC_ATTEND_TYPE(__half)
+MOSAIC_ATTEND_TYPE(__half, with_instance<__half>)
 }

@@ -120,6 +120,15 @@ constexpr float kLeastP = 0x1p-14f, kPassP = 0x1p29f;
 constexpr int kTogether = 4;   // chains of products at a time
 constexpr int kLookup = 4 * 128 + 32;   // bytes of a producer's page ids and live slots
 
+// A stage: K, then V of a unit; each in blocks of 128 bytes of all its rows,
+// 16-byte chunk c of row r at chunk c ^ (r % 8) of its block (the tensor copies'
+// 128-byte swizzle).  8 rows of a chunk are conflict-free (ldmatrix), and so are
+// 8 words of rows r, r + 2, r + 4 and r + 6.
+template <int BLOCK>   // bytes of a block of all rows
+__device__ __forceinline__ uint32_t chunk_at(int r, int c) {
+    return (uint32_t)((c >> 3) * BLOCK + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+}
+
 // DP: head_dim padded to 64, 128 or 256.  NT: tiles of 8 query heads.
 template <class T, int DP, int NT>
 struct Shape {
@@ -146,19 +155,14 @@ struct Shape {
     static constexpr int kQAt = kRing + kMerge + kIds, kMiscAt = kQAt + 4 * kQWords * kQHeads;
     static constexpr int kMisc = 512 + 8 * kHeads * (kQReg ? kWarps : kQHeads);
     static constexpr int kBytes = kMiscAt + kMisc;
+    // Boxes of a row and the bytes of one; tiles of 16 rows of a unit go head by head.
+    static constexpr int kPieces = kRow / 128, kPiece = 128, kTiles = 8;
+    static constexpr bool kParted = false;
+    static __device__ __forceinline__ uint32_t at(int r, int c) { return chunk_at<128 * kUnit>(r, c); }
     static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kBlocks = kFit < 3 ? kFit : 3;   // blocks an SM
     static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 constexpr int kProducers = 2;   // warps that copy
-
-// A stage: K, then V of a unit; each in blocks of 128 bytes of all its rows,
-// 16-byte chunk c of row r at chunk c ^ (r % 8) of its block (the tensor copies'
-// 128-byte swizzle).  8 rows of a chunk are conflict-free (ldmatrix), and so are
-// 8 words of rows r, r + 2, r + 4 and r + 6.
-template <int BLOCK>   // bytes of a block of all rows
-__device__ __forceinline__ uint32_t chunk_at(int r, int c) {
-    return (uint32_t)((c >> 3) * BLOCK + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-}
 
 template <class T, int DP, int NT>
 struct Warp {
@@ -574,7 +578,7 @@ template <class T, int DP, int NT>
 struct Pipe {
     using S = Shape<T, DP, NT>;
     uint64_t full[S::kStages], empty[S::kStages];
-    uint16_t live[S::kStages][8];   // slots of the stage's tiles that count
+    uint16_t live[S::kStages][S::kTiles];   // slots of the stage's tiles that count
     int unit[S::kStages];           // the stage's unit in its job; + kLastUnit: the job's last one here
     long long place[12];
     int aborted;
@@ -606,7 +610,8 @@ struct Producer {
     const CUtensorMap *map;
     Pipe<T, DP, NT> &pipe;
     char *smem;
-    const int per_seq, pw, lane, us, per_tile;   // us: slots of a unit; per_tile: 2^8 over the tiles of a head, rounded up
+    // us: slots of a unit; per_tile: 2^8 over the tiles of a head, rounded up (kParted: the heads' logarithm)
+    const int per_seq, pw, lane, us, per_tile;
     int32_t *ids;       // shared, this warp's: pages of the group being copied
     uint8_t *live;      // and its live slots, a bit each
     Jobs jobs;
@@ -622,7 +627,8 @@ struct Producer {
                                         const CUtensorMap *mv, Pipe<T, DP, NT> &pipe_, int per_seq_, const Jobs &j,
                                         char *smem_, int pw_)
         : kv(kv_), a(a_), map(pw_ ? mv : mk), pipe(pipe_), smem(smem_), per_seq(per_seq_), pw(pw_),
-          lane(threadIdx.x & 31), us(S::kUnit / a_.hpu), per_tile(256 / (us / 16) + 1), jobs(j) {
+          lane(threadIdx.x & 31), us(S::kUnit / a_.hpu),
+          per_tile(S::kParted ? (a_.hpu >= 2) + (a_.hpu >= 4) : 256 / (us / 16) + 1), jobs(j) {
         ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge + pw * kLookup);
         live = reinterpret_cast<uint8_t *>(ids + 128);
         job_units = job_at = count = units = 0;
@@ -634,10 +640,18 @@ struct Producer {
     __device__ __forceinline__ int slot_of(const Group &g, int e, int &head) const {
         const int row = TMA ? 8 * lane : 32 * e + lane, u = row / S::kUnit, in = row - u * S::kUnit;
         head = head_of(in);
-        return g.s + u * kTurn * us + in - head * us;
+        return g.s + u * kTurn * us + slot_in(in, head);
     }
-    // Which of the unit's heads row `in` belongs to: its tile (below 8) over the tiles of a head.
-    __device__ __forceinline__ int head_of(int in) const { return (in >> 4) * per_tile >> 8; }
+    // Which of the unit's heads row `in` belongs to: its tile (below 8) over the tiles of a head, or
+    // (kParted) the tile's number modulo the heads (a power of two); and its slot in the unit.
+    __device__ __forceinline__ int head_of(int in) const {
+        if constexpr (S::kParted) return (in >> 4) & (a.hpu - 1);
+        return (in >> 4) * per_tile >> 8;
+    }
+    __device__ __forceinline__ int slot_in(int in, int head) const {
+        if constexpr (S::kParted) return (in >> (4 + per_tile) << 4) + (in & 15);
+        return in - head * us;
+    }
     __device__ __forceinline__ bool is_page(int id) const { return (uint32_t)id < (uint64_t)kv.c.pages; }
     // The next group becomes `now`, its pages and live slots in shared memory.
     __device__ __forceinline__ void step() {
@@ -733,7 +747,15 @@ struct Producer {
                     if (lane == 0) pipe.unit[stage] = unit | (last ? kLastUnit : 0);
                     __syncwarp();
                 }
-                if constexpr (TMA) {
+                if constexpr (TMA && S::kParted) {
+                    if (a.box == 0) {
+                        if (a.hpu == 4) boxes_of_heads<S::kUnit / 64>(u, s, stage, any);
+                        else boxes_of_heads<S::kUnit / 32>(u, s, stage, any);
+                    } else if (a.box == 8) boxes<8>(u, s, stage);
+                    else if (a.box == 16) boxes<16>(u, s, stage);
+                    else if (a.box == 32) boxes<32>(u, s, stage);
+                    else boxes<64>(u, s, stage);
+                } else if constexpr (TMA) {
                     if (a.box == 0) box_of_all(any != 0, u, s, stage);
                     else if (a.box == 8) boxes<8>(u, s, stage);
                     else if (a.box == 16) boxes<16>(u, s, stage);
@@ -762,6 +784,28 @@ struct Producer {
         }
         __syncwarp();
     }
+    // kParted: boxes of 16 slots of a page, of all a.hpu heads.
+    template <int N>
+    __device__ __forceinline__ void boxes_of_heads(int u, int s, int stage, uint32_t any) {
+        if (lane == 0) {
+            uint64_t *bar = pipe.full + stage;
+            const int hpu = a.hpu;
+            const uint32_t bytes = 16 * hpu * S::kRow, each = (1u << hpu) - 1;
+            uint32_t all = 0;
+            int page[N];
+#pragma unroll
+            for (int b = 0; b < N; ++b) {
+                all += any >> (b * hpu) & each ? bytes : 0u;
+                page[b] = ids[(u * S::kUnit + 16 * b * hpu) / 8];
+            }
+            mbar_expect_tx(bar, all);
+            char *to = smem + stage * S::kStage + pw * (S::kStage / 2);
+#pragma unroll
+            for (int b = 0; b < N; ++b)
+                if (any >> (b * hpu) & each) tma_load_4d(to + b * bytes, map, bar, 0, (int)offset(s + 16 * b), now.h, page[b]);
+        }
+        __syncwarp();
+    }
     // Boxes of one head.  Straight code: a lane issues a copy in about 100
     // cycles, 200 in a loop over boxes.
     template <int BOX>
@@ -786,13 +830,15 @@ struct Producer {
                 int off = off0, h = now.h, row = 0;
 #pragma unroll
                 for (int b = 0; b < N; ++b) {
+                    if constexpr (S::kParted) off = (int)offset(s + slot_in(b * BOX, 0)), h = now.h + head_of(b * BOX);
                     if (mask >> b & 1u) {
                         const int c1 = a.token_major ? h : off, c2 = a.token_major ? off : h;
 #pragma unroll
-                        for (int k = 0; k < S::kRow / 128; ++k)
-                            tma_load_4d(to + b * BOX * 128 + k * 128 * S::kUnit, map, bar, k * 128 / S::kES, c1, c2,
+                        for (int k = 0; k < S::kPieces; ++k)
+                            tma_load_4d(to + b * BOX * S::kPiece + k * 128 * S::kUnit, map, bar, k * 128 / S::kES, c1, c2,
                                         page[b]);
                     }
+                    if constexpr (S::kParted) continue;
                     off += BOX, row += BOX;
                     if (off == (int)kv.page.d) off = 0;
                     if (row == us) off = off0, ++h, row = 0;   // the next head's slots
@@ -803,22 +849,23 @@ struct Producer {
     }
     __device__ __forceinline__ void rows(int u, int s, int stage) {
         const char *kp = static_cast<const char *>(kv.c.k), *vp = static_cast<const char *>(kv.c.v);
-        const int chunks = kv.c.head_dim * S::kES / 16;
+        const int chunks = kv.row16;
         const uint32_t to = smem_u32(smem + stage * S::kStage);
         for (int r0 = 0; r0 < S::kUnit; r0 += 32) {   // a lane's row: 16 or 32 of a head's
             const int in = r0 + lane, e = u * S::kUnit + in, head = head_of(in);
             const bool on = in < S::kUnit && live[e >> 3] >> (e & 7) & 1u;
-            const int64_t row = on ? kv.element(ids[e], now.h + head, offset(s + in - head * us)) * S::kES : -1;
+            const int64_t row = on ? kv.element(ids[e], now.h + head, offset(s + slot_in(in, head))) * S::kES : -1;
             const uint32_t any = __ballot_sync(0xffffffffu, on);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 if (!(any >> (16 * half) & 0xffffu)) continue;   // a tile without a live slot is not read
 #pragma unroll 8
-                for (int x = 0; x < 16 * S::kChunks / 32; ++x) {
+                for (int x = 0; x < (16 * S::kChunks + 31) / 32; ++x) {
                     const int at16 = x * 32 + lane, rr = 16 * half + at16 / S::kChunks, c = at16 % S::kChunks;
                     const int64_t from = __shfl_sync(0xffffffffu, row, rr);
+                    if (16 * S::kChunks % 32 && at16 >= 16 * S::kChunks) continue;
                     const bool ok = from >= 0 && c < chunks;
-                    const uint32_t dst = to + chunk_at<128 * S::kUnit>(r0 + rr, c);
+                    const uint32_t dst = to + S::at(r0 + rr, c);
                     const int64_t src = ok ? from + c * 16 : 0;
                     copy16(dst, kp + src, ok);
                     copy16(dst + S::kStage / 2, vp + src, ok);
@@ -842,6 +889,63 @@ struct Producer {
 template <int THREADS>
 __device__ __forceinline__ void consumers_sync() {
     asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+}
+
+// Weights of a whole job (sequence i, head h, s1 slots) from its scores and its
+// heads' maxima and sums: thread `at0` of `each`.
+__device__ __forceinline__ void whole_weights(const KvView &kv, const AttendArgs &a, const float2 *stats, const float *scores,
+                                              int64_t i, int h, int rows, int s1, int at0, int each) {
+    for (int x = 4 * at0; x < s1; x += 4 * each) {   // a lane four slots
+        const bool quad = a.quads && x + 4 <= s1;
+        int64_t at[4];
+        __align__(16) float old[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (quad && j) {
+                at[j] = at[0] < 0 ? -1 : at[0] + j;
+                continue;
+            }
+            uint32_t off;
+            const int id = x + j < s1 ? kv.page_of(i, (uint32_t)(x + j), off) : -1;
+            at[j] = id < 0 ? -1 : kv.mark(id, h, off);
+        }
+        if (quad && at[0] >= 0) *reinterpret_cast<float4 *>(old) = *reinterpret_cast<const float4 *>(kv.c.weight + at[0]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (!quad && at[j] >= 0) old[j] = kv.c.weight[at[j]];
+#pragma unroll 8
+        for (int r = 0; r < rows; ++r) {   // rows of 16 slots exist in whole
+            const float2 st = stats[r];
+            const float4 v = *reinterpret_cast<const float4 *>(scores + r * a.score_rows + x);
+            sum[0] = fmaf(power2(v.x - st.x), st.y, sum[0]);
+            sum[1] = fmaf(power2(v.y - st.x), st.y, sum[1]);
+            sum[2] = fmaf(power2(v.z - st.x), st.y, sum[2]);
+            sum[3] = fmaf(power2(v.w - st.x), st.y, sum[3]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            // Slots below the bound gather nothing (and may have no score).
+            if (a.first && at[j] >= 0 && kv.c.position[at[j]] < a.first[i]) sum[j] = 0.0f;
+            old[j] = fmaf(old[j], a.decay, sum[j]);
+        }
+        if (quad && at[0] >= 0) *reinterpret_cast<float4 *>(kv.c.weight + at[0]) = *reinterpret_cast<const float4 *>(old);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (!quad && at[j] >= 0) kv.c.weight[at[j]] = old[j];
+    }
+}
+
+// This block's end cuts the job: who has the rest of it?
+__device__ __forceinline__ void cut_job(const AttendArgs &a, const Jobs &jobs, int64_t i, int64_t end, int64_t total, int per_seq) {
+    // Counted unit u is block c's if total c / blocks <= u < total (c + 1) / blocks (rounded down).
+    const int64_t last = end + (jobs.nb - jobs.b1) - 1, n = gridDim.x;
+    int64_t c = last * n / total;
+    while (total * (c + 1) / n <= last) ++c;
+    while (total * c / n > last) --c;
+    a.split[3 * blockIdx.x] = i * per_seq + jobs.r;
+    a.split[3 * blockIdx.x + 1] = c;
+    a.split[3 * blockIdx.x + 2] = total;
 }
 
 template <class T, int DP, int NT, bool TMA>
@@ -1022,71 +1126,23 @@ __global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
         if (a.scores && a.whole && a.hb == 1) {
             // The job's scores are this block's: its weights need no further launch.
             consumers_sync<THREADS>();
-            for (int x = 4 * (32 * sub + lane); x < s1; x += 128 * of_head) {   // a lane four slots
-                const bool quad = a.quads && x + 4 <= s1;
-                int64_t at[4];
-                __align__(16) float old[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (quad && j) {
-                        at[j] = at[0] < 0 ? -1 : at[0] + j;
-                        continue;
-                    }
-                    uint32_t off;
-                    const int id = x + j < s1 ? kv.page_of(i, (uint32_t)(x + j), off) : -1;
-                    at[j] = id < 0 ? -1 : kv.mark(id, h, off);
-                }
-                if (quad && at[0] >= 0) *reinterpret_cast<float4 *>(old) = *reinterpret_cast<const float4 *>(kv.c.weight + at[0]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (!quad && at[j] >= 0) old[j] = kv.c.weight[at[j]];
-#pragma unroll 8
-                for (int r = 0; r < rows; ++r) {   // rows of 16 slots exist in whole
-                    const float2 st = pipe.stats[hi * S::kHeads + r];
-                    const float4 v = *reinterpret_cast<const float4 *>(scores + r * a.score_rows + x);
-                    sum[0] = fmaf(power2(v.x - st.x), st.y, sum[0]);
-                    sum[1] = fmaf(power2(v.y - st.x), st.y, sum[1]);
-                    sum[2] = fmaf(power2(v.z - st.x), st.y, sum[2]);
-                    sum[3] = fmaf(power2(v.w - st.x), st.y, sum[3]);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    // Slots below the bound gather nothing (and may have no score).
-                    if (a.first && at[j] >= 0 && kv.c.position[at[j]] < a.first[i]) sum[j] = 0.0f;
-                    old[j] = fmaf(old[j], a.decay, sum[j]);
-                }
-                if (quad && at[0] >= 0) *reinterpret_cast<float4 *>(kv.c.weight + at[0]) = *reinterpret_cast<const float4 *>(old);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (!quad && at[j] >= 0) kv.c.weight[at[j]] = old[j];
-            }
+            whole_weights(kv, a, pipe.stats + hi * S::kHeads, scores, i, h, rows, s1, 32 * sub + lane, 32 * of_head);
         }
-        if (!whole && jobs.b0 == 0 && tid == 0) {   // this block's end cuts the job: who has the rest of it?
-            // Counted unit u is block c's if total c / blocks <= u < total (c + 1) / blocks (rounded down).
-            const int64_t last = end + (jobs.nb - jobs.b1) - 1, n = gridDim.x;
-            int64_t c = last * n / total;
-            while (total * (c + 1) / n <= last) ++c;
-            while (total * c / n > last) --c;
-            a.split[3 * blockIdx.x] = i * per_seq + jobs.r;
-            a.split[3 * blockIdx.x + 1] = c;
-            a.split[3 * blockIdx.x + 2] = total;
-        }
+        if (!whole && jobs.b0 == 0 && tid == 0) cut_job(a, jobs, i, end, total, per_seq);
         if (of_head > 1 || !S::kQReg) consumers_sync<THREADS>();   // buffers and queries are free again
     }
 }
 
-template <class T, int DP, int NT, bool TMA>
+// Blocks of a wave of `kernel` (of shape S); 0 on an error.
+template <class S, auto kernel>
 int resident() {
     static std::atomic<int> known[64];
     int dev = 0, n = 0;
     static std::atomic<unsigned long long> done{0};
-    using S = Shape<T, DP, NT>;
-    if (!ensure_smem_limit(done, attend_kernel<T, DP, NT, TMA>, S::kBytes, &dev)) return 0;
+    if (!ensure_smem_limit(done, kernel, S::kBytes, &dev)) return 0;
     std::atomic<int> &at = known[dev & 63];
     if ((n = at.load(std::memory_order_relaxed)) > 0) return n;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, attend_kernel<T, DP, NT, TMA>, 32 * (S::kWarps + kProducers), S::kBytes) !=
-        cudaSuccess)
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, 32 * (S::kWarps + kProducers), S::kBytes) != cudaSuccess)
         return 0;
     n *= sm_count(dev);
     at.store(n, std::memory_order_relaxed);
@@ -1094,13 +1150,15 @@ int resident() {
 }
 
 // A pool as a tensor of (channel, slot, head, page), or (channel, head, slot,
-// page) where heads are the closer ones; box: 128 bytes of `slots_box` slots of
-// `heads_box` heads.  False where the strides do not nest (the lanes copy), or
+// page) where heads are the closer ones; box: `row_box` bytes (128, swizzled; 4
+// bits: a whole row) of `slots_box` slots of `heads_box` heads.  False where the strides do not nest (the lanes copy), or
 // for several heads where heads are the closer ones.
 template <class T>
-bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int slots_box, int heads_box, int *token_major) {
-    constexpr int kES = sizeof(T);
-    const cuuint64_t D = (cuuint64_t)c.head_dim * kES, slots = (cuuint64_t)c.page_size, heads = (cuuint64_t)c.kv_heads;
+bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int slots_box, int heads_box, int *token_major, int row_box = 128) {
+    constexpr bool kPacked = std::is_same<T, Q4>::value;
+    constexpr int kES = sizeof(T);   // 4 bits: 1, rows are counted in bytes
+    const cuuint64_t row = kPacked ? 5 * (cuuint64_t)c.head_dim / 8 : (cuuint64_t)c.head_dim;
+    const cuuint64_t D = row * kES, slots = (cuuint64_t)c.page_size, heads = (cuuint64_t)c.kv_heads;
     cuuint64_t slot = (cuuint64_t)c.slot_stride * kES, head = (cuuint64_t)c.head_stride * kES;
     cuuint64_t page = (cuuint64_t)c.page_stride * kES;
     if (heads == 1) head = slot * slots;
@@ -1112,14 +1170,14 @@ bool pool_map(CUtensorMap *map, const mosaic_kv_cache &c, void *pool, int slots_
     if (inner < D || outer < inner || page < outer || outer % inner || page % outer || page >= most) return false;
     auto fn = encode_fn();
     if (!fn) return false;
-    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, tm ? heads : slots, tm ? slots : heads, (cuuint64_t)c.pages};
+    const cuuint64_t dims[4] = {row, tm ? heads : slots, tm ? slots : heads, (cuuint64_t)c.pages};
     const cuuint64_t strides[3] = {inner, outer, page};
-    const cuuint32_t box[4] = {128 / kES, tm ? 1u : (cuuint32_t)slots_box, tm ? (cuuint32_t)slots_box : (cuuint32_t)heads_box, 1}, each[4] = {1, 1, 1, 1};
-    const CUtensorMapDataType type = kES == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+    const cuuint32_t box[4] = {(cuuint32_t)row_box / kES, tm ? 1u : (cuuint32_t)slots_box, tm ? (cuuint32_t)slots_box : (cuuint32_t)heads_box, 1}, each[4] = {1, 1, 1, 1};
+    const CUtensorMapDataType type = kPacked ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : kES == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                      : kTerms<T> == 3 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     *token_major = tm;
-    return fn(map, type, 4, pool, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(map, type, 4, pool, dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              kPacked ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <class T, int DP, int NT>
@@ -1132,7 +1190,7 @@ struct Instance {
     template <bool TMA>
     static mosaic_status go(const KvView &kv, AttendArgs a, const CUtensorMap &mk, const CUtensorMap &mv,
                             int &blocks, cudaStream_t st) {
-        const int wave = resident<T, DP, NT, TMA>();
+        const int wave = resident<S, attend_kernel<T, DP, NT, TMA>>();
         if (wave <= 0) return MOSAIC_ERR_CUDA;
         if (!a.whole && a.blocks > wave) a.blocks = wave;
         blocks = a.blocks;
@@ -1180,22 +1238,21 @@ auto with_instance(int head_dim, int group, F f) {
 
 }  // namespace
 
-#define MOSAIC_ATTEND_TYPE(T)                                                                             \
-    template <> AttendShape attend_shape<T>(int head_dim, int group) {                                    \
-        return with_instance<T>(head_dim, group, [&](auto i) { return decltype(i)::shape(); });           \
-    }                                                                                                     \
-    template <>                                                                                           \
-    mosaic_status attend_launch<T>(const mosaic_kv_cache &c, const AttendArgs &a, int &blocks,            \
-                                   cudaStream_t st) {                                                     \
-        return with_instance<T>(c.head_dim, a.group,                                                      \
-                                [&](auto i) { return decltype(i)::launch(c, a, blocks, st); });           \
-    }                                                                                                     \
-    template <> mosaic_status attend_status<T>() {                                                        \
-        unsigned int e = 0, zero = 0;                                                                     \
-        if (cudaMemcpyFromSymbol(&e, g_attend_error, sizeof(e)) != cudaSuccess) return MOSAIC_ERR_CUDA;   \
-        if (!e) return MOSAIC_OK;                                                                         \
+#define MOSAIC_ATTEND_TYPE(T, WITH)                                                                         \
+    template <> AttendShape attend_shape<T>(int head_dim, int group) {                                      \
+        return WITH(head_dim, group, [&](auto i) { return decltype(i)::shape(); });                         \
+    }                                                                                                       \
+    template <>                                                                                             \
+    mosaic_status attend_launch<T>(const mosaic_kv_cache &c, const AttendArgs &a, int &blocks,              \
+                                   cudaStream_t st) {                                                       \
+        return WITH(c.head_dim, a.group, [&](auto i) { return decltype(i)::launch(c, a, blocks, st); });    \
+    }                                                                                                       \
+    template <> mosaic_status attend_status<T>() {                                                          \
+        unsigned int e = 0, zero = 0;                                                                       \
+        if (cudaMemcpyFromSymbol(&e, g_attend_error, sizeof(e)) != cudaSuccess) return MOSAIC_ERR_CUDA;     \
+        if (!e) return MOSAIC_OK;                                                                           \
         if (cudaMemcpyToSymbol(g_attend_error, &zero, sizeof(zero)) != cudaSuccess) return MOSAIC_ERR_CUDA; \
-        return MOSAIC_ERR_TIMEOUT;                                                                        \
+        return MOSAIC_ERR_TIMEOUT;                                                                          \
     }
 
 }  // namespace mosaic

@@ -8,6 +8,9 @@
 #include "mosaic_internal.cuh"
 
 namespace mosaic {
+
+struct Q4 {};   // the element type of 4-bit caches
+
 namespace {
 
 // n / d for 0 <= n < 2^31 by a multiply and a shift (Granlund and Montgomery,
@@ -21,11 +24,21 @@ struct FastDiv {
     __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
 };
 
+inline int64_t kv_element_bytes(int type) { return type == MOSAIC_KV_F32 ? 4 : type == MOSAIC_KV_Q4 ? 1 : 2; }
+// Bytes of a cached row: 4-bit rows are codes, then step and base of every
+// kQ4Group channels, padded to 16 bytes.
+constexpr int kQ4Group = 32;
+inline int64_t kv_row_bytes(int type, int64_t head_dim) {
+    return type == MOSAIC_KV_Q4 ? (5 * head_dim / 8 + 15) / 16 * 16 : head_dim * kv_element_bytes(type);
+}
+
 // A cache as the kernels see it.
 struct KvView {
     mosaic_kv_cache c;
     FastDiv page;
-    explicit KvView(const mosaic_kv_cache &cache) : c(cache), page((uint32_t)cache.page_size) {}
+    int row16;   // 16-byte chunks of a row
+    explicit KvView(const mosaic_kv_cache &cache)
+        : c(cache), page((uint32_t)cache.page_size), row16((int)(kv_row_bytes(cache.type, cache.head_dim) + 15) / 16) {}
 
     __device__ __forceinline__ int64_t slots() const { return c.table_cols * c.page_size; }
     // Length i, clamped to [0, max_len] and the table.
@@ -52,16 +65,15 @@ struct KvView {
     }
 };
 
-inline int64_t kv_element_bytes(int type) { return type == MOSAIC_KV_F32 ? 4 : 2; }
-
 // What every call asks of a cache.
 inline mosaic_status kv_check(const mosaic_kv_cache *c) {
     if (!c) return MOSAIC_ERR_ARG;
-    if (c->type < MOSAIC_KV_F32 || c->type > MOSAIC_KV_F16) return MOSAIC_ERR_ARG;
+    if (c->type < MOSAIC_KV_F32 || (c->type > MOSAIC_KV_F16 && c->type != MOSAIC_KV_Q4)) return MOSAIC_ERR_ARG;
     if (c->kv_heads < 1 || c->kv_heads > 65535 || c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8 ||
         c->page_size < 1 || c->page_size > 65536 || c->pages < 1 || c->pages > 0x7fffffff || c->seqs < 0 ||
         c->seqs > (1 << 24) || c->table_cols < 1 || c->table_cols > 0x7fffffff || c->ld_table < c->table_cols)
         return MOSAIC_ERR_SHAPE;
+    if (c->type == MOSAIC_KV_Q4 && c->head_dim % kQ4Group) return MOSAIC_ERR_SHAPE;
     // Slots are counted in 31 bits, also at the end of a unit or group of look-ups (512 slots at
     // most) that begins inside a sequence.
     if (c->table_cols * c->page_size > ((int64_t)1 << 31) - 1024) return MOSAIC_ERR_SHAPE;
@@ -71,6 +83,57 @@ inline mosaic_status kv_check(const mosaic_kv_cache *c) {
     if (!aligned16(c->k) || !aligned16(c->v) || c->page_stride % unit || c->head_stride % unit || c->slot_stride % unit)
         return MOSAIC_ERR_ALIGN;
     return MOSAIC_OK;
+}
+
+// Rows of 4-bit codes: channel c of a row is code (word c / 8) >> 4 (c % 8) & 15
+// and stands for base + code step, one fused fp16 operation, where step and
+// base are the halves of word c / 32 of the row's last part.
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
+__device__ __forceinline__ uint32_t as_word(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
+// Codes k and k + 4 (counted from the lowest) of a word as values, k = 0 .. 3,
+// packed with the lower one first.  A code or'ed into the mantissa of 1024 is
+// 1024 + code, or 1024 + 16 code: both come off exactly.
+__device__ __forceinline__ void q4_values(uint32_t w, __half2 step, __half2 base, uint32_t (&y)[4]) {
+    const __half2 one = as_half2(0xe400e400u), part = as_half2(0x2c002c00u), rest = as_half2(0xd400d400u);   // -1024, 1/16, -64
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+        const uint32_t x = k ? w >> 8 : w;
+        const __half2 lo = __hadd2(as_half2((x & 0x000f000fu) | 0x64006400u), one);
+        const __half2 hi = __hfma2(as_half2((x & 0x00f000f0u) | 0x64006400u), part, rest);
+        y[k] = as_word(__hfma2(lo, step, base));
+        y[k + 1] = as_word(__hfma2(hi, step, base));
+    }
+}
+
+// The word of codes of 8 channels, and the group's step and base (in that
+// order).  Every thread of a warp calls it; four neighbours have a group.
+__device__ __forceinline__ uint32_t q4_pack(const float (&y)[8], uint32_t &codes) {
+    constexpr float kMost = 65000.0f;   // base + 15 step stays finite in fp16
+    float x[8], least, most;
+    bool fine = true;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        fine &= fabsf(y[i]) < __int_as_float(0x7f800000);
+        x[i] = fminf(fmaxf(y[i], -kMost), kMost);
+        least = i ? fminf(least, x[i]) : x[i], most = i ? fmaxf(most, x[i]) : x[i];
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+        least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        fine &= (bool)__shfl_xor_sync(0xffffffffu, (int)fine, o);
+    }
+    const __half base = __float2half_rn(least), step = __float2half_rn(__fmul_rn(__fsub_rn(most, least), (float)(1.0 / 15.0)));
+    const float from = __half2float(base), s = __half2float(step), inv = s > 0.0f ? __fdiv_rn(1.0f, s) : 0.0f;
+    codes = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float c = rintf(__fmul_rn(__fsub_rn(x[i], from), inv));
+        codes |= (uint32_t)fminf(fmaxf(c, 0.0f), 15.0f) << (4 * i);
+    }
+    if (fine) return as_word(__halves2half2(step, base));
+    codes = 0;
+    return 0x7fff0000u;   // step 0, base NaN
 }
 
 template <class T> struct Elem;

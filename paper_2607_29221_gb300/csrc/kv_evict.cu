@@ -64,7 +64,7 @@ __device__ __forceinline__ uint32_t slot_key(const KvView &kv, const EvictArgs &
 __device__ __forceinline__ void move32(const KvView &kv, const EvictArgs &a, int64_t job, int64_t i, int h, int m0,
                                        int count) {
     const int lane = threadIdx.x & 31;
-    const int es = kv.c.type == MOSAIC_KV_F32 ? 4 : 2, quads = kv.c.head_dim * es / 16;
+    const int es = kv.c.type == MOSAIC_KV_F32 ? 4 : kv.c.type == MOSAIC_KV_Q4 ? 1 : 2, quads = kv.row16;
     char *const kp = static_cast<char *>(kv.c.k), *const vp = static_cast<char *>(kv.c.v);
     int64_t se = -1, te = 0;
     if (m0 + lane < count) {

@@ -10,6 +10,11 @@ call on the current stream:
   q     = cache.append(qkv, heads, seq, slot, index, rope=rope, pos=pos)
   out   = cache.attend(q, lens, max_len)
   lens  = cache.evict(lens, max_len, keep, recent_from=recent_from)
+  k, v  = cache.rows(seq, slot)
+
+Keys and values are held in float32, bfloat16, float16 or 4 bits (``INT4``: uint8
+pools, rows of codes with a step and a base for every 32 channels).  ``HeadNorm``
+norms the query and key heads on the way in.
 
 Arguments are tensors on the cache's device.  Scratch is kept for the last few
 streams of each host thread until the thread ends (5 us a call to allocate it
@@ -27,7 +32,8 @@ import torch
 from . import mosaic as M
 
 _STREAMS = 4   # streams of a host thread whose scratch is kept
-_TYPES = {torch.float32: M.KV_F32, torch.bfloat16: M.KV_BF16, torch.float16: M.KV_F16}
+INT4 = torch.uint8   # the element type of 4-bit pools: bytes of packed rows
+_TYPES = {torch.float32: M.KV_F32, torch.bfloat16: M.KV_BF16, torch.float16: M.KV_F16, INT4: M.KV_Q4}
 
 
 def _need(ok: bool, what: str) -> None:
@@ -88,9 +94,40 @@ class Rope:
                              _row_stride(pos, pos.shape[1], "pos"))
 
 
+def row_bytes(head_dim: int) -> int:
+    """Bytes of a row of a 4-bit cache: the last axis of its uint8 pools."""
+    n = M.mosaic_kv_row_bytes(M.KV_Q4, head_dim)
+    _need(n > 0, "head_dim: a multiple of 32 up to 256 for 4-bit caches")
+    return n
+
+
+class HeadNorm:
+    """Norms of query and key heads: x / sqrt(mean(x^2) + eps) over a head, times
+    ``q_gain`` or ``k_gain`` (float32, a value a channel, the same for all heads;
+    None: 1).  It keeps the gains alive."""
+
+    def __init__(self, head_dim: int, eps: float = 1e-6, q_gain=None, k_gain=None):
+        _need(eps >= 0.0, "eps: not negative")
+        for g, name in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+            _need(g is None or (g.dtype is torch.float32 and g.shape == (head_dim,)
+                                and (head_dim == 1 or g.stride(0) == 1)),
+                  f"{name}: a contiguous float32 tensor of head_dim values")
+        self.head_dim, self.q_gain, self.k_gain = head_dim, q_gain, k_gain
+        self._c = M.mosaic_head_norm(eps, *(None if g is None else g.data_ptr() for g in (q_gain, k_gain)))
+        self._ref = ctypes.byref(self._c)
+
+    def on(self, head_dim: int, index: int):
+        """The library's argument for a cache of head_dim channels on device ``index``."""
+        _need(head_dim == self.head_dim, "norm: of another head_dim than the cache")
+        _need(all(g is None or g.get_device() == index for g in (self.q_gain, self.k_gain)),
+              "norm: gains on another device than the cache")
+        return self._ref
+
+
 class PagedCache:
     """Handle on a paged cache.  k, v: pages x kv_heads x page_size x head_dim
-    views (float32, bfloat16 or float16; equal strides, channels contiguous),
+    views (float32, bfloat16 or float16; equal strides, channels contiguous; uint8
+    with row_bytes(head_dim) instead of head_dim: 4 bits),
     table: seqs x columns int32 page ids; position (int32) and weight
     (float32): contiguous pages x kv_heads x page_size, or None."""
 
@@ -99,6 +136,9 @@ class PagedCache:
               and k.dtype in _TYPES and k.stride(3) == 1 and k.is_cuda and v.device == k.device,
               "k and v: CUDA tensors of one type and shape (4 axes), equal strides, channels contiguous")
         pages, kv_heads, page, dim = k.shape
+        if k.dtype is INT4:
+            dim = next((d for d in range(32, 257, 32) if row_bytes(d) == dim), 0)
+            _need(dim > 0, "k and v: rows of row_bytes(head_dim) bytes for 4 bits")
         _need(table.dtype == torch.int32 and table.dim() == 2 and table.device == k.device
               and (table.shape[1] <= 1 or table.stride(1) == 1), "table: int32, seqs x columns, rows contiguous")
         for t, dt, name in ((position, torch.int32, "position"), (weight, torch.float32, "weight")):
@@ -122,7 +162,8 @@ class PagedCache:
               weights: bool = True):
         """A new pool (head-major pages), with positions, and weights unless turned off."""
         shape, dev = (pages, kv_heads, page_size), table.device
-        k, v = (torch.zeros(*shape, head_dim, dtype=dtype, device=dev) for _ in range(2))
+        row = row_bytes(head_dim) if dtype is INT4 else head_dim
+        k, v = (torch.zeros(*shape, row, dtype=dtype, device=dev) for _ in range(2))
         return cls(k, v, table, torch.zeros(shape, dtype=torch.int32, device=dev),
                    torch.zeros(shape, dtype=torch.float32, device=dev) if weights else None)
 
@@ -155,15 +196,37 @@ class PagedCache:
         return ws
 
     def read(self, seq: int, n: int):
-        """Keys and values of the first n slots of a sequence, kv_heads x n x head_dim in the cache's type (a copy)."""
+        """Keys and values of the first n slots of a sequence, kv_heads x n x head_dim in the cache's type (a copy;
+        float16 for 4 bits)."""
+        if self.k.dtype is INT4:
+            slot = torch.arange(n, dtype=torch.int32, device=self.device)
+            k, v = self.rows(torch.full_like(slot, seq), slot, token_major=False)
+            return k, v
         page = self.k.shape[2]
         ids = self.table[seq, : -(-n // page)].long()
         return tuple(x[ids].transpose(0, 1).reshape(self.kv_heads, -1, self.head_dim)[:, :n] for x in (self.k, self.v))
 
-    def append(self, qkv, heads: int, seq, slot, index=None, rope: Rope | None = None, pos=None, out=None):
-        """Rotates row t of qkv (l x (heads + 2 kv_heads) head_dim fp32) and
-        stores its keys and values in slot[t] of sequence seq[t] (a negative
-        slot: not stored); returns the queries, l x heads x head_dim fp32."""
+    def rows(self, seq, slot, token_major: bool = True):
+        """Keys and values in slot[t] of sequence seq[t], l x kv_heads x head_dim (or kv_heads x l x head_dim) in the
+        cache's type, the values in float16 for 4 bits; a token without a slot or page reads zeros."""
+        l, h, d = slot.numel(), self.kv_heads, self.head_dim
+        _int32(seq, "seq", l, self._index)
+        _int32(slot, "slot", l, self._index)
+        shape, strides = ((l, h, d), (h * d, d)) if token_major else ((h, l, d), (d, l * d))
+        dtype = torch.float16 if self.k.dtype is INT4 else self.k.dtype
+        k, v = (torch.empty(shape, dtype=dtype, device=self.device) for _ in range(2))
+        status = M.lib().mosaic_kv_rows(self._ref, seq.data_ptr(), slot.data_ptr(), l, k.data_ptr(), v.data_ptr(),
+                                        *strides, self._stream())
+        if status:
+            raise M.MosaicError("mosaic_kv_rows", status)
+        return k, v
+
+    def append(self, qkv, heads: int, seq, slot, index=None, rope: Rope | None = None, pos=None, out=None,
+               norm: HeadNorm | None = None):
+        """Norms (if given) and rotates row t of qkv (l x (heads + 2 kv_heads)
+        head_dim fp32) and stores its keys and values in slot[t] of sequence
+        seq[t] (a negative slot: not stored); returns the queries, l x heads x
+        head_dim fp32."""
         d, width = self.head_dim, (heads + 2 * self.kv_heads) * self.head_dim
         if (qkv.dtype is not torch.float32 or qkv.dim() != 2 or qkv.get_device() != self._index
                 or qkv.shape[1] != width or qkv.stride(1) != 1):
@@ -179,14 +242,17 @@ class PagedCache:
                 raise ValueError("rope: on another device than the cache")
             _need(pos is not None and pos.shape[-1] == l, "pos: a position for every token goes with rope")
             r = rope.at(pos)
+        nm = None if norm is None else norm.on(d, self._index)
         q = torch.empty((l, heads, d), dtype=torch.float32, device=self.device) if out is None else out
-        status = self._calls[0](self._ref, qkv.data_ptr(), ldx, l, heads, seq.data_ptr(),
-                                slot.data_ptr(), None if index is None else index.data_ptr(),
-                                None if r is None else ctypes.byref(r), q.data_ptr(),
-                                heads * d if out is None else _rows(q, "out", l, heads, d, self._index),
-                                self._stream())
+        args = (self._ref, qkv.data_ptr(), ldx, l, heads, seq.data_ptr(), slot.data_ptr(),
+                None if index is None else index.data_ptr(), None if r is None else ctypes.byref(r))
+        to = (q.data_ptr(), heads * d if out is None else _rows(q, "out", l, heads, d, self._index), self._stream())
+        if nm is None:
+            status = self._calls[0](*args, *to)
+        else:
+            status = M.lib().mosaic_kv_append_norm(*args, nm, *to)
         if status:
-            raise M.MosaicError("mosaic_kv_append", status)
+            raise M.MosaicError("mosaic_kv_append" if nm is None else "mosaic_kv_append_norm", status)
         return q
 
     def attend(self, q, lens, max_len: int, first=None, scale: float | None = None, decay: float = 1.0, out=None):

@@ -56,7 +56,7 @@ class mosaic_mask_io(ctypes.Structure):
                 ("pass_dev", ctypes.c_void_p), ("Ux_tm", ctypes.c_void_p), ("K_tm", ctypes.c_void_p)]
 
 
-KV_F32, KV_BF16, KV_F16 = 0, 1, 2
+KV_F32, KV_BF16, KV_F16, KV_Q4 = 0, 1, 2, 4
 
 
 class mosaic_kv_cache(ctypes.Structure):
@@ -72,6 +72,10 @@ class mosaic_rope(ctypes.Structure):
                 ("ldp", ctypes.c_int64)]
 
 
+class mosaic_head_norm(ctypes.Structure):
+    _fields_ = [("eps", ctypes.c_float), ("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p)]
+
+
 class mosaic_kernel_time(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 64), ("launches", ctypes.c_uint64), ("ms", ctypes.c_double)]
 
@@ -84,6 +88,7 @@ _PP = ctypes.POINTER(mosaic_params)
 _PK = ctypes.POINTER(mosaic_key)
 _PC = ctypes.POINTER(mosaic_kv_cache)
 _PR = ctypes.POINTER(mosaic_rope)
+_PN = ctypes.POINTER(mosaic_head_norm)
 
 _SIGS = {
     "mosaic_default_params": ([_PP], None),
@@ -138,6 +143,9 @@ _SIGS = {
                                 _P], _INT),
     "mosaic_rope_turns": ([_I64, ctypes.c_double, _P], _INT),
     "mosaic_kv_append": ([_PC, _P, _I64, _I64, _I64, _P, _P, _P, _PR, _P, _I64, _P], _INT),
+    "mosaic_kv_append_norm": ([_PC, _P, _I64, _I64, _I64, _P, _P, _P, _PR, _PN, _P, _I64, _P], _INT),
+    "mosaic_kv_row_bytes": ([_INT, _I64], _SZ),
+    "mosaic_kv_rows": ([_PC, _P, _P, _I64, _P, _P, _I64, _I64, _P], _INT),
     "mosaic_kv_attention_workspace": ([_PC, _I64, _I64], _SZ),
     "mosaic_kv_attention": ([_PC, _P, _I64, _I64, _P, _I64, _P, _F32, _F32, _P, _I64, _P, _SZ, _P], _INT),
     "mosaic_kv_evict_workspace": ([_PC, _I64, _I64], _SZ),
@@ -455,6 +463,19 @@ def mosaic_rope_turns(rot_dim, base):
 def mosaic_kv_append(cache, qkv, ldx, l, heads, seq, slot, index, rope, q, ldq, stream=None):
     _call("mosaic_kv_append", cache, _ptr(qkv), ldx, l, heads, _ptr(seq), _ptr(slot), _ptr(index), rope, _ptr(q),
           ldq, _stream(stream))
+
+
+def mosaic_kv_append_norm(cache, qkv, ldx, l, heads, seq, slot, index, rope, norm, q, ldq, stream=None):
+    _call("mosaic_kv_append_norm", cache, _ptr(qkv), ldx, l, heads, _ptr(seq), _ptr(slot), _ptr(index), rope, norm,
+          _ptr(q), ldq, _stream(stream))
+
+
+def mosaic_kv_row_bytes(type, head_dim) -> int:
+    return int(lib().mosaic_kv_row_bytes(type, head_dim))
+
+
+def mosaic_kv_rows(cache, seq, slot, l, k, v, ld_token, ld_head, stream=None):
+    _call("mosaic_kv_rows", cache, _ptr(seq), _ptr(slot), l, _ptr(k), _ptr(v), ld_token, ld_head, _stream(stream))
 
 
 def mosaic_kv_attention_workspace(cache, heads, max_len) -> int:

@@ -28,11 +28,12 @@ class DecodeSession:
     """``keep``: slots a sequence may hold (None: no eviction); it may run over
     by ``slack`` slots (up to max_len) before it is cut back, without the
     ``recent`` newest tokens.  ``rope``: its positions are the tokens' ordinals (one axis);
-    default: the usual rotation of the whole head at base 500000."""
+    default: the usual rotation of the whole head at base 500000.  ``norm``: norms of
+    the query and key heads.  ``dtype``: the cache's (``kvcache.INT4``: 4 bits)."""
 
     def __init__(self, layer: SecureDecoderLayer, seqs: int, max_len: int, page_size: int = 16,
                  dtype=torch.bfloat16, rope: KV.Rope | None = None, keep: int | None = None, recent: int = 0,
-                 slack: int = 0):
+                 slack: int = 0, norm: KV.HeadNorm | None = None):
         s, dev = layer.s, torch.device(layer.proto.device)
         if keep is not None and not (0 <= recent <= keep and slack >= 0 and keep >= 1):
             raise ValueError("keep, recent and slack: 1 <= keep, 0 <= recent <= keep, 0 <= slack")
@@ -45,6 +46,7 @@ class DecodeSession:
         self.cache = KV.PagedCache.empty(seqs * columns + 1, s.n_kv, page_size, s.head_dim, self.pages.table, dtype,
                                          weights=keep is not None)
         self.rope = KV.Rope(s.head_dim, 500000.0, device=dev) if rope is None else rope
+        self.norm = norm
         self.host_lens = [0] * seqs
         self.lens = torch.zeros(seqs, dtype=torch.int32, device=dev)     # cached slots
         self.seen = torch.zeros(seqs, dtype=torch.int32, device=dev)     # tokens so far
@@ -59,7 +61,8 @@ class DecodeSession:
         at = torch.arange(l, dtype=torch.int32, device=x.device)
 
         def attend(qkv):
-            q = self.cache.append(qkv, s.n_heads, torch.full_like(at, seq), at, at, rope=self.rope, pos=at)
+            q = self.cache.append(qkv, s.n_heads, torch.full_like(at, seq), at, at, rope=self.rope, pos=at,
+                                  norm=self.norm)
             k, v = (t.float().repeat_interleave(s.n_heads // s.n_kv, dim=0) for t in self.cache.read(seq, l))
             out = F.scaled_dot_product_attention(q.transpose(0, 1)[None], k[None], v[None], is_causal=True)
             return out[0].transpose(0, 1).reshape(l, -1)
@@ -80,7 +83,8 @@ class DecodeSession:
         after = max(self.host_lens) + 1
 
         def attend(qkv):
-            q = self.cache.append(qkv, s.n_heads, self._rows, self.lens, self.seen, rope=self.rope, pos=self.seen)
+            q = self.cache.append(qkv, s.n_heads, self._rows, self.lens, self.seen, rope=self.rope, pos=self.seen,
+                                  norm=self.norm)
             return self.cache.attend(q, self.lens + 1, after).reshape(self.seqs, -1)
 
         y = self.layer.forward(x, masks, attend=attend)
