@@ -35,6 +35,9 @@ constexpr int64_t kFewestJobs = 64;
 // on 8 heads of 64, windowed: 147, 122, 95, 93, 90 (256 KB).  With four heads a
 // unit 64 KB to 384 KB are within 4 and 12 per cent.
 constexpr int64_t kJobBytes = 256 * 1024;
+// Of a 4-bit cache, whose bytes take longer (32 KB, 64 KB, 128 KB, 256 KB): 48 sequences 90, 90, 95, 106; 64 of up to
+// 16384 197, 195, 196, 200; the windowed ones 111, 109, 110, 115.
+constexpr int64_t kJobBytesQ4 = 64 * 1024;
 
 // Block (c, y): the job that block c's end cuts.  Where jobs have many parts
 // (`shared`), query head y of it, its parts taken in turn by eight warps; else
@@ -309,7 +312,8 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     const int64_t jobs = cache->seqs * (cache->kv_heads / a.hpu) * a.hb;
     a.blocks = (int)(a.whole ? jobs : cap);
     const int64_t unit_bytes = 2 * s.unit * kv_row_bytes(cache->type, D);
-    a.job_cost = (int)((kJobBytes + unit_bytes / 2) / unit_bytes);
+    const int64_t job_bytes = cache->type == MOSAIC_KV_Q4 ? kJobBytesQ4 : kJobBytes;
+    a.job_cost = (int)((job_bytes + unit_bytes / 2) / unit_bytes);
     cudaStream_t st = as_stream(stream);
     MOSAIC_TRY(by_type(cache->type, [&](auto t) { return attend_launch<decltype(t)>(*cache, a, a.blocks, st); }));
     if (!a.whole) {

@@ -118,7 +118,7 @@ template <> constexpr float kScaleP<__half> = 0x1p15f;
 constexpr float kLeastP = 0x1p-14f, kPassP = 0x1p29f;
 
 constexpr int kTogether = 4;   // chains of products at a time
-constexpr int kLookup = 4 * 128 + 32;   // bytes of a producer's page ids and live slots
+template <int UNIT> constexpr int kLookup = 4 * (UNIT < 128 ? 128 : UNIT) + 32;   // bytes of a producer's page ids and live slots
 
 // A stage: K, then V of a unit; each in blocks of 128 bytes of all its rows,
 // 16-byte chunk c of row r at chunk c ^ (r % 8) of its block (the tensor copies'
@@ -151,10 +151,11 @@ struct Shape {
     // slots of the producers' groups, the queries' fragments, barriers and so on.
     static constexpr int kRing = kStages * kStage;
     static constexpr int kMerge = 4 * kSlots * kHeads * (kPitch + 2);
-    static constexpr int kIds = 2 * kLookup;
+    static constexpr int kIds = 2 * kLookup<kUnit>;
     static constexpr int kQAt = kRing + kMerge + kIds, kMiscAt = kQAt + 4 * kQWords * kQHeads;
     static constexpr int kMisc = 512 + 8 * kHeads * (kQReg ? kWarps : kQHeads);
     static constexpr int kBytes = kMiscAt + kMisc;
+    static constexpr int kProducers = 2;   // warps that copy
     // Boxes of a row and the bytes of one; tiles of 16 rows of a unit go head by head.
     static constexpr int kPieces = kRow / 128, kPiece = 128, kTiles = 8;
     static constexpr bool kParted = false;
@@ -162,7 +163,6 @@ struct Shape {
     static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kBlocks = kFit < 3 ? kFit : 3;   // blocks an SM
     static_assert(kBytes <= 227 * 1024, "shared memory");
 };
-constexpr int kProducers = 2;   // warps that copy
 
 template <class T, int DP, int NT>
 struct Warp {
@@ -598,8 +598,11 @@ constexpr int kLastUnit = 1 << 30;
 template <class T, int DP, int NT, bool TMA>
 struct Producer {
     using S = Shape<T, DP, NT>;
-    static constexpr int kSpan = TMA ? 256 : 128, kEach = TMA ? 1 : 4;   // rows of a group, look-ups of a lane
-    static constexpr int kUnits = kSpan / S::kUnit, kHalves = S::kUnit / 16, kTurn = TMA ? 1 : kProducers;
+    // Rows of a group, look-ups of a lane.
+    static constexpr int kSpan = TMA ? 256 : S::kUnit < 128 ? 128 : S::kUnit, kEach = TMA ? 1 : kSpan / 32;
+    static_assert(kSpan >= S::kUnit && kSpan % S::kUnit == 0 && kSpan <= 256, "a group holds whole units");
+    static constexpr int kUnits = kSpan / S::kUnit, kHalves = S::kUnit / 16, kTurn = TMA ? 1 : S::kProducers;
+    static constexpr int kBoth = S::kProducers == 1 ? 2 : 1;   // K and V by one warp
     struct Group {
         int h, hb, s, end, units, low;   // first head, first slot, end of the job's slots, units, position bound
         int unit, of, base;              // number of its first unit in the job, of how many, units of all jobs before
@@ -607,7 +610,7 @@ struct Producer {
     };
     const KvView &kv;
     const AttendArgs &a;
-    const CUtensorMap *map;
+    const CUtensorMap *map[kBoth];
     Pipe<T, DP, NT> &pipe;
     char *smem;
     // us: slots of a unit; per_tile: 2^8 over the tiles of a head, rounded up (kParted: the heads' logarithm)
@@ -626,11 +629,12 @@ struct Producer {
     __device__ __forceinline__ Producer(const KvView &kv_, const AttendArgs &a_, const CUtensorMap *mk,
                                         const CUtensorMap *mv, Pipe<T, DP, NT> &pipe_, int per_seq_, const Jobs &j,
                                         char *smem_, int pw_)
-        : kv(kv_), a(a_), map(pw_ ? mv : mk), pipe(pipe_), smem(smem_), per_seq(per_seq_), pw(pw_),
+        : kv(kv_), a(a_), map{pw_ ? mv : mk}, pipe(pipe_), smem(smem_), per_seq(per_seq_), pw(pw_),
           lane(threadIdx.x & 31), us(S::kUnit / a_.hpu),
           per_tile(S::kParted ? (a_.hpu >= 2) + (a_.hpu >= 4) : 256 / (us / 16) + 1), jobs(j) {
-        ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge + pw * kLookup);
-        live = reinterpret_cast<uint8_t *>(ids + 128);
+        if constexpr (kBoth == 2) map[1] = mv;
+        ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge + pw * kLookup<S::kUnit>);
+        live = reinterpret_cast<uint8_t *>(ids + (S::kUnit < 128 ? 128 : S::kUnit));
         job_units = job_at = count = units = 0;
         over = false;
         now.units = mid.units = far.units = 0;
@@ -697,7 +701,7 @@ struct Producer {
             if (!jobs.next(kv, a, us, per_seq)) over = true, job_units = 0;
             // A job without a slot (whole jobs only) is one unit without a live one.
             else job_units = max(1, jobs.b1 - jobs.b0);
-            job_at = TMA ? 0 : (pw + units) & (kProducers - 1);
+            job_at = TMA ? 0 : (pw + units) & (S::kProducers - 1);
         }
         if (!over) {
             far.i = jobs.i, far.h = jobs.r / a.hb * a.hpu, far.hb = jobs.r % a.hb, far.end = jobs.last(us);
@@ -779,7 +783,7 @@ struct Producer {
             if (any) {
 #pragma unroll
                 for (int k = 0; k < S::kRow / 128; ++k)
-                    tma_load_4d(to + k * 128 * S::kUnit, map, bar, k * 128 / S::kES, (int)offset(s), now.h, page);
+                    tma_load_4d(to + k * 128 * S::kUnit, map[0], bar, k * 128 / S::kES, (int)offset(s), now.h, page);
             }
         }
         __syncwarp();
@@ -798,11 +802,16 @@ struct Producer {
                 all += any >> (b * hpu) & each ? bytes : 0u;
                 page[b] = ids[(u * S::kUnit + 16 * b * hpu) / 8];
             }
-            mbar_expect_tx(bar, all);
+            mbar_expect_tx(bar, kBoth * all);
             char *to = smem + stage * S::kStage + pw * (S::kStage / 2);
 #pragma unroll
             for (int b = 0; b < N; ++b)
-                if (any >> (b * hpu) & each) tma_load_4d(to + b * bytes, map, bar, 0, (int)offset(s + 16 * b), now.h, page[b]);
+                if (any >> (b * hpu) & each) {
+                    const int off = (int)offset(s + 16 * b);
+#pragma unroll
+                    for (int x = 0; x < kBoth; ++x)
+                        tma_load_4d(to + x * (S::kStage / 2) + b * bytes, map[x], bar, 0, off, now.h, page[b]);
+                }
         }
         __syncwarp();
     }
@@ -821,7 +830,7 @@ struct Producer {
             const uint32_t mask = __ballot_sync(0xffffffffu, has);
             if (lane == 0) {
                 uint64_t *bar = pipe.full + stage;
-                mbar_expect_tx(bar, (uint32_t)(__popc(mask) * BOX) * S::kRow);
+                mbar_expect_tx(bar, (uint32_t)(kBoth * __popc(mask) * BOX) * S::kRow);
                 int page[N];
 #pragma unroll
                 for (int b = 0; b < N; ++b) page[b] = ids[(u * S::kUnit + b * BOX) / 8];
@@ -835,8 +844,10 @@ struct Producer {
                         const int c1 = a.token_major ? h : off, c2 = a.token_major ? off : h;
 #pragma unroll
                         for (int k = 0; k < S::kPieces; ++k)
-                            tma_load_4d(to + b * BOX * S::kPiece + k * 128 * S::kUnit, map, bar, k * 128 / S::kES, c1, c2,
-                                        page[b]);
+#pragma unroll
+                            for (int x = 0; x < kBoth; ++x)
+                                tma_load_4d(to + x * (S::kStage / 2) + b * BOX * S::kPiece + k * 128 * S::kUnit, map[x], bar,
+                                            k * 128 / S::kES, c1, c2, page[b]);
                     }
                     if constexpr (S::kParted) continue;
                     off += BOX, row += BOX;
@@ -949,11 +960,11 @@ __device__ __forceinline__ void cut_job(const AttendArgs &a, const Jobs &jobs, i
 }
 
 template <class T, int DP, int NT, bool TMA>
-__global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + kProducers),
+__global__ void __launch_bounds__(32 * (Shape<T, DP, NT>::kWarps + Shape<T, DP, NT>::kProducers),
                                   Shape<T, DP, NT>::kBlocks)
     attend_kernel(KvView kv, AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
     using S = Shape<T, DP, NT>;
-    constexpr int W = S::kWarps, P = kProducers, THREADS = 32 * W, ALL = THREADS + 32 * P, MS = S::kSlots;
+    constexpr int W = S::kWarps, P = S::kProducers, THREADS = 32 * W, ALL = THREADS + 32 * P, MS = S::kSlots;
     extern __shared__ __align__(1024) char smem[];
     static_assert(sizeof(Pipe<T, DP, NT>) <= S::kMisc, "pipe");
     Pipe<T, DP, NT> &pipe = *reinterpret_cast<Pipe<T, DP, NT> *>(smem + S::kMiscAt);
@@ -1142,7 +1153,7 @@ int resident() {
     if (!ensure_smem_limit(done, kernel, S::kBytes, &dev)) return 0;
     std::atomic<int> &at = known[dev & 63];
     if ((n = at.load(std::memory_order_relaxed)) > 0) return n;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, 32 * (S::kWarps + kProducers), S::kBytes) != cudaSuccess)
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, 32 * (S::kWarps + S::kProducers), S::kBytes) != cudaSuccess)
         return 0;
     n *= sm_count(dev);
     at.store(n, std::memory_order_relaxed);
@@ -1196,7 +1207,7 @@ struct Instance {
         blocks = a.blocks;
         {
             KernelSpan span("attend", st);
-            const dim3 grid((unsigned)a.blocks), block(32 * (S::kWarps + kProducers));
+            const dim3 grid((unsigned)a.blocks), block(32 * (S::kWarps + S::kProducers));
             // More than one wave (whole jobs) must not stack up early.
             if (a.blocks <= wave) pdl_launch(attend_kernel<T, DP, NT, TMA>, grid, block, S::kBytes, st, kv, a, mk, mv);
             else attend_kernel<T, DP, NT, TMA><<<grid, block, S::kBytes, st>>>(kv, a, mk, mv);

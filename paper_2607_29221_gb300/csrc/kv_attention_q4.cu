@@ -28,23 +28,27 @@
 namespace mosaic {
 namespace {
 
-template <int DP, int NT>
-struct Shape<Q4, DP, NT> {
+// TMA: copies by tensor boxes, one producer warp; else by lanes, two.
+template <bool TMA>
+struct Packed {};
+
+template <bool TMA, int DP, int NT>
+struct Shape<Packed<TMA>, DP, NT> {
     static constexpr int kES = 1, kRow = (5 * DP / 8 + 15) / 16 * 16, kChunks = kRow / 16;
-    static constexpr int kWarps = 4, kUnit = 32 * kWarps, kStage = 2 * kUnit * kRow;
+    static constexpr int kProducers = TMA ? 1 : 2, kWarps = 4, kUnit = 32 * kWarps, kStage = 2 * kUnit * kRow;
     static constexpr int kStages = DP == 64 ? 3 : 2;
     static constexpr int kSlots = 2;
     static constexpr int kSteps = DP / 16, kHeads = 8 * NT, kPitch = DP + 4;
     static constexpr int kQWords = kSteps * NT * 4 * 32;
     static constexpr bool kQReg = false;
     static constexpr int kQHeads = DP * NT <= 128 ? 4 : DP * NT == 256 ? 2 : 1;
-    static constexpr int kRing = kStages * kStage, kMerge = 4 * kSlots * kHeads * (kPitch + 2), kIds = 2 * kLookup;
+    static constexpr int kRing = kStages * kStage, kMerge = 4 * kSlots * kHeads * (kPitch + 2), kIds = kProducers * kLookup<kUnit>;
     static constexpr int kQAt = (kRing + kMerge + kIds + 15) / 16 * 16, kMiscAt = kQAt + 4 * kQWords * kQHeads;
     static constexpr int kMisc = 512 + 8 * kHeads * kQHeads, kBytes = kMiscAt + kMisc;
     static constexpr int kPieces = 1, kPiece = kRow, kTiles = kUnit / 16;
     static constexpr bool kParted = true;
     static __device__ __forceinline__ uint32_t at(int r, int c) { return (uint32_t)(r * kRow + 16 * c); }
-    static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kMost = DP * NT <= 128 ? 3 : DP * NT == 256 ? 2 : 1;
+    static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kMost = DP * NT <= (TMA ? 128 : 64) ? 3 : DP * NT <= 256 ? 2 : 1;
     static constexpr int kBlocks = kFit < kMost ? kFit : kMost;
     static_assert(kBytes <= 227 * 1024 && kBlocks >= 1, "shared memory");
 };
@@ -64,9 +68,9 @@ __device__ __forceinline__ void lds_words(uint32_t *r, uint32_t a) {
                          : "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]) : "r"(a + 4 * i) : "memory");
 }
 
-template <int DP, int NT>
+template <bool TMA, int DP, int NT>
 struct Warp4 {
-    using S = Shape<Q4, DP, NT>;
+    using S = Shape<Packed<TMA>, DP, NT>;
     // Words of codes of a lane: of a key row (channels DP / 4 t on), of a value row (DP / 8 g on); groups of the former.
     static constexpr int kKW = DP / 32, kVW = DP / 64, kKG = DP == 256 ? 2 : 1, kN = DP / 8;
     float m[NT], l[NT], unscale[NT], o[NT][kN][2];   // of head g; channels DP / 8 (2t + j) + i
@@ -267,11 +271,12 @@ struct Warp4 {
 };
 
 template <int DP, int NT, bool TMA>
-__global__ void __launch_bounds__(32 * (Shape<Q4, DP, NT>::kWarps + kProducers), Shape<Q4, DP, NT>::kBlocks)
+__global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Shape<Packed<TMA>, DP, NT>::kProducers),
+                                  Shape<Packed<TMA>, DP, NT>::kBlocks)
     attend4_kernel(KvView kv, AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
-    using S = Shape<Q4, DP, NT>;
-    using P = Pipe<Q4, DP, NT>;
-    constexpr int W = S::kWarps, THREADS = 32 * W, ALL = THREADS + 32 * kProducers, MS = S::kSlots, kN = DP / 8;
+    using S = Shape<Packed<TMA>, DP, NT>;
+    using P = Pipe<Packed<TMA>, DP, NT>;
+    constexpr int W = S::kWarps, THREADS = 32 * W, ALL = THREADS + 32 * S::kProducers, MS = S::kSlots, kN = DP / 8;
     extern __shared__ __align__(1024) char smem[];
     static_assert(sizeof(P) <= S::kMisc, "pipe");
     P &pipe = *reinterpret_cast<P *>(smem + S::kMiscAt);
@@ -281,7 +286,7 @@ __global__ void __launch_bounds__(32 * (Shape<Q4, DP, NT>::kWarps + kProducers),
     if (tid == 0) {
         pipe.aborted = 0;
         for (int x = 0; x < S::kStages; ++x) {
-            mbar_init(pipe.full + x, TMA ? kProducers : 32 + 1);
+            mbar_init(pipe.full + x, TMA ? S::kProducers : 32 + 1);
             mbar_init(pipe.empty + x, W);
         }
         mbar_init_fence();
@@ -302,7 +307,7 @@ __global__ void __launch_bounds__(32 * (Shape<Q4, DP, NT>::kWarps + kProducers),
         if (tid == 0) a.split[3 * blockIdx.x] = -1;
     }
     if (w >= W) {
-        Producer<Q4, DP, NT, TMA> producer(kv, a, &mk, &mv, pipe, per_seq, jobs, smem, w - W);
+        Producer<Packed<TMA>, DP, NT, TMA> producer(kv, a, &mk, &mv, pipe, per_seq, jobs, smem, w - W);
         if (!producer.run()) {
             *(volatile int *)&pipe.aborted = 1;   // results are void; the device status says so
             if (lane == 0) atomicExch(&g_attend_error, 1u);
@@ -311,7 +316,7 @@ __global__ void __launch_bounds__(32 * (Shape<Q4, DP, NT>::kWarps + kProducers),
         return;
     }
 
-    Warp4<DP, NT> wp;
+    Warp4<TMA, DP, NT> wp;
     int stage = 0, parity = 0;
     // The warp's head of a unit's, and which pair of the head's tiles of 16 slots.
     const int of_head = W / a.hpu, hi = w / of_head, sub = w - hi * of_head;
@@ -441,17 +446,18 @@ __global__ void __launch_bounds__(32 * (Shape<Q4, DP, NT>::kWarps + kProducers),
 
 template <int DP, int NT>
 struct Instance4 {
-    using S = Shape<Q4, DP, NT>;
+    using S = Shape<Packed<true>, DP, NT>;   // units, heads and buffers are those of the other one too
     static AttendShape shape() { return {S::kHeads, DP, S::kUnit, S::kQHeads, S::kSlots, S::kBlocks}; }
     template <bool TMA>
     static mosaic_status go(const KvView &kv, AttendArgs a, const CUtensorMap &mk, const CUtensorMap &mv, int &blocks, cudaStream_t st) {
+        using S = Shape<Packed<TMA>, DP, NT>;
         const int wave = resident<S, attend4_kernel<DP, NT, TMA>>();
         if (wave <= 0) return MOSAIC_ERR_CUDA;
         if (!a.whole && a.blocks > wave) a.blocks = wave;
         blocks = a.blocks;
         {
             KernelSpan span("attend4", st);
-            const dim3 grid((unsigned)a.blocks), block(32 * (S::kWarps + kProducers));
+            const dim3 grid((unsigned)a.blocks), block(32 * (S::kWarps + S::kProducers));
             // More than one wave (whole jobs) must not stack up early.
             if (a.blocks <= wave) pdl_launch(attend4_kernel<DP, NT, TMA>, grid, block, S::kBytes, st, kv, a, mk, mv);
             else attend4_kernel<DP, NT, TMA><<<grid, block, S::kBytes, st>>>(kv, a, mk, mv);

@@ -88,18 +88,25 @@ inline mosaic_status kv_check(const mosaic_kv_cache *c) {
 // Rows of 4-bit codes: channel c of a row is code (word c / 8) >> 4 (c % 8) & 15
 // and stands for base + code step, one fused fp16 operation, where step and
 // base are the halves of word c / 32 of the row's last part.
+// (x & mask) | bits as one instruction: with both constants the compiler makes two of it.
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(x), "r"(mask), "r"(bits));
+    return y;
+}
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
 __device__ __forceinline__ uint32_t as_word(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
 // Codes k and k + 4 (counted from the lowest) of a word as values, k = 0 .. 3,
 // packed with the lower one first.  A code or'ed into the mantissa of 1024 is
 // 1024 + code, or 1024 + 16 code: both come off exactly.
 __device__ __forceinline__ void q4_values(uint32_t w, __half2 step, __half2 base, uint32_t (&y)[4]) {
+    const uint32_t magic = 0x64006400u;
     const __half2 one = as_half2(0xe400e400u), part = as_half2(0x2c002c00u), rest = as_half2(0xd400d400u);   // -1024, 1/16, -64
 #pragma unroll
     for (int k = 0; k < 4; k += 2) {
         const uint32_t x = k ? w >> 8 : w;
-        const __half2 lo = __hadd2(as_half2((x & 0x000f000fu) | 0x64006400u), one);
-        const __half2 hi = __hfma2(as_half2((x & 0x00f000f0u) | 0x64006400u), part, rest);
+        const __half2 lo = __hadd2(as_half2(and_or(x, 0x000f000fu, magic)), one);
+        const __half2 hi = __hfma2(as_half2(and_or(x, 0x00f000f0u, magic)), part, rest);
         y[k] = as_word(__hfma2(lo, step, base));
         y[k + 1] = as_word(__hfma2(hi, step, base));
     }
