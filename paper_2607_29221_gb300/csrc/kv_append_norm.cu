@@ -24,7 +24,10 @@
 namespace mosaic {
 namespace {
 
-constexpr int kThreads = 256, kRound = 4;   // heads in flight of a thread
+// Threads, blocks an SM and heads in flight of a thread.  2048 tokens of 64 + 16 heads of 128 with norms / 9001 of 28 +
+// 8 without, 4 bits: 42 / 72 us (4 blocks, 4 heads), 37 / 67 (4, 2), 35 / 64 (5, 2), 36 / 62 (6, 1); 5003 of 32 + 64 with
+// norms, fp32: 84, 86, 82, 84.
+constexpr int kThreads = 256, kResident = 5, kRound = 2;
 
 // A sum h + l of two floats, |l| at most half an ulp of h.
 struct Two {
@@ -80,164 +83,201 @@ __device__ __forceinline__ float root(Two a) {
 
 struct NormArgs {
     float eps;
-    int on;
     const float *q_gain, *k_gain;
-    Two over_dim;   // 1 / head_dim
+    Two over_dim;      // 1 / head_dim
+    int log_threads;   // of a head: head_dim / 8, rounded up to a power of two
 };
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) append_norm_kernel(KvView kv, AppendArgs a, NormArgs nm) {
-    constexpr bool kExact = std::is_same<T, Q4>::value;
-    __shared__ __align__(16) float cs[128], sn[128];
-    __shared__ __align__(16) float stage[kExact ? kRound * kThreads * 8 : 4];
+// Channel c of a staged row: 32 and 4 floats of padding (threads read 32 neighbours each).
+__device__ __forceinline__ int staged(int c) { return c + c / 32 * 4; }
+
+// Sum over the threads of a head (a power of two of neighbours).
+__device__ __forceinline__ float head_sum(float x, int threads) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < threads) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+// 1 / sqrt(mean of the head's squares + eps), rounded once.
+__device__ __forceinline__ float exact_root(const Load4 &x, const Load4 &y, bool live, int threads, const NormArgs &nm) {
+    Two z = {0.0f, 0.0f};
+    if (live) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = i < 4 ? x.x[i & 3] : y.x[i & 3], p = __fmul_rn(v, v);
+            const Two w = two_sum(z.h, p);
+            z = {w.h, __fadd_rn(z.l, __fadd_rn(w.l, __fmaf_rn(v, v, -p)))};
+        }
+    }
+    z = fast_two(z.h, z.l);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < threads) z = add(z, {__shfl_xor_sync(0xffffffffu, z.h, o), __shfl_xor_sync(0xffffffffu, z.l, o)});
+    return root(add(mul(z, nm.over_dim), {nm.eps, 0.0f}));
+}
+template <bool kExact>
+__device__ __forceinline__ void turn(float &p, float &q, float c, float s) {
+    const float p0 = p, q0 = q;
+    if constexpr (kExact) {
+        p = __fsub_rn(__fmul_rn(p0, c), __fmul_rn(q0, s));
+        q = __fadd_rn(__fmul_rn(q0, c), __fmul_rn(p0, s));
+    } else {
+        p = p0 * c - q0 * s;
+        q = q0 * c + p0 * s;
+    }
+}
+
+template <class T, bool kNorm, bool kVec>
+__global__ void __launch_bounds__(kThreads, kResident) append_norm_kernel(KvView kv, AppendArgs a, NormArgs nm) {
+    constexpr bool kPacked = std::is_same<T, Q4>::value;
+    __shared__ __align__(16) float cs[128], sn[128], gain[kNorm ? 512 : 4];   // gains: the queries', then the keys'
+    __shared__ __align__(16) float stage[kPacked ? kRound * kThreads * 9 : 4];
     const int64_t t = blockIdx.y + (int64_t)blockIdx.z * 65535;
     if (t >= a.l) return;
-    const int D = kv.c.head_dim, units = D / 8, rot = a.rope.rot_dim;
-    int pu = 1;   // threads of a head
-    while (pu < units) pu *= 2;
-    const int u = threadIdx.x % pu, lane = threadIdx.x / pu, lanes = kThreads / pu;
-    const bool in = u < units, spins = 8 * u < rot;
+    const int D = kv.c.head_dim, rot = a.rope.rot_dim, threads = 1 << nm.log_threads;
+    const int u = threadIdx.x & (threads - 1), lane = threadIdx.x >> nm.log_threads, lanes = kThreads >> nm.log_threads;
+    const bool in = 8 * u < D, spins = 8 * u < rot;
+    // The thread's channels c0 .. c0 + 3 and c1 .. c1 + 3 of every head, in the
+    // halves of the channels that turn or of those that do not.
     const int c0 = spins ? 4 * u : rot + 4 * (u - rot / 8), c1 = c0 + (spins ? rot : D - rot) / 2;
     const int H = a.heads, KV = kv.c.kv_heads;
-    const int first = blockIdx.x * a.share, last = min(first + a.share, H + 2 * KV);
+    const int first = blockIdx.x * a.share, last = min(first + a.share, H + 2 * KV), queries = min(last, H);
     const float *row = a.qkv + t * a.ldx;
-    float *qrow = a.q + t * a.ldq;
     Load4 xs[kRound], ys[kRound];
-    auto load = [&](int h0) {
+    auto load = [&](int h, int end) {   // heads h + lane, + lanes and so on, below end
+        const float *p = row + (h + lane) * D;
 #pragma unroll
-        for (int k = 0; k < kRound; ++k)
-            if (in && h0 + k * lanes < last) {
-                xs[k] = load4(row + (int64_t)(h0 + k * lanes) * D + c0, a.vec);
-                ys[k] = load4(row + (int64_t)(h0 + k * lanes) * D + c1, a.vec);
-            }
+        for (int k = 0; k < kRound; ++k, p += lanes * D)
+            if (in && h + lane + k * lanes < end) xs[k] = load4(p + c0, kVec), ys[k] = load4(p + c1, kVec);
     };
-    int base = first;
-    load(base + lane);   // under way while the phases are looked up
-    for (int j = threadIdx.x; j < rot / 2; j += kThreads) {
+    int base = max(first, H);   // keys and values first: they are packed while the queries come
+    if (base < last) load(base, last);
+    else load(first, queries);
+    if constexpr (kNorm)
+        for (int j = threadIdx.x; j < 2 * D; j += kThreads) {
+            const float *g = j < D ? nm.q_gain : nm.k_gain;
+            gain[j] = g ? g[j < D ? j : j - D] : 1.0f;
+        }
+    if ((int)threadIdx.x < rot / 2) {
+        const int j = threadIdx.x;
         int ax = a.rope.axis ? a.rope.axis[j] : 0;
         ax = (uint32_t)ax < (uint32_t)a.rope.axes ? ax : 0;
         const int64_t pos = a.rope.pos[ax * a.rope.ldp + t];
         const int32_t phase = (int32_t)(((uint64_t)pos * a.rope.turns[j]) >> 32);
-        if constexpr (kExact) spin(phase, cs[j], sn[j]);
+        if constexpr (kPacked) spin(phase, cs[j], sn[j]);
         else sincospif((float)phase * 0x1p-31f, &sn[j], &cs[j]);
     }
-    const int64_t sq = a.seq[t], sl = a.slot[t];
     int id = -1;
-    uint32_t off = 0;
-    if (sq >= 0 && sq < kv.c.seqs && sl >= 0 && sl < kv.slots()) id = kv.page_of(sq, (uint32_t)sl, off);
-    auto gains = [&](const float *g, Load4 &x, Load4 &y) {
-        for (int i = 0; i < 4; ++i) x.x[i] = g && in ? g[c0 + i] : 1.0f, y.x[i] = g && in ? g[c1 + i] : 1.0f;
-    };
-    Load4 gq[2], gk[2];
-    if (nm.on) gains(nm.q_gain, gq[0], gq[1]), gains(nm.k_gain, gk[0], gk[1]);
+    int64_t at = 0, mark = 0;   // of head 0
+    if (base < last) {
+        const int64_t sq = a.seq[t], sl = a.slot[t];
+        uint32_t off = 0;
+        if (sq >= 0 && sq < kv.c.seqs && sl >= 0 && sl < kv.slots()) id = kv.page_of(sq, (uint32_t)sl, off);
+        if (id >= 0) at = kv.element(id, 0, off), mark = kv.mark(id, 0, off);
+    }
     __syncthreads();
+    float c[4], s[4];   // of c0 + i with c1 + i, or of neighbours
+    if (spins) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = !a.rope.interleaved ? c0 + i : i < 2 ? c0 / 2 + i : c1 / 2 + i - 2;
+            c[i] = cs[j], s[i] = sn[j];
+        }
+    }
+    auto scale = [&](Load4 &x, Load4 &y, float r, const float *g) {
+        const Load4 g0 = load4(g + c0, true), g1 = load4(g + c1, true);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x.x[i] = __fmul_rn(__fmul_rn(x.x[i], r), g0.x[i]);
+            y.x[i] = __fmul_rn(__fmul_rn(y.x[i], r), g1.x[i]);
+        }
+    };
+    auto rotate = [&](Load4 &x, Load4 &y, auto exact) {
+        constexpr bool kExact = decltype(exact)::value;
+        if (!a.rope.interleaved) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) turn<kExact>(x.x[i], y.x[i], c[i], s[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i += 2)
+                turn<kExact>(x.x[i], x.x[i + 1], c[i / 2], s[i / 2]), turn<kExact>(y.x[i], y.x[i + 1], c[2 + i / 2], s[2 + i / 2]);
+        }
+    };
+    auto fast_root = [&](const Load4 &x, const Load4 &y, bool live) {
+        float ss = 0.0f;
+        if (live) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ss = fmaf(x.x[i], x.x[i], fmaf(y.x[i], y.x[i], ss));
+        }
+        return rsqrtf(fmaf(head_sum(ss, threads), nm.over_dim.h, nm.eps));
+    };
+
     for (; base < last; base += kRound * lanes) {   // the block's: shuffles and barriers inside
 #pragma unroll
         for (int k = 0; k < kRound; ++k) {
-            const int h = base + k * lanes + lane;
-            const bool live = in && h < last;
+            if (base + k * lanes >= last) break;   // the block's
+            const int h = base + k * lanes + lane, g = h - H < KV ? h - H : h - H - KV;
+            const bool live = in && h < last, key = h < H + KV;
             Load4 &x = xs[k], &y = ys[k];
-            if (nm.on && base + k * lanes < min(last, H + KV)) {
-                float r, ss = 0.0f;
-                if (live) {
+            if (kNorm && base + k * lanes < H + KV) {
+                float r;
+                if constexpr (kPacked) r = exact_root(x, y, live, threads, nm);
+                else r = fast_root(x, y, live);
+                if (live && key) scale(x, y, r, gain + D);
+            }
+            if (!live || id < 0) continue;
+            if (spins && key) rotate(x, y, std::integral_constant<bool, kPacked>());
+            if constexpr (kPacked) {
+                float *o = stage + (k * lanes + lane) * (D + D / 8);
+                store4(o + staged(c0), x, true);
+                store4(o + staged(c1), y, true);
+            } else {
+                T *o = static_cast<T *>(key ? kv.c.k : kv.c.v) + at + g * kv.c.head_stride;
+                put4(o + c0, x);
+                put4(o + c1, y);
+            }
+            if (u == 0 && key) {
+                if (kv.c.position) kv.c.position[mark + g * kv.c.page_size] = a.index[t];
+                if (kv.c.weight) kv.c.weight[mark + g * kv.c.page_size] = 0.0f;
+            }
+        }
+        const int next = base + kRound * lanes;
+        if (next < last) load(next, last);
+        else load(first, queries);
+        if (!kPacked || id < 0) continue;   // the block's
+        __syncthreads();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) ss = fmaf(x.x[i], x.x[i], fmaf(y.x[i], y.x[i], ss));
-                }
-                for (int o = pu / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                r = rsqrtf(fmaf(ss, nm.over_dim.h, nm.eps));
-                if constexpr (kExact) {
-                    if (__any_sync(0xffffffffu, h >= H && h < H + KV)) {
-                        Two s = {0.0f, 0.0f};
-                        if (live) {
+        for (int k = 0; k < kRound; ++k) {   // a thread 8 channels
+            if (base + k * lanes >= last) break;   // the block's
+            const int r = k * lanes + lane, h = base + r - H;
+            const bool mine = in && base + r < last;
+            uint32_t codes;
+            const uint32_t scales = q4_pack(stage + (mine ? r * (D + D / 8) + staged(8 * u) : 0), codes);
+            if (mine) {
+                char *o = (h < KV ? static_cast<char *>(kv.c.k) : static_cast<char *>(kv.c.v)) + at + (h < KV ? h : h - KV) * kv.c.head_stride;
+                *reinterpret_cast<uint32_t *>(o + 4 * u) = codes;
+                if (u % 4 == 0) *reinterpret_cast<uint32_t *>(o + D / 2 + u) = scales;
+            }
+        }
+        if (next < last) __syncthreads();
+    }
+    float *q = a.q + t * a.ldq + (first + lane) * D;
+    for (base = first; base < queries; base += kRound * lanes) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const float v = i < 4 ? x.x[i & 3] : y.x[i & 3], p = __fmul_rn(v, v);
-                                s = add(s, {p, __fmaf_rn(v, v, -p)});
-                            }
-                        }
-                        for (int o = pu / 2; o > 0; o >>= 1)
-                            s = add(s, {__shfl_xor_sync(0xffffffffu, s.h, o), __shfl_xor_sync(0xffffffffu, s.l, o)});
-                        const float rk = root(add(mul(s, nm.over_dim), {nm.eps, 0.0f}));
-                        r = h >= H ? rk : r;
-                    }
-                }
-                if (h < H + KV) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x.x[i] = __fmul_rn(__fmul_rn(x.x[i], r), h < H ? gq[0].x[i] : gk[0].x[i]);
-                        y.x[i] = __fmul_rn(__fmul_rn(y.x[i], r), h < H ? gq[1].x[i] : gk[1].x[i]);
-                    }
-                }
+        for (int k = 0; k < kRound; ++k, q += lanes * D) {
+            if (base + k * lanes >= queries) break;   // the block's
+            const bool live = in && base + k * lanes + lane < queries;
+            Load4 &x = xs[k], &y = ys[k];
+            if constexpr (kNorm) {
+                const float r = fast_root(x, y, live);
+                if (live) scale(x, y, r, gain);
             }
             if (!live) continue;
-            if (spins && h < H + KV) {
-                auto turn = [&](float &p, float &q, int j) {
-                    const float c = cs[j], s = sn[j], p0 = p, q0 = q;
-                    if constexpr (kExact) {
-                        p = __fsub_rn(__fmul_rn(p0, c), __fmul_rn(q0, s));
-                        q = __fadd_rn(__fmul_rn(q0, c), __fmul_rn(p0, s));
-                    } else {
-                        p = p0 * c - q0 * s;
-                        q = q0 * c + p0 * s;
-                    }
-                };
-                if (!a.rope.interleaved) {   // channel c0 + i with c1 + i
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) turn(x.x[i], y.x[i], c0 + i);
-                } else {                     // neighbours
-#pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        turn(x.x[i], x.x[i + 1], (c0 + i) / 2);
-                        turn(y.x[i], y.x[i + 1], (c1 + i) / 2);
-                    }
-                }
-            }
-            if (h < H) {
-                store4(qrow + (int64_t)h * D + c0, x, a.vec);
-                store4(qrow + (int64_t)h * D + c1, y, a.vec);
-            } else if (id >= 0) {
-                const int g = h < H + KV ? h - H : h - H - KV;
-                if constexpr (kExact) {
-                    float *o = stage + (k * lanes + lane) * D;
-                    store4(o + c0, x, true);
-                    store4(o + c1, y, true);
-                } else {
-                    T *o = static_cast<T *>(h < H + KV ? kv.c.k : kv.c.v) + kv.element(id, g, off);
-                    put4(o + c0, x);
-                    put4(o + c1, y);
-                }
-                if (u == 0 && h < H + KV) {
-                    if (kv.c.position) kv.c.position[kv.mark(id, g, off)] = a.index[t];
-                    if (kv.c.weight) kv.c.weight[kv.mark(id, g, off)] = 0.0f;
-                }
-            }
+            if (spins) rotate(x, y, std::false_type());
+            store4(q + c0, x, kVec);
+            store4(q + c1, y, kVec);
         }
-        const int round = base;
-        load(base + kRound * lanes + lane);
-        if constexpr (kExact) {
-            if (id < 0 || min(last, round + kRound * lanes) <= H) continue;   // the block's
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < kRound; ++k) {
-                const int r = k * lanes + lane, h = round + r;
-                const bool row = in && h >= H && h < last;
-                float y[8];
-                if (row) {
-                    const Load4 p = load4(stage + r * D + 8 * u, true), q = load4(stage + r * D + 8 * u + 4, true);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = p.x[i], y[4 + i] = q.x[i];
-                }
-                uint32_t codes;
-                const uint32_t scales = q4_pack(y, codes);
-                if (row) {
-                    const int g = h < H + KV ? h - H : h - H - KV;
-                    char *o = static_cast<char *>(h < H + KV ? kv.c.k : kv.c.v) + kv.element(id, g, off);
-                    *reinterpret_cast<uint32_t *>(o + 4 * u) = codes;
-                    if (u % 4 == 0) *reinterpret_cast<uint32_t *>(o + D / 2 + u) = scales;
-                }
-            }
-            __syncthreads();
-        }
+        load(base + kRound * lanes, queries);
     }
 }
 
@@ -246,17 +286,21 @@ __global__ void __launch_bounds__(kThreads) append_norm_kernel(KvView kv, Append
 mosaic_status append_norm_launch(const mosaic_kv_cache &c, AppendArgs a, const mosaic_head_norm *norm, cudaStream_t st) {
     const KvView kv(c);
     NormArgs nm = {};
-    if (norm) nm.on = 1, nm.eps = norm->eps, nm.q_gain = norm->q_gain, nm.k_gain = norm->k_gain;
+    if (norm) nm.eps = norm->eps, nm.q_gain = norm->q_gain, nm.k_gain = norm->k_gain;
     nm.over_dim = two(1.0 / kv.c.head_dim);
-    int pu = 1;
-    while (pu < kv.c.head_dim / 8) pu *= 2;
-    const dim3 grid = append_grid(kv.c, a, kThreads / pu);
+    while (8 << nm.log_threads < c.head_dim) ++nm.log_threads;
+    const dim3 grid = append_grid(c, a, kThreads >> nm.log_threads);
     {
         KernelSpan span("append_norm", st);
-        if (kv.c.type == MOSAIC_KV_F32) append_norm_kernel<float><<<grid, kThreads, 0, st>>>(kv, a, nm);
-        else if (kv.c.type == MOSAIC_KV_BF16) append_norm_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(kv, a, nm);
-        else if (kv.c.type == MOSAIC_KV_F16) append_norm_kernel<__half><<<grid, kThreads, 0, st>>>(kv, a, nm);
-        else append_norm_kernel<Q4><<<grid, kThreads, 0, st>>>(kv, a, nm);
+        auto go = [&](auto t, auto on) {
+            if (a.vec) append_norm_kernel<decltype(t), decltype(on)::value, true><<<grid, kThreads, 0, st>>>(kv, a, nm);
+            else append_norm_kernel<decltype(t), decltype(on)::value, false><<<grid, kThreads, 0, st>>>(kv, a, nm);
+        };
+        if (c.type == MOSAIC_KV_F32) go(float(), std::true_type());
+        else if (c.type == MOSAIC_KV_BF16) go(__nv_bfloat16(), std::true_type());
+        else if (c.type == MOSAIC_KV_F16) go(__half(), std::true_type());
+        else if (norm) go(Q4(), std::true_type());
+        else go(Q4(), std::false_type());
     }
     return launch_status();
 }

@@ -112,35 +112,48 @@ __device__ __forceinline__ void q4_values(uint32_t w, __half2 step, __half2 base
     }
 }
 
-// The word of codes of 8 channels, and the group's step and base (in that
-// order).  Every thread of a warp calls it; four neighbours have a group.
-__device__ __forceinline__ uint32_t q4_pack(const float (&y)[8], uint32_t &codes) {
+__device__ __forceinline__ float min_or_nan(float x, float y) {
+    float z;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
+__device__ __forceinline__ float max_or_nan(float x, float y) {
+    float z;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
+// 8 channels (16-byte aligned) of a group that four neighbouring threads have:
+// their word of codes and, in this order, the group's step and base.  Every
+// thread of a warp calls it.
+__device__ __forceinline__ uint32_t q4_pack(const float *channels, uint32_t &codes) {
     constexpr float kMost = 65000.0f;   // base + 15 step stays finite in fp16
-    float x[8], least, most;
-    bool fine = true;
+    const float4 lower = reinterpret_cast<const float4 *>(channels)[0], upper = reinterpret_cast<const float4 *>(channels)[1];
+    float y[8] = {lower.x, lower.y, lower.z, lower.w, upper.x, upper.y, upper.z, upper.w};
+    float least = y[0], most = y[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        fine &= fabsf(y[i]) < __int_as_float(0x7f800000);
-        x[i] = fminf(fmaxf(y[i], -kMost), kMost);
-        least = i ? fminf(least, x[i]) : x[i], most = i ? fmaxf(most, x[i]) : x[i];
-    }
+    for (int i = 1; i < 8; ++i) least = min_or_nan(least, y[i]), most = max_or_nan(most, y[i]);
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
-        least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
-        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        fine &= (bool)__shfl_xor_sync(0xffffffffu, (int)fine, o);
+        least = min_or_nan(least, __shfl_xor_sync(0xffffffffu, least, o));
+        most = max_or_nan(most, __shfl_xor_sync(0xffffffffu, most, o));
+    }
+    codes = 0;
+    if (!(least >= -kMost && most <= kMost)) {
+        if (!(least >= -3.4028234e38f && most <= 3.4028234e38f)) return 0x7fff0000u;   // NaN or infinities among them
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(y[i], -kMost), kMost);
+        least = fminf(fmaxf(least, -kMost), kMost), most = fminf(fmaxf(most, -kMost), kMost);
     }
     const __half base = __float2half_rn(least), step = __float2half_rn(__fmul_rn(__fsub_rn(most, least), (float)(1.0 / 15.0)));
-    const float from = __half2float(base), s = __half2float(step), inv = s > 0.0f ? __fdiv_rn(1.0f, s) : 0.0f;
-    codes = 0;
+    const float from = __half2float(base), s = __half2float(step), inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+    // 2^23 + code, rounded to the nearest even whole number, has the code in its
+    // lowest bits: 8 of them are summed in steps of 16, and what the exponents
+    // add up to is taken off.
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float c = rintf(__fmul_rn(__fsub_rn(x[i], from), inv));
-        codes |= (uint32_t)fminf(fmaxf(c, 0.0f), 15.0f) << (4 * i);
-    }
-    if (fine) return as_word(__halves2half2(step, base));
-    codes = 0;
-    return 0x7fff0000u;   // step 0, base NaN
+    for (int i = 7; i >= 0; --i)
+        codes = codes * 16 + __float_as_uint(__fadd_rn(fminf(fmaxf(__fmul_rn(__fsub_rn(y[i], from), inv), 0.0f), 15.0f), 0x1p23f));
+    codes -= 0x4b000000u * 0x11111111u;
+    return as_word(__halves2half2(step, base));
 }
 
 template <class T> struct Elem;

@@ -212,11 +212,11 @@ class PagedCache:
         l, h, d = slot.numel(), self.kv_heads, self.head_dim
         _int32(seq, "seq", l, self._index)
         _int32(slot, "slot", l, self._index)
-        shape, strides = ((l, h, d), (h * d, d)) if token_major else ((h, l, d), (d, l * d))
         dtype = torch.float16 if self.k.dtype is INT4 else self.k.dtype
-        k, v = (torch.empty(shape, dtype=dtype, device=self.device) for _ in range(2))
+        k = torch.empty((l, h, d) if token_major else (h, l, d), dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
         status = M.lib().mosaic_kv_rows(self._ref, seq.data_ptr(), slot.data_ptr(), l, k.data_ptr(), v.data_ptr(),
-                                        *strides, self._stream())
+                                        h * d if token_major else d, d if token_major else l * d, self._stream())
         if status:
             raise M.MosaicError("mosaic_kv_rows", status)
         return k, v
