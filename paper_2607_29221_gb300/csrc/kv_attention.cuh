@@ -71,6 +71,7 @@ struct AttendArgs {
     float *part_ml, *part_o;
     int64_t *split;             // of block c: the job cut by its end (or -1), the last block with a part of
                                 // it, and the units of the whole call
+    int by_job;                 // split is of job j instead: the block whose end cuts it (or -1), and so on
     float *stats;               // final maximum and 1 / sum of (sequence, head), for the weights
     float *scores;              // (sequence, head) x score_rows, for the weights (none where 16 slots in a
                                 // row do not count)

@@ -580,7 +580,7 @@ struct Pipe {
     uint64_t full[S::kStages], empty[S::kStages];
     uint16_t live[S::kStages][S::kTiles];   // slots of the stage's tiles that count
     int unit[S::kStages];           // the stage's unit in its job; + kLastUnit: the job's last one here
-    long long place[12];
+    long long place[S::kWarps + S::kProducers + 2];
     int aborted;
     float2 stats[S::kHeads * (S::kQReg ? S::kWarps : S::kQHeads)];   // whole jobs: for the weights
 };
@@ -600,6 +600,10 @@ struct Producer {
     using S = Shape<T, DP, NT>;
     // Rows of a group, look-ups of a lane.
     static constexpr int kSpan = TMA ? 256 : S::kUnit < 128 ? 128 : S::kUnit, kEach = TMA ? 1 : kSpan / 32;
+    static_assert((S::kProducers & (S::kProducers - 1)) == 0, "turns");
+    // A producer that waits for the stage of unit u - kStages has seen that of u - kProducers - kStages: a phase's
+    // parity is unambiguous only if that is no earlier than u - 2 kStages.
+    static_assert(S::kProducers <= S::kStages, "parities");
     static_assert(kSpan >= S::kUnit && kSpan % S::kUnit == 0 && kSpan <= 256, "a group holds whole units");
     static constexpr int kUnits = kSpan / S::kUnit, kHalves = S::kUnit / 16, kTurn = TMA ? 1 : S::kProducers;
     static constexpr int kBoth = S::kProducers == 1 ? 2 : 1;   // K and V by one warp
@@ -701,7 +705,7 @@ struct Producer {
             if (!jobs.next(kv, a, us, per_seq)) over = true, job_units = 0;
             // A job without a slot (whole jobs only) is one unit without a live one.
             else job_units = max(1, jobs.b1 - jobs.b0);
-            job_at = TMA ? 0 : (pw + units) & (S::kProducers - 1);
+            job_at = TMA ? 0 : (pw - units) & (S::kProducers - 1);   // unit `units + job_at` of all is pw's turn
         }
         if (!over) {
             far.i = jobs.i, far.h = jobs.r / a.hb * a.hpu, far.hb = jobs.r % a.hb, far.end = jobs.last(us);
@@ -954,9 +958,11 @@ __device__ __forceinline__ void cut_job(const AttendArgs &a, const Jobs &jobs, i
     int64_t c = last * n / total;
     while (total * (c + 1) / n <= last) ++c;
     while (total * c / n > last) --c;
-    a.split[3 * blockIdx.x] = i * per_seq + jobs.r;
-    a.split[3 * blockIdx.x + 1] = c;
-    a.split[3 * blockIdx.x + 2] = total;
+    const int64_t job = i * per_seq + jobs.r;
+    int64_t *split = a.split + 3 * (a.by_job ? job : blockIdx.x);
+    split[0] = a.by_job ? blockIdx.x : job;
+    split[1] = c;
+    split[2] = total;
 }
 
 template <class T, int DP, int NT, bool TMA>

@@ -35,8 +35,8 @@ struct Packed {};
 template <bool TMA, int DP, int NT>
 struct Shape<Packed<TMA>, DP, NT> {
     static constexpr int kES = 1, kRow = (5 * DP / 8 + 15) / 16 * 16, kChunks = kRow / 16;
-    static constexpr int kProducers = TMA ? 1 : 2, kWarps = 4, kUnit = 32 * kWarps, kStage = 2 * kUnit * kRow;
-    static constexpr int kStages = DP == 64 ? 3 : 2;
+    static constexpr int kProducers = TMA ? 1 : DP * NT <= 128 ? 4 : 2, kWarps = 4, kUnit = 32 * kWarps, kStage = 2 * kUnit * kRow;
+    static constexpr int kStages = !TMA && DP * NT <= 128 ? 4 : DP == 64 ? 3 : 2;
     static constexpr int kSlots = 2;
     static constexpr int kSteps = DP / 16, kHeads = 8 * NT, kPitch = DP + 4;
     static constexpr int kQWords = kSteps * NT * 4 * 32;
@@ -48,7 +48,7 @@ struct Shape<Packed<TMA>, DP, NT> {
     static constexpr int kPieces = 1, kPiece = kRow, kTiles = kUnit / 16;
     static constexpr bool kParted = true;
     static __device__ __forceinline__ uint32_t at(int r, int c) { return (uint32_t)(r * kRow + 16 * c); }
-    static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kMost = DP * NT <= (TMA ? 128 : 64) ? 3 : DP * NT <= 256 ? 2 : 1;
+    static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kMost = TMA && DP * NT <= 128 ? 3 : DP * NT <= 256 ? 2 : 1;
     static constexpr int kBlocks = kFit < kMost ? kFit : kMost;
     static_assert(kBytes <= 227 * 1024 && kBlocks >= 1, "shared memory");
 };
@@ -302,9 +302,12 @@ __global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Sha
         find_place<ALL>(kv, a, us, per_seq, blockIdx.x, gridDim.x, total, end, jobs, pipe.place);
         // Sequences without a slot belong to nobody's units: their rows are shared out.
         for (int64_t i = blockIdx.x; i < kv.c.seqs; i += gridDim.x)
-            if (kv.length(a.lens, i, a.max_len) == 0)
+            if (kv.length(a.lens, i, a.max_len) == 0) {
                 for (int x = tid; x < a.heads * D; x += ALL) a.out[i * a.ldo + x] = 0.0f;
-        if (tid == 0) a.split[3 * blockIdx.x] = -1;
+                if (a.by_job)
+                    for (int r = tid; r < per_seq; r += ALL) a.split[3 * (i * per_seq + r)] = -1;
+            }
+        if (!a.by_job && tid == 0) a.split[3 * blockIdx.x] = -1;
     }
     if (w >= W) {
         Producer<Packed<TMA>, DP, NT, TMA> producer(kv, a, &mk, &mv, pipe, per_seq, jobs, smem, w - W);
@@ -439,7 +442,10 @@ __global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Sha
             consumers_sync<THREADS>();
             whole_weights(kv, a, pipe.stats + hi * S::kHeads, scores, i, h, rows, s1, 32 * sub + lane, 32 * of_head);
         }
-        if (!whole && jobs.b0 == 0 && tid == 0) cut_job(a, jobs, i, end, total, per_seq);
+        if (tid == 0 && jobs.b0 == 0) {
+            if (!whole) cut_job(a, jobs, i, end, total, per_seq);
+            else if (a.by_job) a.split[3 * (i * per_seq + jobs.r)] = -1;
+        }
         consumers_sync<THREADS>();   // buffers and queries are free again
     }
 }
