@@ -65,7 +65,7 @@ struct AttendArgs {
     float scale2, decay;        // scale * log2(e): scores are kept in the base-2 domain
     float *out;
     int64_t ldo;
-    int out_quads;              // rows of out hold aligned words of four (4-bit caches)
+    int q_quads, out_quads;     // rows of q and out are aligned words of four (4-bit caches)
     // Partial sums of a block: slot 2c (its first job, begun elsewhere) and
     // 2c + 1 (its last, ended elsewhere): maxima and sums, and outputs.
     float *part_ml, *part_o;

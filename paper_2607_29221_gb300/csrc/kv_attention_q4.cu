@@ -15,7 +15,8 @@
 //    one or two 128-bit loads, with a single step and base; two rows of V become
 //    pairs of slots by one byte permutation a word.
 //  * 32 slots a warp at a time: the softmax, the rescaling of O and the queries'
-//    fragments (in shared memory) are shared by two tiles.
+//    fragments (in shared memory) are shared by two tiles.  (64 at a time: 48
+//    instructions fewer a tile, but twice the code: 208 -> 242 us.)
 //
 // Terms: queries are scaled to [2^14, 2^15) a head, probabilities by 2^15, and
 // each is split into two fp16 numbers, 22 bits or 2^-25 of the scale: smaller
@@ -35,8 +36,10 @@ struct Packed {};
 template <bool TMA, int DP, int NT>
 struct Shape<Packed<TMA>, DP, NT> {
     static constexpr int kES = 1, kRow = (5 * DP / 8 + 15) / 16 * 16, kChunks = kRow / 16;
-    static constexpr int kProducers = TMA ? 1 : DP * NT <= 128 ? 4 : 2, kWarps = 4, kUnit = 32 * kWarps, kStage = 2 * kUnit * kRow;
-    static constexpr int kStages = !TMA && DP * NT <= 128 ? 4 : DP == 64 ? 3 : 2;
+    static constexpr int kProducers = TMA ? 1 : DP * NT <= 128 ? 4 : 2;
+    static constexpr int kWarps = 4, kT = 2;   // kT: tiles of 16 slots that a warp takes at a time
+    static constexpr int kUnit = 16 * kT * kWarps, kStage = 2 * kUnit * kRow;
+    static constexpr int kStages = !TMA && DP * NT <= 128 ? 4 : DP * NT <= 128 ? 3 : 2;
     static constexpr int kSlots = 2;
     static constexpr int kSteps = DP / 16, kHeads = 8 * NT, kPitch = DP + 4;
     static constexpr int kQWords = kSteps * NT * 4 * 32;
@@ -48,7 +51,7 @@ struct Shape<Packed<TMA>, DP, NT> {
     static constexpr int kPieces = 1, kPiece = kRow, kTiles = kUnit / 16;
     static constexpr bool kParted = true;
     static __device__ __forceinline__ uint32_t at(int r, int c) { return (uint32_t)(r * kRow + 16 * c); }
-    static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kMost = TMA && DP * NT <= 128 ? 3 : DP * NT <= 256 ? 2 : 1;
+    static constexpr int kFit = 228 * 1024 / (kBytes + 1024), kMost = TMA && DP * NT <= 64 ? 3 : DP * NT <= 256 ? 2 : 1;
     static constexpr int kBlocks = kFit < kMost ? kFit : kMost;
     static_assert(kBytes <= 227 * 1024 && kBlocks >= 1, "shared memory");
 };
@@ -72,7 +75,7 @@ template <bool TMA, int DP, int NT>
 struct Warp4 {
     using S = Shape<Packed<TMA>, DP, NT>;
     // Words of codes of a lane: of a key row (channels DP / 4 t on), of a value row (DP / 8 g on); groups of the former.
-    static constexpr int kKW = DP / 32, kVW = DP / 64, kKG = DP == 256 ? 2 : 1, kN = DP / 8;
+    static constexpr int kT = S::kT, kKW = DP / 32, kVW = DP / 64, kKG = DP == 256 ? 2 : 1, kN = DP / 8;
     float m[NT], l[NT], unscale[NT], o[NT][kN][2];   // of head g; channels DP / 8 (2t + j) + i
 
     __device__ __forceinline__ void clear() {
@@ -83,50 +86,72 @@ struct Warp4 {
             for (int i = 0; i < kN; ++i) o[n][i][0] = o[n][i][1] = 0.0f;
         }
     }
-    // The job's queries as fragments in shared memory: step 2w + e of a lane has
-    // its channels 8w + 2e, + 4 and 8w + 2e + 1, + 4 (as q4_values gives them).
-    __device__ __forceinline__ void queries(const float *q, int D, int rows, float scale2, uint4 *qs) {
-        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    // The job's queries as fragments in shared memory (step 2w + e of a lane has its
+    // channels 8w + 2e, + 4 and 8w + 2e + 1, + 4, as q4_values gives them), and what
+    // undoes their scaling.  Warp `sub` of `warps` takes every so many-th row, a
+    // lane four neighbouring channels: rows come as whole lines (a lane that
+    // fetched its own fragment's channels waited 15000 cycles, with all SMs at the
+    // same lines).  Rows from `rows` to `last` become zeros, and those after them are.
+    static __device__ __forceinline__ void queries(const float *q, int D, int rows, int last, float scale2, bool quads,
+                                                   uint4 *qs, float2 *unscale, int sub, int warps) {
+        constexpr int kParts = (DP + 127) / 128, kAtOnce = 4;   // rows in flight
+        const int lane = threadIdx.x & 31;
+        __half *const to = reinterpret_cast<__half *>(qs);
+        for (int r0 = sub; r0 < last; r0 += kAtOnce * warps) {
+            float v[kAtOnce][kParts][4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const bool in = 8 * n + g < rows;
-            const float *x = q + (int64_t)(8 * n + g) * D + DP / 4 * t;
-            float v[DP / 4], top = 0.0f;
+            for (int x = 0; x < kAtOnce; ++x)
 #pragma unroll
-            for (int d = 0; d < DP / 4; ++d) v[d] = in && DP / 4 * t + d < D ? x[d] * scale2 : 0.0f;
-#pragma unroll
-            for (int d = 0; d < DP / 4; ++d) top = fmaxf(top, fabsf(v[d]));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            // Largest |q| to [2^14, 2^15); nothing to scale in zeros, NaN and infinities.
-            int e = (int)(__float_as_uint(top) >> 23) - 127;
-            e = e == 128 || top == 0.0f ? 14 : e < -100 ? -100 : e;
-            const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
-            unscale[n] = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
-#pragma unroll
-            for (int k = 0; k < S::kSteps; ++k) {
-                uint32_t f[2][2];   // pair, term
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int d = 8 * (k / 2) + 2 * (k % 2) + b;
-                    const float x0 = v[d] * up, x1 = v[d + 4] * up;
-                    f[b][0] = pack2(x0, x1, __half());
-                    const float2 r = unpack2(f[b][0], __half());
-                    f[b][1] = pack2(x0 - r.x, x1 - r.y, __half());
+                for (int y = 0; y < kParts; ++y) {
+                    const int r = r0 + x * warps, d = 128 * y + 4 * lane;
+                    const float *from = q + (int64_t)r * D + d;
+                    float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (r < rows && d < D) {   // multiples of four
+                        if (quads) z = *reinterpret_cast<const float4 *>(from);
+                        else z = make_float4(from[0], from[1], from[2], from[3]);
+                    }
+                    v[x][y][0] = z.x * scale2, v[x][y][1] = z.y * scale2, v[x][y][2] = z.z * scale2, v[x][y][3] = z.w * scale2;
                 }
-                qs[(k * NT + n) * 32 + lane] = make_uint4(f[0][0], f[0][1], f[1][0], f[1][1]);
+#pragma unroll
+            for (int x = 0; x < kAtOnce; ++x) {
+                const int r = r0 + x * warps, n = r >> 3, g = r & 7;
+                if (r >= last) break;
+                float top = 0.0f;
+#pragma unroll
+                for (int y = 0; y < kParts; ++y)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(v[x][y][i]));
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                // Largest |q| to [2^14, 2^15); nothing to scale in zeros, NaN and infinities.
+                int e = (int)(__float_as_uint(top) >> 23) - 127;
+                e = e == 128 || top == 0.0f ? 14 : e < -100 ? -100 : e;
+                const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
+                if (lane == 0) unscale[r].x = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+#pragma unroll
+                for (int y = 0; y < kParts; ++y) {
+                    const int d = 128 * y + 4 * lane, t = d / (DP / 4), in = d % (DP / 4), half = in >> 2 & 1;
+                    if (d >= DP) continue;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {   // channel in + i: step 2 (in / 8) + i / 2, pair i % 2
+                        const float z = v[x][y][i] * up;
+                        const __half hi = __float2half_rn(z), lo = __float2half_rn(z - __half2float(hi));
+                        __half *f = to + (((2 * (in >> 3) + (i >> 1)) * NT + n) * 32 + 4 * g + t) * 8 + (i & 1) * 4 + half;
+                        f[0] = hi, f[2] = lo;
+                    }
+                }
             }
         }
     }
 
-    // 32 slots: two tiles of 16, keys at k[], values at v[]; bit r of `live`: slot r
+    // kT tiles of 16 slots, keys at k[], values at v[]; bit r of `live`: slot r
     // counts (kMasked: not all of them).  `sc`: where the scores of the tiles' first slots and
     // the job's first head go (a row of `pitch` words a head), or null.
     template <bool kMasked>
-    __device__ __forceinline__ void tile(const uint32_t (&k)[2], const uint32_t (&v)[2], uint32_t live, uint32_t qs,
-                                         float *const (&sc)[2], int64_t pitch, int heads, int D) {
+    __device__ __forceinline__ void tile(const uint32_t (&k)[kT], const uint32_t (&v)[kT], uint32_t live, uint32_t qs,
+                                         float *const (&sc)[kT], int64_t pitch, int heads, int D) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-        float s[NT][4][2];
+        float s[NT][4][2];   // 2t and 2t + 1 of 8 slots
         {
             uint32_t code[4][kKW], scale[4][kKG];
             const int scales = D / 2, groups = D / kQ4Group, g0 = DP == 64 ? t >> 1 : kKG * t;
@@ -176,7 +201,7 @@ struct Warp4 {
                         }
             }
         }
-        uint32_t p[NT][2][4];
+        uint32_t p[NT][kT][4];
         float alpha[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -226,45 +251,56 @@ struct Warp4 {
             }
             l[n] = fmaf(l[n], alpha[n], sum);
         }
-        {
-            uint32_t code[2][4][kVW];   // slots 2t, 2t + 1, 2t + 8, 2t + 9 of a tile
-            __half2 step[2][2], base[2][2];
-            const int gv = DP == 64 ? g >> 2 : DP == 128 ? g >> 1 : g, groups = D / kQ4Group, scales = D / 2 + 4 * min(gv, groups - 1);
+        __half2 step[kT][2], base[kT][2];   // of slots 2t, 2t + 1 and 2t + 8, 2t + 9 of a tile
+        const int gv = DP == 64 ? g >> 2 : DP == 128 ? g >> 1 : g, groups = D / kQ4Group, scales = D / 2 + 4 * min(gv, groups - 1);
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+        for (int y = 0; y < kT; ++y)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    uint32_t sb[2];
+            for (int b = 0; b < 2; ++b) {
+                uint32_t sb[2];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int r = 8 * b + 2 * t + j;
-                        const uint32_t row = v[y] + r * S::kRow;
-                        lds_words<kVW>(code[y][2 * b + j], row + DP / 16 * g);
-                        lds_words<1>(&sb[j], row + scales);
-                        if (gv >= groups || (kMasked && !(live >> (16 * y + r) & 1u))) sb[j] = 0;
-                    }
-                    step[y][b] = as_half2(__byte_perm(sb[0], sb[1], 0x5410));
-                    base[y][b] = as_half2(__byte_perm(sb[0], sb[1], 0x7632));
+                for (int j = 0; j < 2; ++j) {
+                    const int r = 8 * b + 2 * t + j;
+                    lds_words<1>(&sb[j], v[y] + r * S::kRow + scales);
+                    if (gv >= groups || (kMasked && !(live >> (16 * y + r) & 1u))) sb[j] = 0;
                 }
+                step[y][b] = as_half2(__byte_perm(sb[0], sb[1], 0x5410));
+                base[y][b] = as_half2(__byte_perm(sb[0], sb[1], 0x7632));
+            }
+        {
+            uint32_t code[kT][4][kVW];
+#pragma unroll
+            for (int y = 0; y < kT; ++y)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    lds_words<kVW>(code[y][r], v[y] + (8 * (r >> 1) + 2 * t + (r & 1)) * S::kRow + DP / 16 * g);
 #pragma unroll
             for (int i0 = 0; i0 < kN; i0 += 4) {   // half a word: four channels
-                uint32_t f[2][2][4];
+                float c[4][NT][4];
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
+                for (int y = 0; y < kT; ++y) {
+                    uint32_t f[2][4];
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
                         q4_values(__byte_perm(code[y][2 * b][i0 / 8], code[y][2 * b + 1][i0 / 8], i0 % 8 ? 0x7632 : 0x5410),
-                                  step[y][b], base[y][b], f[y][b]);
+                                  step[y][b], base[y][b], f[b]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            if (y == 0) mma0(c[x][n], p[n][y], f[0][x], f[1][x], __half());
+                            else mma(c[x][n], p[n][y], f[0][x], f[1][x], __half());
+                        }
+                }
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        float c[4];
-                        mma0(c, p[n][0], f[0][0][x], f[0][1][x], __half());
-                        mma(c, p[n][1], f[1][0][x], f[1][1][x], __half());
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) o[n][i0 + x][j] = fmaf(o[n][i0 + x][j], alpha[n], c[j] + c[2 + j]);
-                    }
+                        for (int j = 0; j < 2; ++j) {
+                            float &to = o[n][i0 + x][j];
+                            to = fmaf(to, alpha[n], c[x][n][j] + c[x][n][2 + j]);
+                        }
             }
         }
     }
@@ -276,7 +312,7 @@ __global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Sha
     attend4_kernel(KvView kv, AttendArgs a, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv) {
     using S = Shape<Packed<TMA>, DP, NT>;
     using P = Pipe<Packed<TMA>, DP, NT>;
-    constexpr int W = S::kWarps, THREADS = 32 * W, ALL = THREADS + 32 * S::kProducers, MS = S::kSlots, kN = DP / 8;
+    constexpr int W = S::kWarps, THREADS = 32 * W, ALL = THREADS + 32 * S::kProducers, MS = S::kSlots, kN = DP / 8, kT = S::kT;
     extern __shared__ __align__(1024) char smem[];
     static_assert(sizeof(P) <= S::kMisc, "pipe");
     P &pipe = *reinterpret_cast<P *>(smem + S::kMiscAt);
@@ -321,10 +357,13 @@ __global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Sha
 
     Warp4<TMA, DP, NT> wp;
     int stage = 0, parity = 0;
-    // The warp's head of a unit's, and which pair of the head's tiles of 16 slots.
+    // The warp's head of a unit's, and which kT of the head's tiles of 16 slots.
     const int of_head = W / a.hpu, hi = w / of_head, sub = w - hi * of_head;
     uint4 *qs = reinterpret_cast<uint4 *>(smem + S::kQAt) + hi * (S::kQWords / 4);
-    const int tiles[2] = {2 * sub * a.hpu + hi, (2 * sub + 1) * a.hpu + hi};
+    const int tile0 = kT * sub * a.hpu + hi;   // tiles of a head are a.hpu apart
+    int held = 0;   // rows of the queries' fragments that are no zeros
+    for (int x = 32 * sub + lane; x < S::kQWords / 4; x += 32 * of_head) qs[x] = make_uint4(0, 0, 0, 0);
+    consumers_sync<THREADS>();
     while (jobs.next(kv, a, us, per_seq)) {
         const int s0 = jobs.first(us), s1 = jobs.last(us);
         const int h = jobs.r / a.hb * a.hpu + hi, hb = jobs.r % a.hb;
@@ -332,22 +371,31 @@ __global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Sha
         const int64_t i = jobs.i, qh = (int64_t)h * a.group + hb * S::kHeads;
         float *scores = a.scores ? a.scores + (i * a.heads + qh) * a.score_rows + s0 : nullptr;
         wp.clear();
-        wp.queries(a.q + i * a.ldq + qh * D, D, rows, a.scale2, qs);   // every warp of a head the same
+        float2 *stats = pipe.stats + hi * S::kHeads;   // in the end: maxima and sums
+        wp.queries(a.q + i * a.ldq + qh * D, D, rows, max(rows, held), a.scale2, a.q_quads, qs, stats, sub, of_head);
+        held = rows;
         consumers_sync<THREADS>();
+#pragma unroll
+        for (int n = 0; n < NT; ++n) wp.unscale[n] = 8 * n + g < rows ? stats[8 * n + g].x : 1.0f;
         for (int n = max(1, jobs.b1 - jobs.b0); n > 0; --n) {   // at most; the job's last unit ends it
             if (!mbar_wait(pipe.full + stage, parity, &pipe.aborted)) {
                 *(volatile int *)&pipe.aborted = 1;
                 if (lane == 0) atomicExch(&g_attend_error, 1u);
                 break;
             }
-            const uint32_t live = pipe.live[stage][tiles[0]] | (uint32_t)pipe.live[stage][tiles[1]] << 16;
-            const int unit = pipe.unit[stage], at = (unit & (kLastUnit - 1)) * us + 32 * sub;
+            uint32_t live = 0;
+#pragma unroll
+            for (int x = 0; x < kT; ++x) live |= (uint32_t)pipe.live[stage][tile0 + x * a.hpu] << (16 * x);
+            const int unit = pipe.unit[stage], at = (unit & (kLastUnit - 1)) * us + 16 * kT * sub;
             if (live) {
-                const uint32_t base = smem_u32(smem + stage * S::kStage);
-                const uint32_t k[2] = {base + tiles[0] * 16 * S::kRow, base + tiles[1] * 16 * S::kRow};
-                const uint32_t v[2] = {k[0] + S::kStage / 2, k[1] + S::kStage / 2};
-                float *const sc[2] = {scores && s0 + at < s1 ? scores + at : nullptr,   // rows of 16 slots exist in whole
-                                      scores && s0 + at + 16 < s1 ? scores + at + 16 : nullptr};
+                const uint32_t base = smem_u32(smem + stage * S::kStage) + tile0 * 16 * S::kRow;
+                uint32_t k[kT], v[kT];
+                float *sc[kT];   // rows of 16 slots exist in whole
+#pragma unroll
+                for (int x = 0; x < kT; ++x) {
+                    k[x] = base + x * a.hpu * 16 * S::kRow, v[x] = k[x] + S::kStage / 2;
+                    sc[x] = scores && s0 + at + 16 * x < s1 ? scores + at + 16 * x : nullptr;
+                }
                 if (live == 0xffffffffu) wp.template tile<false>(k, v, live, smem_u32(qs), sc, a.score_rows, rows, D);
                 else wp.template tile<true>(k, v, live, smem_u32(qs), sc, a.score_rows, rows, D);
             }
@@ -432,7 +480,7 @@ __global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Sha
                     a.part_ml[2 * (part + head)] = m, a.part_ml[2 * (part + head) + 1] = sum;
                 } else if (a.scores) {
                     const float ref = m == minus_inf() ? 0.0f : m;
-                    if (a.whole && a.hb == 1) pipe.stats[hi * S::kHeads + head] = make_float2(ref, inv);
+                    if (a.whole && a.hb == 1) stats[head] = make_float2(ref, inv);
                     else *reinterpret_cast<float2 *>(a.stats + 2 * (i * a.heads + qh + head)) = make_float2(ref, inv);
                 }
             }
@@ -440,7 +488,7 @@ __global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Sha
         if (a.scores && a.whole && a.hb == 1) {
             // The job's scores are this block's: its weights need no further launch.
             consumers_sync<THREADS>();
-            whole_weights(kv, a, pipe.stats + hi * S::kHeads, scores, i, h, rows, s1, 32 * sub + lane, 32 * of_head);
+            whole_weights(kv, a, stats, scores, i, h, rows, s1, 32 * sub + lane, 32 * of_head);
         }
         if (tid == 0 && jobs.b0 == 0) {
             if (!whole) cut_job(a, jobs, i, end, total, per_seq);
@@ -473,7 +521,7 @@ struct Instance4 {
     static mosaic_status launch(const mosaic_kv_cache &c, AttendArgs a, int &blocks, cudaStream_t st) {
         const KvView kv(c);
         alignas(64) CUtensorMap mk = {}, mv = {};
-        a.out_quads = aligned16(a.out) && a.ldo % 4 == 0;
+        a.out_quads = aligned16(a.out) && a.ldo % 4 == 0, a.q_quads = aligned16(a.q) && a.ldq % 4 == 0;
         // Positions are read 8 at a time.
         if (c.page_size % 8 == 0 && (!a.first || aligned16(c.position))) {
             auto maps = [&](int slots, int heads) {
