@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, kResident) append_norm_kernel(KvView
             const int h = base + k * lanes + lane, g = h - H < KV ? h - H : h - H - KV;
             const bool live = in && h < last, key = h < H + KV;
             Load4 &x = xs[k], &y = ys[k];
-            if (kNorm && base + k * lanes < H + KV) {
+            if (kNorm && __any_sync(0xffffffffu, key)) {   // not a warp of values alone
                 float r;
                 if constexpr (kPacked) r = exact_root(x, y, live, threads, nm);
                 else r = fast_root(x, y, live);

@@ -606,7 +606,6 @@ struct Producer {
     static_assert(S::kProducers <= S::kStages, "parities");
     static_assert(kSpan >= S::kUnit && kSpan % S::kUnit == 0 && kSpan <= 256, "a group holds whole units");
     static constexpr int kUnits = kSpan / S::kUnit, kHalves = S::kUnit / 16, kTurn = TMA ? 1 : S::kProducers;
-    static constexpr int kBoth = S::kProducers == 1 ? 2 : 1;   // K and V by one warp
     struct Group {
         int h, hb, s, end, units, low;   // first head, first slot, end of the job's slots, units, position bound
         int unit, of, base;              // number of its first unit in the job, of how many, units of all jobs before
@@ -614,7 +613,7 @@ struct Producer {
     };
     const KvView &kv;
     const AttendArgs &a;
-    const CUtensorMap *map[kBoth];
+    const CUtensorMap *map;
     Pipe<T, DP, NT> &pipe;
     char *smem;
     // us: slots of a unit; per_tile: 2^8 over the tiles of a head, rounded up (kParted: the heads' logarithm)
@@ -633,10 +632,9 @@ struct Producer {
     __device__ __forceinline__ Producer(const KvView &kv_, const AttendArgs &a_, const CUtensorMap *mk,
                                         const CUtensorMap *mv, Pipe<T, DP, NT> &pipe_, int per_seq_, const Jobs &j,
                                         char *smem_, int pw_)
-        : kv(kv_), a(a_), map{pw_ ? mv : mk}, pipe(pipe_), smem(smem_), per_seq(per_seq_), pw(pw_),
+        : kv(kv_), a(a_), map(pw_ ? mv : mk), pipe(pipe_), smem(smem_), per_seq(per_seq_), pw(pw_),
           lane(threadIdx.x & 31), us(S::kUnit / a_.hpu),
           per_tile(S::kParted ? (a_.hpu >= 2) + (a_.hpu >= 4) : 256 / (us / 16) + 1), jobs(j) {
-        if constexpr (kBoth == 2) map[1] = mv;
         ids = reinterpret_cast<int32_t *>(smem + S::kRing + S::kMerge + pw * kLookup<S::kUnit>);
         live = reinterpret_cast<uint8_t *>(ids + (S::kUnit < 128 ? 128 : S::kUnit));
         job_units = job_at = count = units = 0;
@@ -787,7 +785,7 @@ struct Producer {
             if (any) {
 #pragma unroll
                 for (int k = 0; k < S::kRow / 128; ++k)
-                    tma_load_4d(to + k * 128 * S::kUnit, map[0], bar, k * 128 / S::kES, (int)offset(s), now.h, page);
+                    tma_load_4d(to + k * 128 * S::kUnit, map, bar, k * 128 / S::kES, (int)offset(s), now.h, page);
             }
         }
         __syncwarp();
@@ -806,16 +804,11 @@ struct Producer {
                 all += any >> (b * hpu) & each ? bytes : 0u;
                 page[b] = ids[(u * S::kUnit + 16 * b * hpu) / 8];
             }
-            mbar_expect_tx(bar, kBoth * all);
+            mbar_expect_tx(bar, all);
             char *to = smem + stage * S::kStage + pw * (S::kStage / 2);
 #pragma unroll
             for (int b = 0; b < N; ++b)
-                if (any >> (b * hpu) & each) {
-                    const int off = (int)offset(s + 16 * b);
-#pragma unroll
-                    for (int x = 0; x < kBoth; ++x)
-                        tma_load_4d(to + x * (S::kStage / 2) + b * bytes, map[x], bar, 0, off, now.h, page[b]);
-                }
+                if (any >> (b * hpu) & each) tma_load_4d(to + b * bytes, map, bar, 0, (int)offset(s + 16 * b), now.h, page[b]);
         }
         __syncwarp();
     }
@@ -834,7 +827,7 @@ struct Producer {
             const uint32_t mask = __ballot_sync(0xffffffffu, has);
             if (lane == 0) {
                 uint64_t *bar = pipe.full + stage;
-                mbar_expect_tx(bar, (uint32_t)(kBoth * __popc(mask) * BOX) * S::kRow);
+                mbar_expect_tx(bar, (uint32_t)(__popc(mask) * BOX) * S::kRow);
                 int page[N];
 #pragma unroll
                 for (int b = 0; b < N; ++b) page[b] = ids[(u * S::kUnit + b * BOX) / 8];
@@ -848,10 +841,8 @@ struct Producer {
                         const int c1 = a.token_major ? h : off, c2 = a.token_major ? off : h;
 #pragma unroll
                         for (int k = 0; k < S::kPieces; ++k)
-#pragma unroll
-                            for (int x = 0; x < kBoth; ++x)
-                                tma_load_4d(to + x * (S::kStage / 2) + b * BOX * S::kPiece + k * 128 * S::kUnit, map[x], bar,
-                                            k * 128 / S::kES, c1, c2, page[b]);
+                            tma_load_4d(to + b * BOX * S::kPiece + k * 128 * S::kUnit, map, bar, k * 128 / S::kES, c1, c2,
+                                        page[b]);
                     }
                     if constexpr (S::kParted) continue;
                     off += BOX, row += BOX;

@@ -29,14 +29,15 @@
 namespace mosaic {
 namespace {
 
-// TMA: copies by tensor boxes, one producer warp; else by lanes, two.
+// TMA: copies by tensor boxes, else by lanes, which takes more warps (400 x 1500
+// slots in pages of 20: 88 us with two, 78 with four).
 template <bool TMA>
 struct Packed {};
 
 template <bool TMA, int DP, int NT>
 struct Shape<Packed<TMA>, DP, NT> {
     static constexpr int kES = 1, kRow = (5 * DP / 8 + 15) / 16 * 16, kChunks = kRow / 16;
-    static constexpr int kProducers = TMA ? 1 : DP * NT <= 128 ? 4 : 2;
+    static constexpr int kProducers = TMA || DP * NT > 128 ? 2 : 4;
     static constexpr int kWarps = 4, kT = 2;   // kT: tiles of 16 slots that a warp takes at a time
     static constexpr int kUnit = 16 * kT * kWarps, kStage = 2 * kUnit * kRow;
     static constexpr int kStages = !TMA && DP * NT <= 128 ? 4 : DP * NT <= 128 ? 3 : 2;
