@@ -4,10 +4,10 @@
 //   y = rotate((x r) gain),  r = 1 / sqrt(mean x^2 + eps) over a head
 //
 // Bound by HBM as kv_append.cu is (fp32 rows in, fp32 queries and the cache's
-// rows out); the same split: a block the heads of one token, a thread 4 + 4
-// channels of a head, half a head apart, four heads in flight.  The threads of
-// a head lie in one warp (their number rounded up to a power of two), which
-// sums the squares.
+// rows out: 5003 tokens into an fp32 cache 79 us, 91% of the copy rate); the same
+// split: a block the heads of one token, a thread 4 + 4 channels of a head, half a
+// head apart, two heads in flight.  The threads of a head lie in one warp (their
+// number rounded up to a power of two), which sums the squares.
 //
 // 4-bit rows: 32 neighbouring channels share a step and a base, and the halves
 // of a head that a thread rotates do not lie in one group, so rotated keys and
@@ -18,7 +18,10 @@
 // two-float arithmetic (Dekker, "A floating-point technique for extending the
 // available precision", 1971; Taylor's series and one Newton step) rounded once,
 // and the rest is IEEE operations without contraction.  Doubles would do the
-// same at a sixty-fourth of the rate.
+// same at a sixty-fourth of the rate.  Keys and values go first and are packed by
+// all warps while the queries come (a thread a group of 32: 42 us on 2048 tokens
+// of 64 + 16 heads, two of eight warps at work; now 35 with 68% of the issue
+// slots taken).
 #include "kv_append.cuh"
 
 namespace mosaic {

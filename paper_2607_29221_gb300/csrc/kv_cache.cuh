@@ -85,10 +85,7 @@ inline mosaic_status kv_check(const mosaic_kv_cache *c) {
     return MOSAIC_OK;
 }
 
-// Rows of 4-bit codes: channel c of a row is code (word c / 8) >> 4 (c % 8) & 15
-// and stands for base + code step, one fused fp16 operation, where step and
-// base are the halves of word c / 32 of the row's last part.
-// (x & mask) | bits as one instruction: with both constants the compiler makes two of it.
+// (x & mask) | bits as one instruction (the compiler makes two of it where both are constants).
 __device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) {
     uint32_t y;
     asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(x), "r"(mask), "r"(bits));
@@ -96,6 +93,10 @@ __device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t b
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
 __device__ __forceinline__ uint32_t as_word(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
+// Rows of 4-bit codes: channel c of a row is code (word c / 8) >> 4 (c % 8) & 15
+// and stands for base + code step, one fused fp16 operation, where step and
+// base are the halves of word c / 32 of the row's last part.
+//
 // Codes k and k + 4 (counted from the lowest) of a word as values, k = 0 .. 3,
 // packed with the lower one first.  A code or'ed into the mantissa of 1024 is
 // 1024 + code, or 1024 + 16 code: both come off exactly.

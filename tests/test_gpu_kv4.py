@@ -7,9 +7,10 @@ Tolerances, set from the number formats before any run:
   attention  as for the other caches (a product carried to 22 bits and summed in
              fp32 over at most 256 channels moves a score by at most E = 2^-20
              scale sum |q_d k_d|, a probability by 2 E relative, and exp, the sums
-             and the join add at most 2^-19); besides, query channels are off by up
-             to 2^-40 of the head's largest and weights by up to 2^-40 of the row's
-             largest: E + 2^-40 scale max|q| sum |k_d|, and
+             and the join add at most 2^-19); besides, the lower fp16 terms are off by
+             up to 2^-25, of queries scaled to 2^14 or more a head (2^-39 of the
+             largest) and of weights scaled to 2^15 (2^-40 of the row's largest):
+             E + 2^-39 scale max|q| sum |k_d|, and
              |d out| <= (2 E + 2^-19) sum p |v| + 2^-40 max p sum |v|.
   append     the bytes of a row are defined by IEEE operations on sines, cosines
              and 1 / rms rounded once: equal.  Queries: phase 2^-25 turns, three
@@ -156,7 +157,7 @@ def reference(c, q, scale, first=None, decay=1.0):
         qi = q[i].double().reshape(c.kv_heads, -1, d)
         s = torch.einsum("hgd,hnd->hgn", qi, k) * scale
         err = abs(scale) * (2.0 ** -20 * torch.einsum("hgd,hnd->hgn", qi.abs(), k.abs())
-                            + 2.0 ** -40 * qi.abs().amax(2, keepdim=True) * k.abs().sum(2)[:, None])
+                            + 2.0 ** -39 * qi.abs().amax(2, keepdim=True) * k.abs().sum(2)[:, None])
         if first is not None:
             s = s.masked_fill(slots(c, c.position, i, n)[:, None] < int(first[i]), -math.inf)
         gone = s == -math.inf
