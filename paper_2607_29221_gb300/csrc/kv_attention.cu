@@ -23,6 +23,11 @@ constexpr int kMaxGroup = 64;
 // / 60, 1024: 25 / 22, 28 / 31, 56 / 79; fp32 heads of 128, 512: 16 / 13, 18 / 26, 46 /
 // 60, 1024: 27 / 14, 29 / 36, 83 / 96: it shares some that are faster whole.
 constexpr int64_t kWholeFew = 512, kWholeMany = 1024, kManyJobs = 128, kWholeBytes = 128 * 1024;
+// With a lower bound, 4-bit caches up to here: the split counts units that the
+// bound leaves out, and the blocks whose units are all live end last.  400
+// sequences of up to 1500, heads of 64, bound 512: 80 us shared, 71 whole; 64 of up
+// to 2000 with 64 query heads of 128, bound 300: 52, 42; 400 of up to 1500 that the bound leaves as they are 94, 108.
+constexpr int64_t kWholeBound = 2048;
 // Heads share a unit (the blocks' warps then have a head each and nothing to
 // merge) while so many jobs remain to be shared out; whole jobs while there is
 // more than a wave of them.  Shared jobs with 1 / 2 / 4 heads a unit, up to 1024
@@ -234,12 +239,13 @@ AttendShape shape_of(const mosaic_kv_cache &c, int64_t heads) {
     return by_type(c.type, [&](auto t) { return attend_shape<decltype(t)>(c.head_dim, group); });
 }
 // How many blocks may share the units that the lengths may add up to.
-int64_t most_blocks(const mosaic_kv_cache &c, const AttendShape &s, int64_t heads, int64_t max_len) {
+int64_t most_blocks(const mosaic_kv_cache &c, const AttendShape &s, int64_t heads, int64_t max_len, bool bound = false) {
     const int64_t group = heads / c.kv_heads, hb = (group + s.heads - 1) / s.heads;
     const int64_t units = c.seqs * c.kv_heads * hb * ((max_len + s.unit - 1) / s.unit);
     const bool many = c.seqs * c.kv_heads * hb >= kManyJobs;
     const int64_t row = kv_row_bytes(c.type, c.head_dim);
-    const bool whole = max_len <= (many ? kWholeMany : kWholeFew) && max_len * row <= (many ? 2 : 1) * kWholeBytes;
+    const int64_t most = !many ? kWholeFew : bound && c.type == MOSAIC_KV_Q4 ? kWholeBound : kWholeMany;
+    const bool whole = max_len <= most && max_len * row <= (many ? 2 : 1) * kWholeBytes;
     return whole ? 0 : units < kAttendWave ? units : kAttendWave;
 }
 mosaic_status check(const mosaic_kv_cache *c, int64_t heads, int64_t max_len) {
@@ -286,7 +292,7 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     if (cache->seqs == 0) return MOSAIC_OK;
     if (!q || !out || !lens || (first && !cache->position)) return MOSAIC_ERR_ARG;
     const AttendShape s = shape_of(*cache, heads);
-    const int64_t cap = most_blocks(*cache, s, heads, max_len);
+    const int64_t cap = most_blocks(*cache, s, heads, max_len, first != nullptr);   // with a bound as many or fewer
     const Parts p = parts(*cache, s, heads, cap, rows_of(max_len));
     if (ws_bytes < p.total()) return MOSAIC_ERR_WORKSPACE;
     if (!ws && p.total()) return MOSAIC_ERR_ARG;

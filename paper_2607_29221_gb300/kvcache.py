@@ -113,14 +113,14 @@ class HeadNorm:
                                 and (head_dim == 1 or g.stride(0) == 1)),
                   f"{name}: a contiguous float32 tensor of head_dim values")
         self.head_dim, self.q_gain, self.k_gain = head_dim, q_gain, k_gain
+        self._devices = {g.get_device() for g in (q_gain, k_gain) if g is not None}
         self._c = M.mosaic_head_norm(eps, *(None if g is None else g.data_ptr() for g in (q_gain, k_gain)))
         self._ref = ctypes.byref(self._c)
 
     def on(self, head_dim: int, index: int):
         """The library's argument for a cache of head_dim channels on device ``index``."""
         _need(head_dim == self.head_dim, "norm: of another head_dim than the cache")
-        _need(all(g is None or g.get_device() == index for g in (self.q_gain, self.k_gain)),
-              "norm: gains on another device than the cache")
+        _need(self._devices <= {index}, "norm: gains on another device than the cache")
         return self._ref
 
 

@@ -237,6 +237,9 @@ def test_attention(case, window):
     (5, 1300, 20, 2, 256, 8, "head", False),
     (80, 1100, 16, 8, 256, 16, "head", True),
     (70, 1200, 32, 2, 128, 16, "head", True),
+    (20, 2100, 64, 8, 128, 16, "head", True),       # shared jobs with a lower bound
+    (40, 2100, 24, 8, 64, 20, "token", True),
+    (300, 1, 128, 8, 256, 16, "token", False),
 ])
 def test_attention_of_many_sequences(seqs, most, heads, kv, dim, page, layout, window):
     """The ways in which jobs are shared out: heads a unit, whole jobs, boxes."""
