@@ -198,11 +198,11 @@ class PagedCache:
     def read(self, seq: int, n: int):
         """Keys and values of the first n slots of a sequence, kv_heads x n x head_dim in the cache's type (a copy;
         float16 for 4 bits)."""
-        if self.k.dtype is INT4:
-            slot = torch.arange(n, dtype=torch.int32, device=self.device)
-            k, v = self.rows(torch.full_like(slot, seq), slot, token_major=False)
-            return k, v
         page = self.k.shape[2]
+        if self.k.dtype is INT4:
+            seqs, columns = self.table.shape
+            slot = torch.arange(min(n, columns * page), dtype=torch.int32, device=self.device)
+            return self.rows(torch.full_like(slot, range(seqs)[seq]), slot, token_major=False)   # refused as an index is
         ids = self.table[seq, : -(-n // page)].long()
         return tuple(x[ids].transpose(0, 1).reshape(self.kv_heads, -1, self.head_dim)[:, :n] for x in (self.k, self.v))
 

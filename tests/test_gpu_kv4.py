@@ -703,6 +703,22 @@ def test_append_and_rows_on_another_stream_in_a_graph():
     assert all(torch.equal(a, b) for a, b in zip(e.rows(seq, slot), want))
 
 
+def test_read_takes_the_table_as_other_types_do():
+    """Sequences are counted from the end where negative, none past the table is read, and slots end with the table."""
+    from paper_2607_29221_gb300 import kvcache as KV
+    c = make([12, 7], 2, 64, 4, seed=3)
+    shape = (c.k.shape[0], 2, 4, 64)
+    f = KV.PagedCache(torch.zeros(shape, device="cuda"), torch.zeros(shape, device="cuda"), torch.zeros_like(c.table))
+    most = c.table.shape[1] * 4
+    for n in (1, 5, most, most + 9):
+        assert [x.shape for x in c.read(1, n)] == [x.shape for x in f.read(1, n)]
+    assert all(torch.equal(a, b) for a, b in zip(c.read(-2, 12), c.read(0, 12)))
+    for seq in (2, -3):
+        for cache in (c, f):
+            with pytest.raises(IndexError):
+                cache.read(seq, 4)
+
+
 def test_a_session_on_a_4_bit_cache():
     """Prefill, steps and a budget through a masked layer: every step's attention is that over the cache's own values."""
     from paper_2607_29221_gb300 import decoder as DEC, kvcache as KV, mosaic as M, protocol as PR, workloads as wl
