@@ -46,6 +46,8 @@ class DecodeSession:
         self.cache = KV.PagedCache.empty(seqs * columns + 1, s.n_kv, page_size, s.head_dim, self.pages.table, dtype,
                                          weights=keep is not None)
         self.rope = KV.Rope(s.head_dim, 500000.0, device=dev) if rope is None else rope
+        if norm is not None:
+            norm.on(s.head_dim, self.cache.k.get_device())      # refused before a prompt takes pages
         self.norm = norm
         self.host_lens = [0] * seqs
         self.lens = torch.zeros(seqs, dtype=torch.int32, device=dev)     # cached slots

@@ -719,6 +719,16 @@ def test_read_takes_the_table_as_other_types_do():
                 cache.read(seq, 4)
 
 
+def test_a_session_refuses_norms_of_another_head():
+    from paper_2607_29221_gb300 import decoder as DEC, kvcache as KV, mosaic as M, protocol as PR, workloads as wl
+    from paper_2607_29221_gb300.session import DecodeSession
+    s = DEC.LayerShape(hidden=256, n_heads=8, n_kv=2, head_dim=64, ffn=512)
+    layer = DEC.SecureDecoderLayer(PR.Protocol(wl.mask_key(), M.default_params()), DEC.LayerWeights(s))
+    for norm in (KV.HeadNorm(32), KV.HeadNorm(64, 1e-6, torch.ones(64))):      # its size, host gains
+        with pytest.raises(ValueError, match="norm"):
+            DecodeSession(layer, seqs=1, max_len=16, dtype=KV.INT4, norm=norm)
+
+
 def test_a_session_on_a_4_bit_cache():
     """Prefill, steps and a budget through a masked layer: every step's attention is that over the cache's own values."""
     from paper_2607_29221_gb300 import decoder as DEC, kvcache as KV, mosaic as M, protocol as PR, workloads as wl
