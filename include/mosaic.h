@@ -720,7 +720,8 @@ mosaic_status mosaic_kv_rows(const mosaic_kv_cache *cache, const int32_t *seq, c
  * head's largest and weights p down to 2^-87 of the row's largest; smaller ones
  * are off by up to 2^-51 and 2^-110 of those; 4-bit caches: down to 2^-17 of the
  * head's largest channel and 2^-18 of the row's largest weight, smaller ones are off by up
- * to 2^-39 and 2^-40 of those).  heads: a multiple of kv_heads, at most 64 query
+ * to 2^-39 and 2^-40 of those, or 2^-32 where scores are so large (from 2^27 / log2(e)) that fp32
+ * has them in steps of 16).  heads: a multiple of kv_heads, at most 64 query
  * heads a key/value head.  max_len (max_len heads < 2^34): an upper bound of
  * the lengths, which sizes the workspace (mosaic_kv_attention_workspace bytes for the same
  * cache, heads and max_len; 0 if none is needed or they are not valid).  out: seqs x heads

@@ -24,7 +24,10 @@
 // Terms: queries are scaled to [2^14, 2^15) a head, probabilities by 2^15, and
 // each is split into two fp16 numbers, 22 bits or 2^-25 of the scale: smaller
 // query channels are off by up to 2^-39 of the head's largest, smaller weights
-// by up to 2^-40 of the row's largest.  Products are exact in fp32; chains of
+// by up to 2^-40 of the row's largest.  The 2^15 lies in the maximum that
+// scores are taken off, lowered by 15 and rounded up, and so the same number
+// for sums, outputs and joins at any score: probabilities reach 2^15 and never
+// more (from scores of 2^24 on, whose steps are 2 and more, some bits less).  Products are exact in fp32; chains of
 // four or two steps are added to the rest in fp32 with rounding to nearest, since
 // the tensor cores truncate.
 //
@@ -83,7 +86,9 @@ struct Warp4 {
     using S = Shape<Packed<TMA>, DP, NT>;
     // Words of codes of a lane: of a key row (channels DP / 4 t on), of a value row (DP / 8 g on); groups of the former.
     static constexpr int kT = S::kT, kKW = DP / 32, kVW = DP / 64, kKG = DP == 256 ? 2 : 1, kN = DP / 8;
-    float m[NT], l[NT], unscale[NT], o[NT][kN][2];   // of head g; channels DP / 8 (2t + j) + i
+    // Of head g; channels DP / 8 (2t + j) + i.  m: the largest score so far less 15, rounded up; l, o and what is made of
+    // them (partial sums, statistics) are relative to it.
+    float m[NT], l[NT], unscale[NT], o[NT][kN][2];
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -242,14 +247,13 @@ struct Warp4 {
             for (int x = 1; x < 4; ++x) top = fmaxf(top, fmaxf(s[n][x][0], s[n][x][1]));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            top = fmaxf(m[n], top * unscale[n]);
+            top = fmaxf(m[n], __fadd_ru(top * unscale[n], -15.0f));
             alpha[n] = power2(m[n] - top);
             m[n] = top;
-            const float from = 15.0f - top;
             float sum = 0.0f;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const float p0 = power2(fmaf(s[n][x][0], unscale[n], from)), p1 = power2(fmaf(s[n][x][1], unscale[n], from));
+                const float p0 = power2(fmaf(s[n][x][0], unscale[n], -top)), p1 = power2(fmaf(s[n][x][1], unscale[n], -top));
                 sum += p0 + p1;
                 const uint32_t hi = pack2(p0, p1, __half());
                 const float2 r = unpack2(hi, __half());
@@ -418,9 +422,6 @@ __global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Sha
         for (int n = 0; n < NT; ++n) {
             wp.l[n] += __shfl_xor_sync(0xffffffffu, wp.l[n], 1);
             wp.l[n] += __shfl_xor_sync(0xffffffffu, wp.l[n], 2);
-            wp.l[n] *= 0x1p-15f;
-#pragma unroll
-            for (int x = 0; x < kN; ++x) wp.o[n][x][0] *= 0x1p-15f, wp.o[n][x][1] *= 0x1p-15f;
         }
         auto put = [&](int slot) {
 #pragma unroll

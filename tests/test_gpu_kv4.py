@@ -754,3 +754,73 @@ def test_a_session_on_a_4_bit_cache():
         y = ses.step(torch.randn(2, 256, generator=g, device="cuda"))
         assert torch.isfinite(y).all()
     assert max(ses.host_lens) <= 24 and ses.lens.tolist() == ses.host_lens
+
+
+# ---------------------------------------------------------------------------
+# Scores in units of log2: the scale whose product with log2(e) is one in fp32.
+def unit_scale():
+    f = np.float32
+    near = [f(math.log(2))]
+    for _ in range(4):
+        near += [np.nextafter(near[-1], f(1))]
+    near += [np.nextafter(f(math.log(2)), f(0))]
+    return float(next(x for x in near if f(x * f(1.44269504088896341)) == 1))
+
+
+def level(pool, group, dim, base):
+    """Channels of a group of 32 of all rows: `base`, whatever the codes."""
+    at = dim // 2 + 4 * group
+    pool[..., at: at + 4] = torch.stack([torch.zeros_like(base), base], -1).half().contiguous().view(torch.uint8)
+
+
+@pytest.mark.parametrize("lens,heads,kv,dim,page,window", [
+    ([5, 40, 300], 16, 2, 64, 16, False), ([5, 40, 300], 24, 2, 64, 20, True), ([5, 40, 300, 5000], 16, 2, 128, 16, True),
+    ([33, 3000], 16, 1, 128, 20, False), ([40, 700], 32, 2, 256, 8, True)])
+def test_attention_of_large_equal_scores(lens, heads, kv, dim, page, window):
+    """Scores of 2^23 to 2^119 of both signs, the same in every slot: means of the values, whatever the score.
+    Probabilities are the same power of two; what remains is the sums' and the join's 2^-19."""
+    c = make(lens, kv, dim, page, seed=7)
+    for group in range(dim // 32):
+        level(c.k, group, dim, torch.full(c.k.shape[:3], 1.0, device="cuda"))
+    tops = [2.0 ** 23 + 1, 16777240.0, 3e7, 1e8, 2.0 ** 28 + 32, 1e10, 1e20, 5e35]
+    q = torch.zeros(len(lens), heads, dim, device="cuda")
+    q[..., 1] = torch.tensor([t * s for s in (1, -1) for t in tops] * 2, device="cuda")[:heads]
+    first = None
+    if window:
+        c.position.copy_(torch.randint(0, 1000, c.position.shape, generator=gen(8), device="cuda"))
+        first = torch.full((len(lens),), 300, dtype=torch.int32, device="cuda")
+    want, _, weights = reference(c, torch.zeros_like(q), 1.0, first, 0.5)      # equal scores: those of no query
+    size = torch.zeros_like(want)
+    for i, n in enumerate(lens):
+        on = slots(c, c.position, i, n) >= (-1 if first is None else 300)
+        v = values(slots(c, c.v, i, n), dim).abs() * on[..., None]
+        size[i] = (v.sum(1) / on.sum(1, keepdim=True).clamp(min=1)).repeat_interleave(heads // kv, 0)
+    out = c.attend(q, ints(lens), max(lens), first=first, scale=unit_scale(), decay=0.5)
+    off = (out.double() - want).abs()
+    assert (off <= 2.0 ** -19 * size).all(), [h for h in range(heads) if not (off[:, h] <= 2.0 ** -19 * size[:, h]).all()]
+    for i, n in enumerate(lens):
+        w = weights[i][0]
+        assert ((slots(c, c.weight, i, n).double() - w).abs() <= 2.0 ** -18 * w + 1e-30).all(), i
+
+
+@pytest.mark.parametrize("top", [2.0 ** 24, -2.0 ** 24, 2.0 ** 25, -2.0 ** 25 - 8, 2.0 ** 26 - 512, -2.0 ** 26 + 512])
+@pytest.mark.parametrize("lens", [[9, 50, 400], [31, 2000, 5000]])
+def test_attention_of_large_scores_that_differ(lens, top):
+    """Scores top - 8 j, j < 4: multiples of 8 below 2^26 + 2^25, exact in fp32 and in two fp16 terms of the
+    queries (2^25 and 1, scaled to 2^14 and 2^-11); probabilities 2^-8j are exact too."""
+    dim, kv, heads = 64, 2, 16
+    c = make(lens, kv, dim, 16, seed=3)
+    j = torch.randint(0, 4, c.k.shape[:3], generator=gen(4), device="cuda").float()
+    level(c.k, 0, dim, torch.ones_like(j))
+    level(c.k, 1, dim, -8.0 * j)
+    q = torch.zeros(len(lens), heads, dim, device="cuda")
+    q[..., 1], q[..., 40] = top, 1.0
+    out = c.attend(q, ints(lens), max(lens), scale=unit_scale())
+    for i, n in enumerate(lens):
+        p = 2.0 ** (-8.0 * slots(c, j, i, n).double())
+        p = p / p.sum(1, keepdim=True)
+        v = values(slots(c, c.v, i, n), dim)
+        got = out[i].reshape(kv, heads // kv, dim).double()
+        want, size = (torch.einsum("hn,hnd->hd", p, x)[:, None] for x in (v, v.abs()))
+        tol = 2.0 ** -19 * size + (2.0 ** -40 * p.amax(1)[:, None] * v.abs().sum(1))[:, None]
+        assert ((got - want).abs() <= tol).all(), (i, float(((got - want).abs() / tol).max()))
