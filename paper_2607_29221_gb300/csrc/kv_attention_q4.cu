@@ -217,16 +217,16 @@ struct Warp4 {
         float alpha[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float most = 0.0f;   // an infinite score counts as NaN
+            float most = 0.0f;   // an infinite score counts as NaN, also if only its scale makes it one
 #pragma unroll
             for (int x = 0; x < 4; ++x)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) most = fmaxf(most, fabsf(s[n][x][j]));
-            if (__any_sync(0xffffffffu, most == __int_as_float(0x7f800000))) {
+            if (__any_sync(0xffffffffu, most * unscale[n] == __int_as_float(0x7f800000))) {
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) s[n][x][j] = finite_or_nan(s[n][x][j]);
+                    for (int j = 0; j < 2; ++j) s[n][x][j] = fabsf(s[n][x][j] * unscale[n]) < __int_as_float(0x7f800000) ? s[n][x][j] : __int_as_float(0x7fffffff);
             }
             if constexpr (kMasked) {
 #pragma unroll

@@ -824,3 +824,48 @@ def test_attention_of_large_scores_that_differ(lens, top):
         want, size = (torch.einsum("hn,hnd->hd", p, x)[:, None] for x in (v, v.abs()))
         tol = 2.0 ** -19 * size + (2.0 ** -40 * p.amax(1)[:, None] * v.abs().sum(1))[:, None]
         assert ((got - want).abs() <= tol).all(), (i, float(((got - want).abs() / tol).max()))
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("lens,heads,kv,page", [([5, 32, 40, 300, 77], 16, 2, 16), ([5, 40, 300, 5000, 9], 48, 2, 20),
+                                                ([1, 2, 3, 31, 33], 2, 2, 8)])
+def test_attention_of_scores_beyond_fp32(lens, heads, kv, page, sign):
+    """A finite query and a finite key whose product is beyond fp32, of either sign: the score counts as NaN, and so
+    do the row's output and the weights of its key/value head; not where the slot does not count."""
+    dim = 64
+    c = make(lens, kv, dim, page, seed=13)
+    at = lambda i, s: (int(c.table[i, s // page]), slice(None), s % page)
+    level(c.k, 0, dim, torch.zeros(c.k.shape[:3], device="cuda"))
+    q = torch.randn(len(lens), heads, dim, generator=gen(14), device="cuda")
+    per = heads // kv
+    q[..., :32] = 0.0
+    q[:, per - 1] = 0.0
+    q[:, per - 1, 4] = sign * 1e37                              # the first key/value head's last query
+    last = len(lens) - 1
+    first = torch.zeros(len(lens), dtype=torch.int32, device="cuda")
+    first[last] = 1
+    c.position.fill_(1)
+    for i, n in enumerate(lens):
+        row = c.k[at(i, n // 2)]
+        row[..., dim // 2: dim // 2 + 4] = torch.tensor([0.0, 65000.0], dtype=torch.float16, device="cuda").view(torch.uint8)
+        c.k[at(i, n // 2)] = row
+    c.position[at(last, lens[last] // 2)] = 0                   # of the last sequence that slot is below the bound
+    calm = q.clone()
+    calm[:, per - 1, 4] = 0.0
+    want, tol, weights = reference(c, calm, 0.125, first)
+    out = c.attend(q, ints(lens), max(lens), first=first)
+    other = [h for h in range(heads) if h != per - 1]
+    assert torch.isnan(out[:last, per - 1]).all()
+    assert ((out[:, other].double() - want[:, other]).abs() <= tol[:, other]).all()
+    assert ((out[last].double() - want[last]).abs() <= tol[last]).all()
+    for i, n in enumerate(lens):
+        w, wt = weights[i]
+        got = slots(c, c.weight, i, n).double()
+        assert ((got[1] - w[1]).abs() <= wt[1]).all()
+        if i < last:
+            assert torch.isnan(got[0]).all(), i
+        else:
+            assert ((got[0] - w[0]).abs() <= wt[0]).all()
+    bare = type(c)(c.k, c.v, c.table, position=c.position)     # and without weights
+    again = bare.attend(q, ints(lens), max(lens), first=first)
+    assert torch.equal(torch.nan_to_num(again, nan=7.5), torch.nan_to_num(out, nan=7.5))
