@@ -680,18 +680,19 @@ mosaic_status mosaic_kv_append(const mosaic_kv_cache *cache, const float *qkv, i
 
 /* Norms of query and key heads: y = (x r) gain with r = 1 / sqrt(mean x^2 + eps)
  * over the head's channels, before the rotation.  q_gain and k_gain: head_dim
- * fp32 device values, the same for every head; NULL: ones.  eps >= 0.  The sum of
- * squares has to stay finite in fp32. */
+ * fp32 device values, the same for every head; NULL: ones.  eps >= 0.  Channels may
+ * have any finite size, and so may r: squares beyond fp32 do not matter (x r is off by up to
+ * 2^-145 besides its rounding). */
 typedef struct {
     float eps;
     const float *q_gain, *k_gain;
 } mosaic_head_norm;
 
 /* mosaic_kv_append with norms of the queries and keys (norm may be NULL: the
- * same call).  Keys of MOSAIC_KV_Q4 caches: sines, cosines and r are rounded
- * once to fp32 (their errors before that are below 2^-34 relative), and every
- * product and sum after that is rounded on its own; the row is packed from the
- * result. */
+ * same call).  Keys of MOSAIC_KV_Q4 caches: sines and cosines (of the phase's upper 32
+ * bits) and r are rounded once to 24 bits (their errors before that are below 2^-34
+ * relative), and every product and sum after that is rounded on its own; the row is
+ * packed from the result. */
 mosaic_status mosaic_kv_append_norm(const mosaic_kv_cache *cache, const float *qkv, int64_t ldx, int64_t l,
                                     int64_t heads, const int32_t *seq, const int32_t *slot, const int32_t *index,
                                     const mosaic_rope *rope, const mosaic_head_norm *norm, float *q, int64_t ldq,

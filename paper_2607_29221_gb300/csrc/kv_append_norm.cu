@@ -73,10 +73,12 @@ __device__ __forceinline__ void spin(int32_t phase, float &cosine, float &sine) 
     if (quarter == 1 || quarter == 2) cosine = -cosine;
     if (quarter & 2) sine = -sine;
 }
-// 1 / sqrt(a), rounded once but where a is not a normal number.
+// Means of squares between these lose nothing that counts below 2^-149 and have no sum past 2^108.
+__device__ __forceinline__ bool ordinary(float mean) { return mean > 0x1p-100f && mean < 0x1p100f; }
+// 1 / sqrt(a), rounded once (ordinary a; others are zeros, infinities and NaN).
 __device__ __forceinline__ float root(Two a) {
     const float y = rsqrtf(a.h);
-    if (!(a.h > 0x1p-100f && a.h < 0x1p100f)) return y;
+    if (!ordinary(a.h)) return y;
     const float t = __fmul_rn(y, y), tl = __fmaf_rn(y, y, -t);
     const float p = __fmul_rn(a.h, t);   // near 1
     const float pl = __fmaf_rn(a.l, t, __fmaf_rn(a.h, tl, __fmaf_rn(a.h, t, -p)));
@@ -101,8 +103,8 @@ __device__ __forceinline__ float head_sum(float x, int threads) {
         if (o < threads) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
-// 1 / sqrt(mean of the head's squares + eps), rounded once.
-__device__ __forceinline__ float exact_root(const Load4 &x, const Load4 &y, bool live, int threads, const NormArgs &nm) {
+// mean of the head's squares + eps, to 2^-40.
+__device__ __forceinline__ Two exact_mean(const Load4 &x, const Load4 &y, bool live, int threads, float eps, Two over_dim) {
     Two z = {0.0f, 0.0f};
     if (live) {
 #pragma unroll
@@ -116,7 +118,25 @@ __device__ __forceinline__ float exact_root(const Load4 &x, const Load4 &y, bool
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
         if (o < threads) z = add(z, {__shfl_xor_sync(0xffffffffu, z.h, o), __shfl_xor_sync(0xffffffffu, z.l, o)});
-    return root(add(mul(z, nm.over_dim), {nm.eps, 0.0f}));
+    return add(mul(z, over_dim), {eps, 0.0f});
+}
+// A head with other than ordinary means (`far`) is scaled by the power of two that brings the larger of its channels
+// and sqrt(eps) to [1, 4): x r is the same, but for channels that then are below 2^-126.  Returns eps to that scale.
+__device__ __forceinline__ float rescale(Load4 &x, Load4 &y, bool live, bool far, int threads, float eps) {
+    float top = 0.0f;
+    if (live) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(x.x[i]), fabsf(y.x[i])));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < threads) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    top = fmaxf(top, sqrtf(eps));
+    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -126), 126);
+    const float up = far && top < __int_as_float(0x7f800000) ? __uint_as_float((uint32_t)(127 - e) << 23) : 1.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.x[i] *= up, y.x[i] *= up;
+    return eps * up * up;
 }
 template <bool kExact>
 __device__ __forceinline__ void turn(float &p, float &q, float c, float s) {
@@ -206,13 +226,29 @@ __global__ void __launch_bounds__(kThreads, kResident) append_norm_kernel(KvView
                 turn<kExact>(x.x[i], x.x[i + 1], c[i / 2], s[i / 2]), turn<kExact>(y.x[i], y.x[i + 1], c[2 + i / 2], s[2 + i / 2]);
         }
     };
-    auto fast_root = [&](const Load4 &x, const Load4 &y, bool live) {
-        float ss = 0.0f;
-        if (live) {
+    // 1 / rms of a head (`head`: one that counts; `live`: the thread has channels of it); rounded once if `exact`.
+    auto head_root = [&](Load4 &x, Load4 &y, bool head, bool live, auto exact) {
+        float eps = nm.eps;
+#pragma unroll 1
+        for (bool again = false;; again = true) {
+            Two mean;
+            if constexpr (decltype(exact)::value) {
+                mean = exact_mean(x, y, live, threads, eps, nm.over_dim);
+            } else {
+                float ss = 0.0f;
+                if (live) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ss = fmaf(x.x[i], x.x[i], fmaf(y.x[i], y.x[i], ss));
+                    for (int i = 0; i < 4; ++i) ss = fmaf(x.x[i], x.x[i], fmaf(y.x[i], y.x[i], ss));
+                }
+                mean.h = fmaf(head_sum(ss, threads), nm.over_dim.h, eps);
+            }
+            const bool far = head && !ordinary(mean.h);
+            if (again || !__any_sync(0xffffffffu, far)) {
+                if constexpr (decltype(exact)::value) return root(mean);
+                else return rsqrtf(mean.h);
+            }
+            eps = rescale(x, y, live, far, threads, eps);
         }
-        return rsqrtf(fmaf(head_sum(ss, threads), nm.over_dim.h, nm.eps));
     };
 
     for (; base < last; base += kRound * lanes) {   // the block's: shuffles and barriers inside
@@ -223,9 +259,7 @@ __global__ void __launch_bounds__(kThreads, kResident) append_norm_kernel(KvView
             const bool live = in && h < last, key = h < H + KV;
             Load4 &x = xs[k], &y = ys[k];
             if (kNorm && __any_sync(0xffffffffu, key)) {   // not a warp of values alone
-                float r;
-                if constexpr (kPacked) r = exact_root(x, y, live, threads, nm);
-                else r = fast_root(x, y, live);
+                const float r = head_root(x, y, key && h < last, live, std::integral_constant<bool, kPacked>());
                 if (live && key) scale(x, y, r, gain + D);
             }
             if (!live || id < 0) continue;
@@ -272,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, kResident) append_norm_kernel(KvView
             const bool live = in && base + k * lanes + lane < queries;
             Load4 &x = xs[k], &y = ys[k];
             if constexpr (kNorm) {
-                const float r = fast_root(x, y, live);
+                const float r = head_root(x, y, base + k * lanes + lane < queries, live, std::false_type());
                 if (live) scale(x, y, r, gain);
             }
             if (!live) continue;

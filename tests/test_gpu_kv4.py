@@ -869,3 +869,60 @@ def test_attention_of_scores_beyond_fp32(lens, heads, kv, page, sign):
     bare = type(c)(c.k, c.v, c.table, position=c.position)     # and without weights
     again = bare.attend(q, ints(lens), max(lens), first=first)
     assert torch.equal(torch.nan_to_num(again, nan=7.5), torch.nan_to_num(out, nan=7.5))
+
+
+@pytest.mark.parametrize("typ", ["q4", "f32", "bf16", "f16"])
+@pytest.mark.parametrize("eps", [0.0, 1e-6, 1e-38, 3e38])
+@pytest.mark.parametrize("dim,heads,kv,rot", [(64, 3, 2, 64), (96, 5, 3, 32), (256, 2, 1, 0), (32, 40, 8, 32)])
+def test_norms_of_heads_of_any_size(dim, heads, kv, rot, eps, typ):
+    """Heads from 2^-140 to 2^122 in one call, beside ordinary ones: what their squares are does not matter.
+    1 / rms is rounded once to 24 bits, whatever its exponent: rows of 4 bits are equal, the rest as elsewhere."""
+    from paper_2607_29221_gb300 import kvcache as KV
+    f = np.float32
+    powers = [0, -140, -126, -80, -63, -62, -50, -49, -20, 20, 49, 50, 51, 60, 63, 64, 100, 120]
+    l, rng = len(powers), np.random.default_rng(dim)
+    x = rng.standard_normal((l, heads + 2 * kv, dim)).astype(f)
+    power = np.stack([np.roll(powers, h) for h in range(heads + kv)], 1)       # a token has heads of several sizes
+    x[:, : heads + kv] = np.ldexp(x[:, : heads + kv], power[..., None].astype(np.int32))
+    x[:, : heads + kv, 1] = np.ldexp(x[:, : heads + kv, 1], -20)               # and a head channels of several
+    gains = [np.exp(rng.standard_normal(dim) / 3).astype(f) for _ in range(2)]
+    qk = x[:, : heads + kv].astype(np.float64)
+    gain = np.concatenate([np.broadcast_to(g, (n, dim)) for g, n in zip(gains, (heads, kv))])
+    # Scaled by a power of two: r keeps its 24 bits.
+    up = np.maximum(np.frexp(np.abs(qk).max(-1, keepdims=True))[1], np.frexp(np.sqrt(np.float64(f(eps))))[1] if eps else -10000)
+    near = np.ldexp(qk, -up)
+    r = 1 / np.sqrt((near * near).mean(-1, keepdims=True) + np.ldexp(np.float64(f(eps)), -2 * up))
+    ref = near * r * gain
+    y = (near * r.astype(f).astype(np.float64)).astype(f) * gain
+    rope = KV.Rope(rot, 500000.0) if rot else None
+    pos = ints(rng.integers(0, 5000, l).tolist())
+    if rot:
+        phase = (rope.turns.cpu().numpy().view(np.uint64)[:, None] * pos.cpu().numpy().astype(np.uint64)[None]) >> 32
+        angle = phase.astype(np.uint32).view(np.int32).T.astype(np.float64) * (2 * np.pi / 2 ** 32)
+        ref = spin(ref, np.cos(angle), np.sin(angle), rot, False)
+        y = spin(y, np.cos(angle).astype(f), np.sin(angle).astype(f), rot, False)
+    assert y.dtype == f
+    table = torch.arange(1, 4, dtype=torch.int32, device="cuda")[None]
+    c = KV.PagedCache.empty(4, kv, 8, dim, table, KV.INT4 if typ == "q4" else TYPES[typ])
+    at, zero = torch.arange(l, dtype=torch.int32, device="cuda"), torch.zeros(l, dtype=torch.int32, device="cuda")
+    hn = KV.HeadNorm(dim, eps, *(torch.from_numpy(g).cuda() for g in gains))
+    q = c.append(torch.from_numpy(x.reshape(l, -1)).cuda(), heads, zero, at, at, rope=rope, pos=pos if rot else None, norm=hn)
+
+    def pairs(z):
+        b = np.abs(z)
+        if rot:
+            half = b.copy()
+            b[..., : rot // 2] = b[..., rot // 2: rot] = np.sqrt(2.0) * np.hypot(half[..., : rot // 2], half[..., rot // 2: rot])
+        return b
+    # Of results near the end of fp32: a scaled channel is off by up to 2^-150, times r (at most 16 here), a gain
+    # (below 8) and two terms of a rotation; five roundings besides.
+    tiny = 2.0 ** -141
+    assert (np.abs(q.cpu().numpy() - ref[:, :heads]) <= 2.0 ** -18 * pairs(ref[:, :heads]) + tiny).all()
+    k = slots(c, c.k, 0, l).transpose(0, 1)
+    if typ == "q4":
+        assert same_bytes(k, pack(np.ascontiguousarray(y[:, heads:])), dim)
+        return
+    rel, least = {"f32": (0.0, tiny), "bf16": (2.0 ** -8, 2.0 ** -134), "f16": (2.0 ** -11, 2.0 ** -25)}[typ]
+    want = ref[:, heads:]
+    err = 2.0 ** -18 * pairs(want) + tiny
+    assert (np.abs(k.double().cpu().numpy() - want) <= err + rel * (np.abs(want) + err) + least).all()
