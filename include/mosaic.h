@@ -604,8 +604,8 @@ typedef enum { MOSAIC_KV_F32 = 0, MOSAIC_KV_BF16 = 1, MOSAIC_KV_F16 = 2, MOSAIC_
 
 /* Rows of MOSAIC_KV_Q4: head_dim (a multiple of 32) codes of 4 bits, channel c
  * in bits 4 (c % 2) of byte c / 2; then, for every 32 channels, a step and a
- * base in fp16; padded to a multiple of 16 bytes (the padding is neither read
- * nor written, but for the move of whole rows by mosaic_kv_evict).  A channel
+ * base in fp16; padded to a multiple of 16 bytes (the padding does not matter and
+ * is not written, but for the move of whole rows by mosaic_kv_evict).  A channel
  * stands for base + code step, rounded once to fp16.  A row is written from
  * fp32 channels y by IEEE operations, each rounded to nearest on its own, so
  * that its bytes do not depend on the run: y is cut to +-65000; base = the

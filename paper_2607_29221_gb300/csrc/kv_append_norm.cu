@@ -4,7 +4,7 @@
 //   y = rotate((x r) gain),  r = 1 / sqrt(mean x^2 + eps) over a head
 //
 // Bound by HBM as kv_append.cu is (fp32 rows in, fp32 queries and the cache's
-// rows out: 5003 tokens into an fp32 cache 79 us, 91% of the copy rate); the same
+// rows out: 5003 tokens into an fp32 cache 80 us, 91% of the copy rate); the same
 // split: a block the heads of one token, a thread 4 + 4 channels of a head, half a
 // head apart, two heads in flight.  The threads of a head lie in one warp (their
 // number rounded up to a power of two), which sums the squares.
@@ -20,8 +20,13 @@
 // and the rest is IEEE operations without contraction.  Doubles would do the
 // same at a sixty-fourth of the rate.  Keys and values go first and are packed by
 // all warps while the queries come (a thread a group of 32: 42 us on 2048 tokens
-// of 64 + 16 heads, two of eight warps at work; now 35 with 68% of the issue
+// of 64 + 16 heads, two of eight warps at work; now 35 with 71% of the issue
 // slots taken).
+//
+// Squares of channels past 2^-50 or 2^50 need not be fp32 numbers: a warp with a
+// head whose mean is not an ordinary one scales it by a power of two and sums
+// again (the test costs 1%: 36.9 -> 37.3 us with reading back, fp32 78.9 -> 79.9; the
+// second sum written out instead of a loop: 38.9, 80.0).
 #include "kv_append.cuh"
 
 namespace mosaic {

@@ -24,9 +24,11 @@ constexpr int kMaxGroup = 64;
 // 60, 1024: 27 / 14, 29 / 36, 83 / 96: it shares some that are faster whole.
 constexpr int64_t kWholeFew = 512, kWholeMany = 1024, kManyJobs = 128, kWholeBytes = 128 * 1024;
 // With a lower bound, 4-bit caches up to here: the split counts units that the
-// bound leaves out, and the blocks whose units are all live end last.  400
-// sequences of up to 1500, heads of 64, bound 512: 80 us shared, 71 whole; 64 of up
-// to 2000 with 64 query heads of 128, bound 300: 52, 42; 400 of up to 1500 that the bound leaves as they are 94, 108.
+// bound leaves out, and the blocks whose units are all live end last.  It is the
+// device that knows what a bound leaves out; where that is nothing, whole jobs
+// lose.  Shared / whole, us, caches flushed: 400 sequences of up to 1500, heads of 64,
+// the last 512 positions 85 / 74, all of them 103 / 115; 64 query heads of 128, 64 of
+// up to 2000, the last 300 44 / 27, all 53 / 58, 16 of them, all 35 / 33.
 constexpr int64_t kWholeBound = 2048;
 // Heads share a unit (the blocks' warps then have a head each and nothing to
 // merge) while so many jobs remain to be shared out; whole jobs while there is
@@ -40,8 +42,9 @@ constexpr int64_t kFewestJobs = 64;
 // on 8 heads of 64, windowed: 147, 122, 95, 93, 90 (256 KB).  With four heads a
 // unit 64 KB to 384 KB are within 4 and 12 per cent.
 constexpr int64_t kJobBytes = 256 * 1024;
-// Of a 4-bit cache, whose bytes take longer (32 KB, 64 KB, 128 KB, 256 KB): 48 sequences 90, 90, 95, 106; 64 of up to
-// 16384 197, 195, 196, 200; the windowed ones 111, 109, 110, 115.
+// Of a 4-bit cache, whose bytes take longer (32 KB, 64 KB, 128 KB, 256 KB; caches flushed): 48 sequences of up to 2000 on
+// 32 heads 97, 95, 99, 111, on 8 heads in pages of 20 64, 65, 65, 69; 64 of up to 16384 199, 200, 197, 202; 400 of up to
+// 1500 on 8 heads of 64, pages of 20 99, 99, 109, 118.
 constexpr int64_t kJobBytesQ4 = 64 * 1024;
 
 // Block (c, y): the job that block c's end cuts (a.by_job: job c).  Where jobs have many parts
@@ -323,8 +326,8 @@ mosaic_status mosaic_kv_attention(const mosaic_kv_cache *cache, const float *q, 
     const int64_t unit_bytes = 2 * s.unit * kv_row_bytes(cache->type, D);
     const int64_t job_bytes = cache->type == MOSAIC_KV_Q4 ? kJobBytesQ4 : kJobBytes;
     a.job_cost = (int)((job_bytes + unit_bytes / 2) / unit_bytes);
-    // A block of the join for each of a few jobs, not for each block of the kernel (131071 slots 68.9 -> 66.9
-    // us, 16384 28.7 -> 25.3).
+    // A block of the join for each of a few jobs, not for each block of the kernel (caches flushed: 131071 slots 69.3 ->
+    // 67.7 us, 16384 30.4 -> 27.3).
     a.by_job = cache->type == MOSAIC_KV_Q4 && !a.whole && jobs * 4 <= cap;
     cudaStream_t st = as_stream(stream);
     MOSAIC_TRY(by_type(cache->type, [&](auto t) { return attend_launch<decltype(t)>(*cache, a, a.blocks, st); }));

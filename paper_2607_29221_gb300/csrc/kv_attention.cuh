@@ -8,7 +8,7 @@
 // Bound by reading K and V once (8 query heads a key/value head: 8 operations
 // a byte of a 16-bit cache); the rest has to keep out of the copies' way.
 //
-//  * Two producer warps a block look pages up and fill a ring of units (16
+//  * Two producer warps a block (four where lanes copy 4-bit rows) look pages up and fill a ring of units (16
 //    rows a consumer warp, K and V) by tensor copies where rows share pages (a
 //    lane issues one in about 100 cycles, so a box is as large as a page
 //    allows: 64 x 16384 slots in pages of 16 took 436 us with one producer, 385

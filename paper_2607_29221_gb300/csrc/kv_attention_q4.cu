@@ -38,8 +38,11 @@
 namespace mosaic {
 namespace {
 
-// TMA: copies by tensor boxes, else by lanes, which takes more warps (400 x 1500
-// slots in pages of 20: 88 us with two, 78 with four).
+// TMA: copies by tensor boxes, else by lanes, which takes more warps: two / four,
+// us, caches flushed, pages of 20.  400 sequences of up to 1500 on 8 key/value
+// heads, bound 512: heads of 64 105 / 74, of 128 128 / 103; without a bound 111
+// / 99, 149 / 151.  8 query heads each of 128, 48 of up to 2000: 63 / 65, 16 of
+// up to 8000: 56 / 58.  (Four leave 128 registers, and heads of 128 spill 100 bytes.)
 template <bool TMA>
 struct Packed {};
 
@@ -510,7 +513,9 @@ __global__ void __launch_bounds__(32 * (Shape<Packed<TMA>, DP, NT>::kWarps + Sha
 
 template <int DP, int NT>
 struct Instance4 {
-    using S = Shape<Packed<true>, DP, NT>;   // units, heads and buffers are those of the other one too
+    // Units, heads and buffers are those of the other one too.  Blocks an SM are not: where lanes copy heads of 64 there
+    // are two, and the rule of heads a unit for whole jobs counts three.
+    using S = Shape<Packed<true>, DP, NT>;
     static AttendShape shape() { return {S::kHeads, DP, S::kUnit, S::kQHeads, S::kSlots, S::kBlocks}; }
     template <bool TMA>
     static mosaic_status go(const KvView &kv, AttendArgs a, const CUtensorMap &mk, const CUtensorMap &mv, int &blocks, cudaStream_t st) {

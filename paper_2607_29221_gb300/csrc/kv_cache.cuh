@@ -99,7 +99,8 @@ __device__ __forceinline__ uint32_t as_word(__half2 x) { return *reinterpret_cas
 //
 // Codes k and k + 4 (counted from the lowest) of a word as values, k = 0 .. 3,
 // packed with the lower one first.  A code or'ed into the mantissa of 1024 is
-// 1024 + code, or 1024 + 16 code: both come off exactly.
+// 1024 + code, or 1024 + 16 code: both come off exactly (Kim, Henry, Fahim and
+// Awadalla, "Who says elephants can't run", 2022, for integer weights).
 __device__ __forceinline__ void q4_values(uint32_t w, __half2 step, __half2 base, uint32_t (&y)[4]) {
     const uint32_t magic = 0x64006400u;
     const __half2 one = as_half2(0xe400e400u), part = as_half2(0x2c002c00u), rest = as_half2(0xd400d400u);   // -1024, 1/16, -64
